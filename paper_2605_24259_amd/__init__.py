@@ -85,6 +85,8 @@ def load():
         lib.rkc_query_telemetry.restype = ctypes.c_int
         lib.rkc_status_string.argtypes = [ctypes.c_int]
         lib.rkc_status_string.restype = ctypes.c_char_p
+        from . import cache
+        cache.declare(lib)
         if lib.rkc_abi_version() != ABI_VERSION:
             raise RuntimeError(f"{LIB_PATH} implements ABI {lib.rkc_abi_version()}, this binding "
                                f"ABI {ABI_VERSION}; rebuild the library")
@@ -194,3 +196,6 @@ class DeviceBatch:
 def replay(trace, stream=None):
     """Replay a trace (tracegen.Trace) on the GPU; returns host (outcomes, pool_tel, claim_tel)."""
     return DeviceBatch.from_trace(trace).replay(stream).results()
+
+
+from .cache import PagedCache  # noqa: E402  (operators on the contents of a paged KV cache)

@@ -1,0 +1,155 @@
+// rkc_attend.hip -- C ABI of the attention over a paged cache: checks, choice of kernel, join of the chunks.
+#include "rkc_cache_dev.h"
+
+namespace {
+
+// Joins the chunks of a row: one wave per packed row, D / 64 elements a lane.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_join(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+  constexpr int E = D / 64;
+  const int H = c.kv_heads, G = a.q_heads / H, per = pl.tiles * pl.rows;
+  const int64_t id = (int64_t)blockIdx.x * 4 + uni(threadIdx.x >> 6);
+  const int64_t unit = id / per;
+  const int m = (int)(id % per), s = (int)(unit / H), h = (int)(unit % H), lane = threadIdx.x & 63;
+  if (s >= c.n_seqs) return;
+  const Seq q = load_seq(c, a, s);
+  if (!q.ok || m >= q.n * G) return;
+  const int qt = m / pl.rows, last = (min(q.n * G, (qt + 1) * pl.rows) - 1) / G;
+  const int n = max(1, (rows_end(a, q, s, last) + pl.chunk - 1) / pl.chunk);
+  const int64_t at = (unit * pl.tiles + qt) * pl.splits * pl.rows + m % pl.rows;
+  const float* st = (const float*)((const char*)a.d_scratch + pl.stat_at) + at * 2;
+  const float* part = (const float*)((const char*)a.d_scratch + pl.part_at) + at * D + lane * E;
+  float top = -kInf;
+  for (int k = lane; k < n; k += 64) top = fmaxf(top, st[(int64_t)k * pl.rows * 2]);
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  float sum = 0.f, o[E] = {};
+#pragma unroll 4
+  for (int k = 0; k < n; k++) {
+    const float m_k = st[(int64_t)k * pl.rows * 2], l_k = st[(int64_t)k * pl.rows * 2 + 1];
+    const float by = m_k == -kInf ? 0.f : ex2(m_k - top);
+    sum += l_k * by;
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+      const float x = part[(int64_t)k * pl.rows * D + e];
+      o[e] += m_k == -kInf ? 0.f : x * by;
+    }
+  }
+  const float by = sum == 0.f ? 0.f : 1.f / sum;
+  const int64_t row = q.row0 + m / G, qh = h * G + m % G;
+  T* to = (T*)a.d_out + row * a.out_row_stride + qh * a.out_head_stride + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; e++) to[e] = (T)(o[e] * by);
+  if (lane == 0) a.d_lse[row * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
+}
+
+template <typename T>
+rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  const int64_t waves = (int64_t)c->n_seqs * c->kv_heads * p->tiles * p->rows;
+  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+  if (c->head_dim == 64) attend_join<T, 64><<<grid, block, 0, s>>>(*c, *a, *p);
+  else if (c->head_dim == 128) attend_join<T, 128><<<grid, block, 0, s>>>(*c, *a, *p);
+  else attend_join<T, 256><<<grid, block, 0, s>>>(*c, *a, *p);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
+bool off16(const void* p) { return (uintptr_t)p & 15; }
+bool off4(const void* p) { return (uintptr_t)p & 3; }
+// a stride whose multiple by `times` is an element offset that the kernels keep in 32 bits
+bool bad_stride(int64_t x, int64_t times) { return x < 0 || x % 8 || x > ((int64_t)1 << 30) / times; }
+constexpr int64_t kFar = (int64_t)1 << 40;  // strides between blocks and rows: products stay far below 64 bits
+
+}  // namespace
+
+rkc_status rkc_cache_check(const rkc_cache* c) {
+  if (!c) return RKC_E_NULL;
+  if (c->n_seqs < 0 || c->n_blocks < 0 || c->max_pages < 0 || c->reserved) return RKC_E_RANGE;
+  if (c->kv_heads < 1 || c->kv_heads > 1024 || c->n_seqs > 1 << 20) return RKC_E_RANGE;
+  if (c->dtype != RKC_BF16 && c->dtype != RKC_F16) return RKC_E_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return RKC_E_UNSUPPORTED;
+  if (c->page_tokens < 16 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1))) return RKC_E_UNSUPPORTED;
+  for (int64_t x : {c->k_slot_stride, c->v_slot_stride})
+    if (bad_stride(x, c->page_tokens)) return RKC_E_RANGE;
+  for (int64_t x : {c->k_block_stride, c->v_block_stride, c->k_head_stride, c->v_head_stride})
+    if (x < 0 || x % 8 || x > kFar) return RKC_E_RANGE;
+  if (c->n_seqs == 0) return RKC_OK;
+  if (!c->d_k || !c->d_v || !c->d_block_table) return RKC_E_NULL;
+  if (off16(c->d_k) || off16(c->d_v) || off4(c->d_block_table) || off4(c->d_status)) return RKC_E_ALIGN;
+  if (c->n_blocks < 1 || c->max_pages < 1) return RKC_E_RANGE;
+  return RKC_OK;
+}
+
+rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool weigh) {
+  if (rkc_status st = rkc_cache_check(c)) return st;
+  if (!a) return RKC_E_NULL;
+  if (a->n_rows < 0 || a->max_rows < 0 || a->max_len < 0 || a->reserved) return RKC_E_RANGE;
+  if (a->max_len > RKC_MAX_CACHE_LEN || a->max_len > (int64_t)c->max_pages * c->page_tokens) return RKC_E_RANGE;
+  if (a->q_heads < 1 || a->q_heads % c->kv_heads || a->q_heads > 1 << 16) return RKC_E_RANGE;
+  if ((int64_t)a->max_rows * (a->q_heads / c->kv_heads) > 1 << 30) return RKC_E_RANGE;
+  if (!(a->softcap >= 0.f) || a->softcap == kInf || a->scale != a->scale) return RKC_E_RANGE;
+  for (int64_t x : {a->q_row_stride, a->q_head_stride, a->out_row_stride, a->out_head_stride})
+    if (x < 0 || x % 8 || x > kFar) return RKC_E_RANGE;
+  if (a->d_parent && a->max_rows > RKC_MAX_TREE_ROWS) return RKC_E_UNSUPPORTED;
+  if (a->weight_seq_stride < 0 || a->weight_head_stride < 0 || a->weight_seq_stride > kFar || a->weight_head_stride > kFar) return RKC_E_RANGE;
+  if (c->n_seqs == 0 || (a->n_rows == 0 && !weigh)) return RKC_OK;
+  if (!a->d_row_offset || !a->d_length || (a->n_rows && (!a->d_q || !a->d_lse))) return RKC_E_NULL;
+  if (weigh ? !a->d_weight : !a->d_out) return RKC_E_NULL;
+  if (off16(a->d_q) || (!weigh && off16(a->d_out))) return RKC_E_ALIGN;
+  for (const void* p : {(const void*)a->d_row_offset, (const void*)a->d_length, (const void*)a->d_row_start, (const void*)a->d_prefix,
+                        (const void*)a->d_parent, (const void*)a->d_slope, (const void*)a->d_lse, (const void*)a->d_weight_in, (const void*)a->d_weight})
+    if (off4(p)) return RKC_E_ALIGN;
+  return RKC_OK;
+}
+
+// Which kernel and how a sequence is cut.  Few packed rows: the kernel that reads the cache as fast as it can;
+// more: the one that keeps the matrix units busy.  A sequence is cut where the sequences, heads and row tiles alone
+// would not fill the card's 256 CUs a few times over.
+rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
+  rkc_plan p = {};
+  const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
+  p.few = M <= 16 || (M <= 32 && c->head_dim <= 128);
+  p.rows = p.few ? (M <= 16 ? 16 : 32) : 128;
+  p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
+  const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
+  p.units = (int)units;
+  const int64_t want = p.few ? 6 * 256 : 2 * 256, grain = p.few ? 128 : 256;
+  const int64_t cut = units ? (want + units - 1) / units : 1;  // workgroups along a sequence
+  int64_t chunk = (a->max_len + cut - 1) / cut;
+  chunk = (chunk + grain - 1) / grain * grain;
+  if (chunk < grain) chunk = grain;
+  p.chunk = (int)chunk;
+  p.splits = (int)((a->max_len + chunk - 1) / chunk);
+  if (p.splits < 1) p.splits = 1;
+  if (p.splits > 1) {
+    const size_t rows = (size_t)units * p.splits * p.rows;
+    p.part_at = 0;
+    p.stat_at = rows * c->head_dim * 4;
+    p.bytes = p.stat_at + rows * 8;
+  }
+  return p;
+}
+
+extern "C" {
+
+size_t rkc_attend_scratch_bytes(const rkc_cache* c, const rkc_attention* a) {
+  if (!c || !a || c->kv_heads < 1 || a->q_heads < 1 || a->q_heads % c->kv_heads || c->n_seqs < 1 || a->max_rows < 1 || a->max_len < 1) return 0;
+  return rkc_attend_plan(c, a).bytes;
+}
+
+rkc_status rkc_attend(const rkc_cache* c, const rkc_attention* a, void* stream) {
+  if (rkc_status st = rkc_attention_check(c, a, false)) return st;
+  if (c->n_seqs == 0) return RKC_OK;
+  if (a->n_rows == 0 || a->max_rows == 0) return a->d_weight ? rkc_weigh(c, a, stream) : RKC_OK;
+  hipStream_t s = (hipStream_t)stream;
+  const rkc_plan p = rkc_attend_plan(c, a);
+  if ((int64_t)p.units * p.splits > 0x7fffffff || (int64_t)c->n_seqs * c->kv_heads * p.tiles > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  if (p.bytes) {
+    if (!a->d_scratch || a->scratch_bytes < p.bytes) return RKC_E_SCRATCH;
+    if ((uintptr_t)a->d_scratch & 255) return RKC_E_ALIGN;
+  }
+  rkc_status st = p.few ? rkc_attend_few(c, a, &p, s) : rkc_attend_tile(c, a, &p, s);
+  if (st == RKC_OK && p.splits > 1) st = c->dtype == RKC_BF16 ? join<__bf16>(c, a, &p, s) : join<_Float16>(c, a, &p, s);
+  if (st == RKC_OK && a->d_weight) st = rkc_weigh(c, a, stream);
+  return st;
+}
+
+}  // extern "C"

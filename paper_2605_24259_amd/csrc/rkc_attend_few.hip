@@ -1,0 +1,312 @@
+// rkc_attend_few.hip -- attention of few rows over a paged cache (decode steps, small trees).
+//
+// Up to 32 packed rows (rows x query heads of one key/value head) make one or two column tiles of a 16x16x32
+// matrix product, so every key and value is read once for all of them; what bounds the kernel is that read.
+// A workgroup takes a chunk of one sequence's slots for one head, its four waves take 32 slots at a time:
+//   K goes from memory straight into the product's operand (a lane holds 8 elements of its slot's key),
+//   V goes through the wave's own 32-slot tile in LDS, from where it is read transposed (no barriers),
+//   both for the next 32 slots are in flight while these are worked on.
+// Waves keep maxima, sums and outputs of their own (32 bits) and join them once at the end; chunks are joined by a
+// second kernel where a sequence has more than one.
+#include "rkc_cache_dev.h"
+
+namespace {
+
+constexpr int kWaves = 4;
+
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+  typedef typename Vec8<T>::t V8;
+  constexpr int KC = D / 32, DB = D / 16, VP = D / 16;  // key operands, output blocks, 16-byte pieces of V per lane
+  constexpr int kTile = 32 * D;                         // elements of a wave's V tile
+  constexpr int kJoin = 16 * NT * D * 4;                // bytes of a wave's output tile at the join
+  constexpr int kLds = kTile * 2 > kJoin ? kTile * 2 : kJoin;
+  __shared__ __attribute__((aligned(16))) char lds[kWaves * kLds];
+  __shared__ float stat[kWaves][16 * NT][2], total[16 * NT];
+
+  const int H = c.kv_heads, G = a.q_heads / H;
+  const int split = blockIdx.x % pl.splits, h = blockIdx.x / pl.splits % H, s = blockIdx.x / (pl.splits * H);
+  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), quad = lane >> 4, col = lane & 15;
+  const Seq q = load_seq(c, a, s);
+  if (!q.ok) {
+    if (split == 0 && h == 0 && threadIdx.x == 0) flag(c, s, RKC_CS_LENGTH);
+    return;
+  }
+  const int M = q.n * G;
+  if (!M) return;
+  const int c0 = split * pl.chunk, c1 = min(q.len, c0 + pl.chunk);
+  if (split && c0 >= q.len) return;
+  const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
+  const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
+
+  Row row[NT];
+  int qh[NT], qi[NT];
+  V8 qf[NT][KC];
+  float slope[NT];
+#pragma unroll
+  for (int t = 0; t < NT; t++) {
+    const int m = min(16 * t + col, M - 1);
+    qi[t] = m / G, qh[t] = h * G + m % G;
+    row[t] = load_row(a, q, s, qi[t]);
+    slope[t] = a.d_slope ? a.d_slope[qh[t]] * kLog2e : 0.f;
+    const T* p = (const T*)a.d_q + (q.row0 + qi[t]) * a.q_row_stride + qh[t] * a.q_head_stride + quad * 8;
+#pragma unroll
+    for (int k = 0; k < KC; k++) qf[t][k] = *(const V8*)(p + 32 * k);
+  }
+  // a tree's rows are at most 32 here: lines as bits of a register, walked through the lanes' parents
+  uint32_t line[NT] = {};
+  int depth_of = 0;  // depth of row `lane`
+  if (a.d_parent && c1 > q.base) {
+    int par = -1;
+    if (lane < q.n) {
+      par = a.d_parent[q.row0 + lane];
+      if (par < -1 || par >= lane) {
+        flag(c, s, RKC_CS_PARENT);
+        par = -1;
+      }
+    }
+    uint32_t mine = lane < 32 ? 1u << lane : 0;
+    for (int at = par; __any(at >= 0);) {
+      const int up = __shfl(par, at & 63);
+      if (at >= 0) mine |= 1u << at, at = up;
+    }
+    depth_of = __popc(mine) - 1;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      line[t] = (uint32_t)__shfl((int)mine, qi[t]);
+      row[t].pos = q.base + __shfl(depth_of, qi[t]);
+    }
+  } else if (a.d_parent && a.d_slope) {
+    // distances need the rows' depths in every chunk
+    int par = lane < q.n ? a.d_parent[q.row0 + lane] : -1;
+    if (par < -1 || par >= lane) par = -1;
+    int d = 0;
+    for (int at = par; __any(at >= 0);) {
+      const int up = __shfl(par, at & 63);
+      if (at >= 0) d++, at = up;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; t++) row[t].pos = q.base + __shfl(d, qi[t]);
+  }
+  // slots that all rows see, and slots that any sees
+  int all_from = row[0].start, all_to = row[0].end, all_pre = row[0].prefix, any_from = row[0].start;
+  int any_to = max(row[0].end, row[0].prefix);
+#pragma unroll
+  for (int t = 1; t < NT; t++) {
+    all_from = max(all_from, row[t].start), all_to = min(all_to, row[t].end), any_from = min(any_from, row[t].start);
+    any_to = max(any_to, max(row[t].end, row[t].prefix));
+  }
+  all_from = wave_max(all_from), all_to = wave_min(all_to), any_from = wave_min(any_from), any_to = wave_max(any_to);
+  all_pre = uni(all_pre);
+  if (a.d_parent) any_to = q.len;
+  const int end = min(c1, any_to);  // of what is looked at here: a chunk is a multiple of 32 slots
+
+  const float mul = a.softcap > 0.f ? a.scale / a.softcap * 2.f * kLog2e : a.scale * kLog2e;
+  const float cap = a.softcap * kLog2e;
+  const T* kp = (const T*)c.d_k + h * c.k_head_stride;
+  const T* vp = (const T*)c.d_v + h * c.v_head_stride;
+  T* tile = (T*)(lds + wave * kLds);
+
+  float top[NT], sum[NT];
+  f32x4 o[NT][DB];
+#pragma unroll
+  for (int t = 0; t < NT; t++) {
+    top[t] = -kInf, sum[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; d++) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  V8 kf[2][KC];
+  u32x4 vf[VP];
+  // the 32 slots from t0 on: two runs of 16, each within a page; a run behind the chunk repeats the first
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      const int at = u && t0 + 16 >= end ? t0 : t0 + 16 * u;
+      const int64_t page = page_of(c, table, shift, at, s);
+      const T* kb = kp + page * c.k_block_stride + (at & in_page) * c.k_slot_stride;
+      const T* vb = vp + page * c.v_block_stride + (at & in_page) * c.v_slot_stride;
+#pragma unroll
+      for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + (int)(col * (int)c.k_slot_stride) + quad * 8 + 32 * k);
+#pragma unroll
+      for (int p = 0; p < VP / 2; p++) {
+        const int piece = p * 64 + lane, r = piece / (D / 8), e = piece % (D / 8) * 8;
+        vf[u * (VP / 2) + p] = *(const u32x4*)(vb + (int)(r * (int)c.v_slot_stride) + e);
+      }
+    }
+  };
+
+  const int step = 32 * kWaves;
+  int t0 = c0 + 32 * wave;
+  auto skip = [&](int t) { return t + 32 <= any_from && t >= all_pre; };  // no row sees anything there
+  while (t0 < end && skip(t0)) t0 += step;
+  if (t0 < end) load(t0);
+  while (t0 < end) {
+    f32x4 sc[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; t++)
+#pragma unroll
+      for (int u = 0; u < 2; u++) {
+        sc[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KC; k++) sc[t][u] = mma16(kf[u][k], qf[t][k], sc[t][u]);
+      }
+    const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
+    bool hurt = false;
+#pragma unroll
+    for (int p = 0; p < VP; p++) {
+      const int piece = (p % (VP / 2)) * 64 + lane, r = p / (VP / 2) * 16 + piece / (D / 8), j = t0 + r;
+      u32x4 x = vf[p];
+      if (!whole) {
+        if (j >= end || (j < any_from && j >= all_pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
+        hurt |= any_hurt<T>(x);
+      }
+      *(u32x4*)(tile + tile_at<D>(r, piece % (D / 8))) = x;
+    }
+    hurt = __any(hurt);
+    int next = t0 + step;
+    while (next < end && skip(next)) next += step;
+    if (next < end) load(next);
+
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      float x[8];
+      V8 seen_by;
+#pragma unroll
+      for (int e = 0; e < 8; e++) x[e] = sc[t][e >> 2][e & 3] * mul;
+      if (a.softcap > 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[e] = cap - 2.f * cap * __builtin_amdgcn_rcpf(ex2(x[e]) + 1.f);
+      }
+      const int j0 = t0 + quad * 4;  // of x[0..3]; x[4..7] are 16 further
+      if (a.d_slope) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          int j = j0 + (e >> 2) * 16 + (e & 3);
+          if (a.d_parent && t0 + 32 > q.base) {
+            const int d = __shfl(depth_of, (j - q.base) & 63);
+            j = j >= q.base ? q.base + d : j;
+          }
+          x[e] -= slope[t] * fabsf((float)(row[t].pos - j));
+        }
+      }
+      if (!whole) {
+        const int from = t0 - q.base;
+        const uint32_t seen = from >= 32 || from <= -32 ? 0 : from >= 0 ? line[t] >> from : line[t] << -from;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const int off = quad * 4 + (e >> 2) * 16 + (e & 3), j = t0 + off;
+          const bool see = (j >= row[t].start && j < row[t].end) || j < row[t].prefix || (seen >> off & 1);
+          x[e] = see ? x[e] : -kInf;
+          seen_by[e] = (T)(see ? 1.f : 0.f);
+        }
+      }
+      float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      most = max32(max16(most));
+      if (__any(most > top[t])) {
+        const float now = fmaxf(top[t], most), by = now == -kInf ? 1.f : ex2(top[t] - now);
+        top[t] = now, sum[t] *= by;
+#pragma unroll
+        for (int d = 0; d < DB; d++) o[t][d] *= by;
+      }
+      const float m = top[t] == -kInf ? 0.f : top[t];
+      f32x8 p;
+#pragma unroll
+      for (int e = 0; e < 8; e++) p[e] = ex2(x[e] - m);
+      sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
+      const V8 pb = __builtin_convertvector(p, V8);
+#pragma unroll
+      for (int d = 0; d < DB; d++) {
+        const int r = quad * 4 + (col >> 2), ch = d * 2 + ((col & 3) >> 1), e = (col & 1) * 4;
+        V8 vt = read_tr2<T>(tile + tile_at<D>(r, ch) + e, tile + tile_at<D>(r + 16, ch) + e);
+        if (hurt) {
+          const f32x4 n = mma16(strip<T>(vt), seen_by, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int k = 0; k < 4; k++) o[t][d][k] += hurt_by(n[k]);
+        }
+        o[t][d] = mma16(vt, pb, o[t][d]);
+      }
+    }
+    t0 = next;
+  }
+
+  // join the waves
+#pragma unroll
+  for (int t = 0; t < NT; t++) {
+    sum[t] = sum32(sum16(sum[t]));
+    if (quad == 0) stat[wave][16 * t + col][0] = top[t], stat[wave][16 * t + col][1] = sum[t];
+  }
+  __syncthreads();
+  float m_all[NT], l_all[NT];
+#pragma unroll
+  for (int t = 0; t < NT; t++) {
+    float m = -kInf, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) m = fmaxf(m, stat[w][16 * t + col][0]);
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) {
+      const float x = stat[w][16 * t + col][0];
+      l += x == -kInf ? 0.f : stat[w][16 * t + col][1] * ex2(x - m);
+    }
+    m_all[t] = m, l_all[t] = l;
+    const float by = top[t] == -kInf ? 0.f : ex2(top[t] - m);
+    float* to = (float*)(lds + wave * kLds) + (16 * t + col) * D + quad * 4;
+#pragma unroll
+    for (int d = 0; d < DB; d++) {
+      f32x4 x = o[t][d] * by;
+      // 16 rows of D floats: rotated so that the rows' 16-byte pieces do not share banks
+      *(f32x4*)(to + 16 * ((d + col) % DB)) = top[t] == -kInf ? f32x4{0.f, 0.f, 0.f, 0.f} : x;
+    }
+  }
+  const int unit = s * H + h;
+  if (wave == 0 && quad == 0) {
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      const int m = 16 * t + col;
+      if (pl.splits == 1) {
+        if (m < M) a.d_lse[(int64_t)(q.row0 + qi[t]) * a.q_heads + qh[t]] = l_all[t] > 0.f || l_all[t] != l_all[t] ? kLn2 * (m_all[t] + lg2(l_all[t])) : -kInf;
+      } else {
+        float* st = (float*)((char*)a.d_scratch + pl.stat_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + m) * 2;
+        st[0] = m_all[t], st[1] = l_all[t];
+      }
+      total[m] = l_all[t];
+    }
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < min(16 * NT, M) * (D / 4); x += 64 * kWaves) {
+    const int m = x / (D / 4), b = x % (D / 4), d = b >> 2;
+    const float* from = (const float*)lds + m * D + 16 * ((d + (m & 15)) % DB) + (b & 3) * 4;
+    f32x4 y = *(const f32x4*)from;
+#pragma unroll
+    for (int w = 1; w < kWaves; w++) y += *(const f32x4*)((const char*)from + w * kLds);
+    if (pl.splits == 1) {
+      const float l = total[m];
+      const float by = l == 0.f ? 0.f : 1.f / l;
+      T* to = (T*)a.d_out + (q.row0 + m / G) * a.out_row_stride + (h * G + m % G) * a.out_head_stride + b * 4;
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      *(T4*)to = __builtin_convertvector(y * by, T4);
+    } else {
+      *(f32x4*)((float*)((char*)a.d_scratch + pl.part_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + m) * D + b * 4) = y;
+    }
+  }
+}
+
+template <typename T, int D>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  const dim3 grid(p->units * p->splits), block(64 * kWaves);
+  if (p->rows == 16) attend_few<T, D, 1><<<grid, block, 0, s>>>(*c, *a, *p);
+  else attend_few<T, D, 2><<<grid, block, 0, s>>>(*c, *a, *p);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
+template <typename T>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  return c->head_dim == 64 ? go<T, 64>(c, a, p, s) : c->head_dim == 128 ? go<T, 128>(c, a, p, s) : go<T, 256>(c, a, p, s);
+}
+
+}  // namespace
+
+rkc_status rkc_attend_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  return c->dtype == RKC_BF16 ? go<__bf16>(c, a, p, s) : go<_Float16>(c, a, p, s);
+}

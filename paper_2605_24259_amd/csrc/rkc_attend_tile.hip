@@ -1,0 +1,260 @@
+// rkc_attend_tile.hip -- attention of many rows over a paged cache (chunks of prompts, larger trees).
+//
+// A workgroup holds 128 packed rows (rows x query heads of one key/value head), 32 of them in each of its four
+// waves as columns of 32x32x16 matrix products, and goes over the slots that any of them sees in tiles of 64 (32
+// at 256 elements a head).  K and V of the next tile travel through registers into the other half of LDS while this
+// one is worked on; one barrier a tile.  Tiles that every row sees skip the masks, waves whose rows see nothing of a
+// tile skip it.  What bounds it: matrix products and the exponentials between them, which take about as long.
+#include "rkc_cache_dev.h"
+
+namespace {
+
+constexpr int kRows = 128, kThreads = 256;
+static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+  typedef typename Vec8<T>::t V8;
+  constexpr int BK = D == 256 ? 32 : 64, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
+  constexpr int P = BK * CH / kThreads;  // 16-byte pieces of K, and of V, per thread
+  constexpr int kTile = BK * D;
+  __shared__ __attribute__((aligned(16))) T lds[4 * kTile];  // K, V of two tiles
+  __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
+  __shared__ int depths[RKC_MAX_TREE_ROWS], lim[4][4], hurt_at[2];
+
+  const int H = c.kv_heads, G = a.q_heads / H;
+  int b = blockIdx.x;
+  const int h = b % H;
+  b /= H;
+  const int split = b % pl.splits;
+  b /= pl.splits;
+  const int qt = pl.tiles - 1 - b % pl.tiles, s = b / pl.tiles;  // the rows that see most go first
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5, col = lane & 31;
+  const Seq q = load_seq(c, a, s);
+  if (!q.ok) {
+    if (split == 0 && h == 0 && b % pl.tiles == 0 && tid == 0) flag(c, s, RKC_CS_LENGTH);
+    return;
+  }
+  const int M = q.n * G, m0 = qt * kRows;
+  if (m0 >= M) return;
+  const int last = (min(M, m0 + kRows) - 1) / G;
+  const int c0 = split * pl.chunk, c1 = min(rows_end(a, q, s, last), c0 + pl.chunk);
+  if (split && c0 >= c1) return;
+  const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
+  const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
+
+  const int m = min(m0 + 32 * wave + col, M - 1), qi = m / G, qh = h * G + m % G;
+  const bool mine = m0 + 32 * wave + col < M;
+  Row row = load_row(a, q, s, qi);
+  const float slope = a.d_slope ? a.d_slope[qh] * kLog2e : 0.f;
+  V8 qf[KC];
+  {
+    const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + half * 8;
+#pragma unroll
+    for (int k = 0; k < KC; k++) qf[k] = *(const V8*)(p + 16 * k);
+  }
+  const bool tree = a.d_parent != nullptr, drafts = tree && c1 > q.base;
+  if (drafts || (tree && a.d_slope)) {
+    tree_lines(c, a, q, s, split == 0 && h == 0 && qt == 0, lines, depths);
+    row.pos = q.base + depths[qi];
+  }
+  // slots that all of the wave's rows see, and slots that any of them, and of the workgroup's, sees
+  const int all_from = wave_max(row.start), all_to = wave_min(row.end), pre = uni(row.prefix);
+  const int any_from = wave_min(row.start), any_to = tree ? q.len : max(pre, wave_max(row.end));
+  if (lane == 0) lim[wave][0] = all_from, lim[wave][1] = all_to, lim[wave][2] = any_from, lim[wave][3] = any_to;
+  if (tid < 2) hurt_at[tid] = -1;
+  __syncthreads();
+  const int g_all_from = max(max(lim[0][0], lim[1][0]), max(lim[2][0], lim[3][0]));
+  const int g_all_to = min(min(lim[0][1], lim[1][1]), min(lim[2][1], lim[3][1]));
+  const int g_any_from = min(min(lim[0][2], lim[1][2]), min(lim[2][2], lim[3][2]));
+  const int g_any_to = max(max(lim[0][3], lim[1][3]), max(lim[2][3], lim[3][3]));
+  const int end = min(c1, g_any_to);
+
+  const float mul = a.softcap > 0.f ? a.scale / a.softcap * 2.f * kLog2e : a.scale * kLog2e;
+  const float cap = a.softcap * kLog2e;
+  const T* kp = (const T*)c.d_k + h * c.k_head_stride;
+  const T* vp = (const T*)c.d_v + h * c.v_head_stride;
+
+  float top = -kInf, sum = 0.f;
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; d++)
+#pragma unroll
+    for (int k = 0; k < 16; k++) o[d][k] = 0.f;
+
+  u32x4 ks[P], vs[P];
+  // this thread's pieces of the tile at t0: a wave's pieces lie in rows of one page
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+      const int piece = p * kThreads + tid, r = piece / CH, e = piece % CH * 8;
+      int at = t0 + uni(r & ~15);
+      at = at < end ? at : t0;  // a run of 16 behind the end repeats the first one
+      const int64_t page = page_of(c, table, shift, at, s);
+      ks[p] = *(const u32x4*)(kp + page * c.k_block_stride + (at & in_page) * c.k_slot_stride + (int)((r & 15) * (int)c.k_slot_stride) + e);
+      vs[p] = *(const u32x4*)(vp + page * c.v_block_stride + (at & in_page) * c.v_slot_stride + (int)((r & 15) * (int)c.v_slot_stride) + e);
+    }
+  };
+  auto store = [&](int t0, int buf) {
+    T* to = lds + buf * 2 * kTile;
+    const bool whole = t0 + BK <= pre || (t0 >= g_all_from && t0 + BK <= g_all_to);
+    bool bad = false;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+      const int piece = p * kThreads + tid, r = piece / CH, j = t0 + r;
+      u32x4 x = vs[p];
+      if (!whole) {
+        if (j >= end || (j < g_any_from && j >= pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
+        bad |= any_hurt<T>(x);
+      }
+      *(u32x4*)(to + tile_at<D>(r, piece % CH)) = ks[p];
+      *(u32x4*)(to + kTile + tile_at<D>(r, piece % CH)) = x;
+    }
+    if (bad) hurt_at[buf] = t0;
+  };
+  auto skip = [&](int t) { return t + BK <= g_any_from && t >= pre; };
+
+  int t0 = c0, buf = 0;
+  while (t0 < end && skip(t0)) t0 += BK;
+  if (t0 < end) {
+    load(t0);
+    store(t0, 0);
+  }
+  __syncthreads();
+  while (t0 < end) {
+    int next = t0 + BK;
+    while (next < end && skip(next)) next += BK;
+    if (next < end) load(next);
+    const T* kt_ = lds + buf * 2 * kTile;
+    const T* vt_ = kt_ + kTile;
+    // whether any of the wave's rows sees anything of the tile, and whether all see all of it
+    if ((t0 + BK > any_from && t0 < any_to) || t0 < pre) {
+      const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
+      const bool hurt = hurt_at[buf] == t0;
+      f32x16 sc[KT];
+#pragma unroll
+      for (int u = 0; u < KT; u++) {
+#pragma unroll
+        for (int k = 0; k < 16; k++) sc[u][k] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KC; k++) sc[u] = mma32(*(const V8*)(kt_ + tile_at<D>(32 * u + col, 2 * k + half)), qf[k], sc[u]);
+      }
+      uint32_t seen[KT];
+      float most = -kInf;
+#pragma unroll
+      for (int u = 0; u < KT; u++) {
+#pragma unroll
+        for (int k = 0; k < 16; k++) sc[u][k] *= mul;
+        if (a.softcap > 0.f) {
+#pragma unroll
+          for (int k = 0; k < 16; k++) sc[u][k] = cap - 2.f * cap * __builtin_amdgcn_rcpf(ex2(sc[u][k]) + 1.f);
+        }
+        const int j0 = t0 + 32 * u;
+        if (a.d_slope) {
+#pragma unroll
+          for (int k = 0; k < 16; k++) {
+            int j = j0 + (k & 3) + 8 * (k >> 2) + 4 * half;
+            if (drafts && j >= q.base) j = q.base + depths[min(j - q.base, RKC_MAX_TREE_ROWS - 1)];
+            sc[u][k] -= slope * fabsf((float)(row.pos - j));
+          }
+        }
+        if (!whole) {
+          const uint32_t line = drafts ? line_window(lines[qi], 4, j0 - q.base) : 0;
+          uint32_t bits = 0;
+#pragma unroll
+          for (int k = 0; k < 16; k++) {
+            const int off = (k & 3) + 8 * (k >> 2) + 4 * half, j = j0 + off;
+            const bool see = (j >= row.start && j < row.end) || j < row.prefix || (line >> off & 1);
+            sc[u][k] = see ? sc[u][k] : -kInf;
+            bits |= (see ? 1u : 0u) << k;
+          }
+          seen[u] = bits;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; k++) most = fmaxf(most, sc[u][k]);
+      }
+      most = max32(most);
+      // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+      if (__any(most > top + 8.f)) {
+        const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
+        top = now, sum *= by;
+#pragma unroll
+        for (int d = 0; d < DB; d++) o[d] *= by;
+      }
+      const float mx = top == -kInf ? 0.f : top;
+#pragma unroll
+      for (int u = 0; u < KT; u++) {
+#pragma unroll
+        for (int v = 0; v < 2; v++) {
+          f32x8 p;
+#pragma unroll
+          for (int k = 0; k < 8; k++) p[k] = ex2(sc[u][8 * v + k] - mx);
+          sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+          // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
+          const V8 pb = __builtin_convertvector(p, V8);
+          const int i = lane & 15, r = 32 * u + 16 * v + 4 * half + (i >> 2), ch = (lane >> 4 & 1) * 2 + ((i & 3) >> 1), e = (i & 1) * 4;
+#pragma unroll
+          for (int d = 0; d < DB; d++) {
+            V8 vt = read_tr2<T>(vt_ + tile_at<D>(r, 4 * d + ch) + e, vt_ + tile_at<D>(r + 8, 4 * d + ch) + e);
+            if (hurt && !whole) {
+              V8 by;
+#pragma unroll
+              for (int k = 0; k < 8; k++) by[k] = (T)(seen[u] >> (8 * v + k) & 1 ? 1.f : 0.f);
+              f32x16 n;
+#pragma unroll
+              for (int k = 0; k < 16; k++) n[k] = 0.f;
+              n = mma32(strip<T>(vt), by, n);
+#pragma unroll
+              for (int k = 0; k < 16; k++) o[d][k] += hurt_by(n[k]);
+            }
+            o[d] = mma32(vt, pb, o[d]);
+          }
+        }
+      }
+    }
+    buf ^= 1;
+    if (next < end) store(next, buf);
+    __syncthreads();
+    t0 = next;
+  }
+
+  sum = sum32(sum);
+  if (!mine) return;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  if (pl.splits == 1) {
+    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    T* to = (T*)a.d_out + (q.row0 + qi) * a.out_row_stride + qh * a.out_head_stride + 4 * half;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        f32x4 x = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * by;
+        *(T4*)(to + 32 * d + 8 * k) = __builtin_convertvector(x, T4);
+      }
+    if (half == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
+  } else {
+    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + 32 * wave + col;
+    float* to = (float*)((char*)a.d_scratch + pl.part_at) + at * D + 4 * half;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+      for (int k = 0; k < 4; k++) *(f32x4*)(to + 32 * d + 8 * k) = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
+    float* st = (float*)((char*)a.d_scratch + pl.stat_at) + at * 2;
+    if (half == 0) st[0] = top, st[1] = sum;
+  }
+}
+
+template <typename T>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  const dim3 grid(p->units * p->splits), block(kThreads);
+  if (c->head_dim == 64) attend_tile<T, 64><<<grid, block, 0, s>>>(*c, *a, *p);
+  else if (c->head_dim == 128) attend_tile<T, 128><<<grid, block, 0, s>>>(*c, *a, *p);
+  else attend_tile<T, 256><<<grid, block, 0, s>>>(*c, *a, *p);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
+}  // namespace
+
+rkc_status rkc_attend_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  return c->dtype == RKC_BF16 ? go<__bf16>(c, a, p, s) : go<_Float16>(c, a, p, s);
+}

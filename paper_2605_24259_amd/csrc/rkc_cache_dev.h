@@ -1,0 +1,241 @@
+// rkc_cache_dev.h -- what the kernels on a paged KV cache share: matrix instructions over both types, the
+// layout of a tile in LDS, and what a row of a query sees.
+//
+// All of them compute scores transposed, S^T = K Q^T, so that a query row is a lane's column: its softmax
+// statistics are one register per lane, a rescale of the output is one multiplication per register, and the
+// probabilities come out of the first product in the layout in which the second one, O^T = V^T P^T, reads them.
+// The sum over slots may take the slots in any order as long as V^T has the same: V goes through LDS and is
+// read by transposing loads in that order.
+#ifndef RKC_CACHE_DEV_H
+#define RKC_CACHE_DEV_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "rkc_cache.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kInf = __builtin_inff();
+
+template <typename T> struct Vec8;
+template <> struct Vec8<__bf16> { typedef bf16x8 t; };
+template <> struct Vec8<_Float16> { typedef f16x8 t; };
+
+__device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// exp2 and log2 of the hardware (within one unit of the last place; below the smallest normal result: 0)
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float lg2(float x) { return __builtin_amdgcn_logf(x); }
+
+// Of lanes l and l ^ 16 (l ^ 32): both values, in an order that all lanes agree on up to a swap.
+__device__ __forceinline__ void pair16(float x, float& a, float& b) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void pair32(float x, float& a, float& b) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max16(float x) { float a, b; pair16(x, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float max32(float x) { float a, b; pair32(x, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float sum16(float x) { float a, b; pair16(x, a, b); return a + b; }
+__device__ __forceinline__ float sum32(float x) { float a, b; pair32(x, a, b); return a + b; }
+
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int wave_min(int x) {
+  for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d));
+  return uni(x);
+}
+__device__ __forceinline__ int wave_max(int x) {
+  for (int d = 32; d; d >>= 1) x = max(x, __shfl_xor(x, d));
+  return uni(x);
+}
+
+// A tile of slots in LDS: rows of D elements in 16-byte chunks, the chunk's number xored with a number of
+// the row so that neither a column of chunks over 16 rows (keys) nor 32 bytes of 4, 8 or 16 neighbouring rows
+// (transposing reads of values) share banks.  Element offset of chunk `c` of row `r`.
+template <int D> __device__ __forceinline__ int tile_at(int r, int c) {
+  const int x = D == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
+  return r * D + ((c ^ x) << 3);
+}
+
+// 4 slots x 16 columns, transposed within each 16 lanes: lane i gets column i of the 4 slots whose addresses
+// lanes 4 s .. 4 s + 3 give (8 bytes each).
+__device__ __forceinline__ s16x4 read_tr(const void* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+}
+
+template <typename T> __device__ __forceinline__ typename Vec8<T>::t read_tr2(const T* a, const T* b) {
+  const s16x4 x = read_tr(a), y = read_tr(b);
+  const s16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(typename Vec8<T>::t, z);
+}
+
+// Values that are not finite must not reach the rows that do not see their slot, where a product would meet them
+// with a weight of zero.  Tiles that have such values and are not seen whole (`hurt`) are multiplied with them
+// replaced by zeros, and once more with a code in their place against "seen" in place of the weights; the counts
+// in that sum say what the rows get.
+template <typename T> struct Bits;
+template <> struct Bits<__bf16> { static constexpr uint16_t e = 0x7f80; };
+template <> struct Bits<_Float16> { static constexpr uint16_t e = 0x7c00; };
+
+template <typename T> __device__ __forceinline__ bool any_hurt(u32x4 x) {
+  bool bad = false;
+  constexpr uint32_t m = Bits<T>::e;
+#pragma unroll
+  for (int k = 0; k < 4; k++) bad |= (x[k] & m) == m || (x[k] & m << 16) == m << 16;
+  return bad;
+}
+
+// Zeroes what is not finite in v; returns 1 for each NaN, 128 for each infinity, 16384 for each negative one.
+template <typename T> __device__ __forceinline__ typename Vec8<T>::t strip(typename Vec8<T>::t& v) {
+  s16x8 b = __builtin_bit_cast(s16x8, v);
+  typename Vec8<T>::t code;
+#pragma unroll
+  for (int k = 0; k < 8; k++) {
+    const uint16_t w = (uint16_t)b[k];
+    const bool bad = (w & Bits<T>::e) == Bits<T>::e;
+    code[k] = (T)(!bad ? 0.f : (w & 0x7fff) != Bits<T>::e ? 1.f : w >> 15 ? 16384.f : 128.f);
+    if (bad) b[k] = 0;
+  }
+  v = __builtin_bit_cast(typename Vec8<T>::t, b);
+  return code;
+}
+
+// What a sum of codes over at most 64 slots adds to an output.
+__device__ __forceinline__ float hurt_by(float codes) {
+  const int n = (int)codes;
+  float x = n & 127 ? __builtin_nanf("") : 0.f;
+  if (n >> 7 & 127) x += kInf;
+  if (n >> 14) x -= kInf;
+  return x;
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// What a row sees.  Slots [start, end) and [0, prefix), and of a tree's drafted slots those of `line`.
+struct Row {
+  int start, end, prefix;
+  int pos;  // position that distances are counted from
+};
+
+struct Seq {
+  int row0, n, len, base;  // base: the slot of the first row
+  bool ok;
+};
+
+// Reads and checks a sequence's row range and length.
+__device__ __forceinline__ Seq load_seq(const rkc_cache& c, const rkc_attention& a, int s) {
+  Seq q;
+  const int r0 = a.d_row_offset[s], r1 = a.d_row_offset[s + 1];
+  q.row0 = r0, q.n = r1 - r0, q.len = a.d_length[s], q.base = q.len - q.n;
+  q.ok = r0 >= 0 && r1 >= r0 && r1 <= a.n_rows && q.n <= a.max_rows && q.len >= 0 && q.len <= a.max_len && q.n <= q.len;
+  return q;
+}
+
+__device__ __forceinline__ void flag(const rkc_cache& c, int s, int bit) {
+  if (c.d_status) atomicOr(c.d_status + s, bit);
+}
+
+__device__ __forceinline__ Row load_row(const rkc_attention& a, const Seq& q, int s, int i) {
+  Row r;
+  r.start = a.d_row_start ? max(0, a.d_row_start[q.row0 + i]) : 0;
+  r.end = a.d_parent ? q.base : q.base + i + 1;
+  r.prefix = a.d_prefix ? max(0, min(a.d_prefix[s], a.d_parent ? q.base : q.len)) : 0;
+  r.pos = q.base + i;
+  return r;
+}
+
+// Lines of a tree of at most RKC_MAX_TREE_ROWS rows, by a workgroup of as many threads: every row joins the line
+// of the row that its own line ends at, until all end at a root.  On return depths holds the rows' depths.
+__device__ __forceinline__ void tree_lines(const rkc_cache& c, const rkc_attention& a, const Seq& q, int s, bool tell, uint64_t (*lines)[4], int* depths) {
+  const int tid = threadIdx.x;
+  uint64_t w[4] = {};
+  int up = -1;
+  if (tid < q.n) {
+    up = a.d_parent[q.row0 + tid];
+    if (up < -1 || up >= tid) {
+      if (tell) flag(c, s, RKC_CS_PARENT);
+      up = -1;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k++) w[k] = tid >> 6 == k ? 1ull << (tid & 63) : 0;
+  }
+  for (int reach = 1;; reach *= 2) {
+#pragma unroll
+    for (int k = 0; k < 4; k++) lines[tid][k] = w[k];
+    depths[tid] = up;
+    __syncthreads();
+    if (reach >= q.n) break;
+    if (up >= 0) {
+#pragma unroll
+      for (int k = 0; k < 4; k++) w[k] |= lines[up][k];
+      up = depths[up];
+    }
+    __syncthreads();
+  }
+  depths[tid] = __popcll(w[0]) + __popcll(w[1]) + __popcll(w[2]) + __popcll(w[3]) - 1;
+  __syncthreads();
+}
+
+// Bits of `line` (bit d: drafted row d) for the 32 slots from t0 on.
+__device__ __forceinline__ uint32_t line_window(const uint64_t* line, int words, int from) {
+  if (from <= -32 || from >= 64 * words) return 0;
+  if (from < 0) return (uint32_t)(line[0] << -from);
+  const int w = from >> 6, sh = from & 63;
+  uint64_t x = line[w] >> sh;
+  if (sh > 32 && w + 1 < words) x |= line[w + 1] << (64 - sh);
+  return (uint32_t)x;
+}
+
+// The end of the slots that the tile's rows up to `last` see.
+__device__ __forceinline__ int rows_end(const rkc_attention& a, const Seq& q, int s, int last) {
+  if (a.d_parent) return q.len;
+  const int pre = a.d_prefix ? max(0, min(a.d_prefix[s], q.len)) : 0;
+  return max(pre, q.base + last + 1);
+}
+
+// Block of the page that slot t lies in (block 0 for an id outside the pool, which sets the status).
+__device__ __forceinline__ int64_t page_of(const rkc_cache& c, const int32_t* table, int shift, int t, int s) {
+  const int id = table[t >> shift];
+  if ((uint32_t)id >= (uint32_t)c.n_blocks) {
+    flag(c, s, RKC_CS_BLOCK);
+    return 0;
+  }
+  return id;
+}
+
+}  // namespace
+
+// Host side: what every call checks.
+rkc_status rkc_cache_check(const rkc_cache* c);
+rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool weigh);
+
+// Entry of the two attention kernels: one for up to 32 packed rows (rows x query heads of a key/value head) of a
+// sequence, one for tiles of 128; chunk: slots per workgroup, splits: workgroups along a sequence.
+struct rkc_plan {
+  bool few;
+  int units;   // sequences x key/value heads x row tiles
+  int tiles;   // row tiles per sequence and head
+  int rows;    // packed rows of a tile
+  int chunk, splits;
+  size_t part_at, stat_at, bytes;  // scratch: partial outputs, their maxima and sums, in all
+};
+rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a);
+rkc_status rkc_attend_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
+rkc_status rkc_attend_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
+
+#endif
