@@ -15,7 +15,7 @@ namespace {
 constexpr int kWaves = 4;
 
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+__global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int KC = D / 32, DB = D / 16, VP = D / 16;  // key operands, output blocks, 16-byte pieces of V per lane
   constexpr int kTile = 32 * D;                         // elements of a wave's V tile
@@ -39,6 +39,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
+  const Scale f = load_scale(a);
   Row row[NT];
   int qh[NT], qi[NT];
   V8 qf[NT][KC];
@@ -48,10 +49,13 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
     const int m = min(16 * t + col, M - 1);
     qi[t] = m / G, qh[t] = h * G + m % G;
     row[t] = load_row(a, q, s, qi[t]);
-    slope[t] = a.d_slope ? a.d_slope[qh[t]] * kLog2e : 0.f;
+    slope[t] = a.d_slope ? a.d_slope[qh[t]] * kLog2e / f.post : 0.f;
     const T* p = (const T*)a.d_q + (q.row0 + qi[t]) * a.q_row_stride + qh[t] * a.q_head_stride + quad * 8;
 #pragma unroll
-    for (int k = 0; k < KC; k++) qf[t][k] = *(const V8*)(p + 32 * k);
+    for (int k = 0; k < KC; k++) {
+      qf[t][k] = *(const V8*)(p + 32 * k);
+      if (f.negate) qf[t][k] = negated(qf[t][k]);
+    }
   }
   // a tree's rows are at most 32 here: lines as bits of a register, walked through the lanes' parents
   uint32_t line[NT] = {};
@@ -101,8 +105,6 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
   if (a.d_parent) any_to = q.len;
   const int end = min(c1, any_to);  // of what is looked at here: a chunk is a multiple of 32 slots
 
-  const float mul = a.softcap > 0.f ? a.scale / a.softcap * 2.f * kLog2e : a.scale * kLog2e;
-  const float cap = a.softcap * kLog2e;
   const T* kp = (const T*)c.d_k + h * c.k_head_stride;
   const T* vp = (const T*)c.d_v + h * c.v_head_stride;
   T* tile = (T*)(lds + wave * kLds);
@@ -118,12 +120,13 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
 
   V8 kf[2][KC];
   u32x4 vf[VP];
+  bool bad = false;
   // the 32 slots from t0 on: two runs of 16, each within a page; a run behind the chunk repeats the first
   auto load = [&](int t0) {
 #pragma unroll
     for (int u = 0; u < 2; u++) {
       const int at = u && t0 + 16 >= end ? t0 : t0 + 16 * u;
-      const int64_t page = page_of(c, table, shift, at, s);
+      const int64_t page = page_of(c, table, shift, at, bad);
       const T* kb = kp + page * c.k_block_stride + (at & in_page) * c.k_slot_stride;
       const T* vb = vp + page * c.v_block_stride + (at & in_page) * c.v_slot_stride;
 #pragma unroll
@@ -168,42 +171,47 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
     while (next < end && skip(next)) next += step;
     if (next < end) load(next);
 
+    uint32_t seen[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
-      float x[8];
-      V8 seen_by;
-#pragma unroll
-      for (int e = 0; e < 8; e++) x[e] = sc[t][e >> 2][e & 3] * mul;
       if (a.softcap > 0.f) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = cap - 2.f * cap * __builtin_amdgcn_rcpf(ex2(x[e]) + 1.f);
+        for (int e = 0; e < 8; e++) sc[t][e >> 2][e & 3] = capped(sc[t][e >> 2][e & 3], f);
       }
-      const int j0 = t0 + quad * 4;  // of x[0..3]; x[4..7] are 16 further
       if (a.d_slope) {
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          int j = j0 + (e >> 2) * 16 + (e & 3);
+          int j = t0 + quad * 4 + (e >> 2) * 16 + (e & 3);
           if (a.d_parent && t0 + 32 > q.base) {
             const int d = __shfl(depth_of, (j - q.base) & 63);
             j = j >= q.base ? q.base + d : j;
           }
-          x[e] -= slope[t] * fabsf((float)(row[t].pos - j));
+          sc[t][e >> 2][e & 3] -= slope[t] * fabsf((float)(row[t].pos - j));
         }
       }
+      seen[t] = 0xff;
       if (!whole) {
         const int from = t0 - q.base;
-        const uint32_t seen = from >= 32 || from <= -32 ? 0 : from >= 0 ? line[t] >> from : line[t] << -from;
+        const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line[t] >> from : line[t] << -from;
+        seen[t] = 0;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
           const int off = quad * 4 + (e >> 2) * 16 + (e & 3), j = t0 + off;
-          const bool see = (j >= row[t].start && j < row[t].end) || j < row[t].prefix || (seen >> off & 1);
-          x[e] = see ? x[e] : -kInf;
-          seen_by[e] = (T)(see ? 1.f : 0.f);
+          const bool see = (j >= row[t].start && j < row[t].end) || j < row[t].prefix || (drafted >> off & 1);
+          sc[t][e >> 2][e & 3] = see ? sc[t][e >> 2][e & 3] : -kInf;
+          seen[t] |= (see ? 1u : 0u) << e;
         }
       }
-      float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      most = max32(max16(most));
-      if (__any(most > top[t])) {
+    }
+    const int vr = quad * 4 + (col >> 2), vc = (col & 3) >> 1, ve = (col & 1) * 4;
+    V8 pb[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      float most = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
+                         fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
+      most = max32(max16(most)) * f.post;
+      // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+      if (__any(most > top[t] + 8.f)) {
         const float now = fmaxf(top[t], most), by = now == -kInf ? 1.f : ex2(top[t] - now);
         top[t] = now, sum[t] *= by;
 #pragma unroll
@@ -212,24 +220,41 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
       const float m = top[t] == -kInf ? 0.f : top[t];
       f32x8 p;
 #pragma unroll
-      for (int e = 0; e < 8; e++) p[e] = ex2(x[e] - m);
+      for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[t][e >> 2][e & 3], f.post, -m));
       sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
-      const V8 pb = __builtin_convertvector(p, V8);
+      pb[t] = __builtin_convertvector(p, V8);
+    }
+    if (hurt) {
 #pragma unroll
-      for (int d = 0; d < DB; d++) {
-        const int r = quad * 4 + (col >> 2), ch = d * 2 + ((col & 3) >> 1), e = (col & 1) * 4;
-        V8 vt = read_tr2<T>(tile + tile_at<D>(r, ch) + e, tile + tile_at<D>(r + 16, ch) + e);
-        if (hurt) {
-          const f32x4 n = mma16(strip<T>(vt), seen_by, f32x4{0.f, 0.f, 0.f, 0.f});
+      for (int t = 0; t < NT; t++) {
+        V8 by;
+#pragma unroll
+        for (int e = 0; e < 8; e++) by[e] = (T)(seen[t] >> e & 1 ? 1.f : 0.f);
+#pragma unroll
+        for (int d = 0; d < DB; d++) {
+          V8 vt = read_tr2<T>(tile + tile_at<D>(vr, d * 2 + vc) + ve, tile + tile_at<D>(vr + 16, d * 2 + vc) + ve);
+          const f32x4 n = mma16(strip<T>(vt), by, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int k = 0; k < 4; k++) o[t][d][k] += hurt_by(n[k]);
         }
-        o[t][d] = mma16(vt, pb, o[t][d]);
       }
+      for (int k = lane; k < kTile / 8; k += 64) {
+        V8 v = *(const V8*)(tile + 8 * k);
+        strip<T>(v);
+        *(V8*)(tile + 8 * k) = v;
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DB; d++) {
+      const V8 vt = read_tr2<T>(tile + tile_at<D>(vr, d * 2 + vc) + ve, tile + tile_at<D>(vr + 16, d * 2 + vc) + ve);
+#pragma unroll
+      for (int t = 0; t < NT; t++) o[t][d] = mma16(vt, pb[t], o[t][d]);
     }
     t0 = next;
   }
+
+  if (bad) flag(c, s, RKC_CS_BLOCK);
 
   // join the waves
 #pragma unroll
@@ -295,8 +320,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_few(const rkc_cache c, con
 template <typename T, int D>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
   const dim3 grid(p->units * p->splits), block(64 * kWaves);
+  if constexpr (D <= 128) {
+    if (p->rows == 32) attend_few<T, D, 2><<<grid, block, 0, s>>>(*c, *a, *p);
+  }
   if (p->rows == 16) attend_few<T, D, 1><<<grid, block, 0, s>>>(*c, *a, *p);
-  else attend_few<T, D, 2><<<grid, block, 0, s>>>(*c, *a, *p);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 

@@ -45,13 +45,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
 
   const int m = min(m0 + 32 * wave + col, M - 1), qi = m / G, qh = h * G + m % G;
   const bool mine = m0 + 32 * wave + col < M;
+  const Scale f = load_scale(a);
   Row row = load_row(a, q, s, qi);
-  const float slope = a.d_slope ? a.d_slope[qh] * kLog2e : 0.f;
+  const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
   V8 qf[KC];
   {
     const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + half * 8;
 #pragma unroll
-    for (int k = 0; k < KC; k++) qf[k] = *(const V8*)(p + 16 * k);
+    for (int k = 0; k < KC; k++) {
+      qf[k] = *(const V8*)(p + 16 * k);
+      if (f.negate) qf[k] = negated(qf[k]);
+    }
   }
   const bool tree = a.d_parent != nullptr, drafts = tree && c1 > q.base;
   if (drafts || (tree && a.d_slope)) {
@@ -70,8 +74,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   const int g_any_to = max(max(lim[0][3], lim[1][3]), max(lim[2][3], lim[3][3]));
   const int end = min(c1, g_any_to);
 
-  const float mul = a.softcap > 0.f ? a.scale / a.softcap * 2.f * kLog2e : a.scale * kLog2e;
-  const float cap = a.softcap * kLog2e;
   const T* kp = (const T*)c.d_k + h * c.k_head_stride;
   const T* vp = (const T*)c.d_v + h * c.v_head_stride;
 
@@ -83,55 +85,70 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
     for (int k = 0; k < 16; k++) o[d][k] = 0.f;
 
   u32x4 ks[P], vs[P];
-  // this thread's pieces of the tile at t0: a wave's pieces lie in rows of one page
+  int page[P];  // of this thread's pieces of the tile after the next: a wave's pieces lie in rows of one page
+  bool bad = false;
+  auto run_of = [&](int t0, int p) {  // first slot of the 16 that piece p lies in; one behind the end stands for the first
+    const int at = t0 + uni((p * kThreads + tid) / CH & ~15);
+    return at < end ? at : t0;
+  };
+  auto look_up = [&](int t0) {
+#pragma unroll
+    for (int p = 0; p < P; p++) page[p] = page_of(c, table, shift, run_of(t0, p), bad);
+  };
   auto load = [&](int t0) {
 #pragma unroll
     for (int p = 0; p < P; p++) {
-      const int piece = p * kThreads + tid, r = piece / CH, e = piece % CH * 8;
-      int at = t0 + uni(r & ~15);
-      at = at < end ? at : t0;  // a run of 16 behind the end repeats the first one
-      const int64_t page = page_of(c, table, shift, at, s);
-      ks[p] = *(const u32x4*)(kp + page * c.k_block_stride + (at & in_page) * c.k_slot_stride + (int)((r & 15) * (int)c.k_slot_stride) + e);
-      vs[p] = *(const u32x4*)(vp + page * c.v_block_stride + (at & in_page) * c.v_slot_stride + (int)((r & 15) * (int)c.v_slot_stride) + e);
+      const int piece = p * kThreads + tid, r = piece / CH, e = piece % CH * 8, at = run_of(t0, p) & in_page;
+      ks[p] = *(const u32x4*)(kp + page[p] * c.k_block_stride + at * c.k_slot_stride + (int)((r & 15) * (int)c.k_slot_stride) + e);
+      vs[p] = *(const u32x4*)(vp + page[p] * c.v_block_stride + at * c.v_slot_stride + (int)((r & 15) * (int)c.v_slot_stride) + e);
     }
   };
   auto store = [&](int t0, int buf) {
     T* to = lds + buf * 2 * kTile;
     const bool whole = t0 + BK <= pre || (t0 >= g_all_from && t0 + BK <= g_all_to);
-    bool bad = false;
+    bool hurt = false;
 #pragma unroll
     for (int p = 0; p < P; p++) {
       const int piece = p * kThreads + tid, r = piece / CH, j = t0 + r;
       u32x4 x = vs[p];
       if (!whole) {
         if (j >= end || (j < g_any_from && j >= pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
-        bad |= any_hurt<T>(x);
+        hurt |= any_hurt<T>(x);
       }
       *(u32x4*)(to + tile_at<D>(r, piece % CH)) = ks[p];
       *(u32x4*)(to + kTile + tile_at<D>(r, piece % CH)) = x;
     }
-    if (bad) hurt_at[buf] = t0;
+    if (hurt) hurt_at[buf] = t0;
   };
   auto skip = [&](int t) { return t + BK <= g_any_from && t >= pre; };
 
-  int t0 = c0, buf = 0;
-  while (t0 < end && skip(t0)) t0 += BK;
+  auto after = [&](int t) {
+    while (t < end && skip(t)) t += BK;
+    return t;
+  };
+  int t0 = after(c0), next = end, buf = 0;
   if (t0 < end) {
+    look_up(t0);
     load(t0);
+    next = after(t0 + BK);
+    if (next < end) look_up(next);
     store(t0, 0);
   }
   __syncthreads();
   while (t0 < end) {
-    int next = t0 + BK;
-    while (next < end && skip(next)) next += BK;
+    const int then = next < end ? after(next + BK) : end;
     if (next < end) load(next);
-    const T* kt_ = lds + buf * 2 * kTile;
-    const T* vt_ = kt_ + kTile;
+    if (then < end) look_up(then);
+    T* kt_ = lds + buf * 2 * kTile;
+    T* vt_ = kt_ + kTile;
+    const int vi = lane & 15, vr = 4 * half + (vi >> 2), vc = (lane >> 4 & 1) * 2 + ((vi & 3) >> 1), ve = (vi & 1) * 4;
     // whether any of the wave's rows sees anything of the tile, and whether all see all of it
-    if ((t0 + BK > any_from && t0 < any_to) || t0 < pre) {
-      const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
-      const bool hurt = hurt_at[buf] == t0;
-      f32x16 sc[KT];
+    const bool sees = (t0 + BK > any_from && t0 < any_to) || t0 < pre;
+    const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
+    const bool hurt = hurt_at[buf] == t0;
+    f32x16 sc[KT];
+    uint32_t seen[KT];
+    if (sees) {
 #pragma unroll
       for (int u = 0; u < KT; u++) {
 #pragma unroll
@@ -139,26 +156,31 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
 #pragma unroll
         for (int k = 0; k < KC; k++) sc[u] = mma32(*(const V8*)(kt_ + tile_at<D>(32 * u + col, 2 * k + half)), qf[k], sc[u]);
       }
-      uint32_t seen[KT];
-      float most = -kInf;
+      if (a.softcap > 0.f) {
 #pragma unroll
-      for (int u = 0; u < KT; u++) {
+        for (int u = 0; u < KT; u++)
 #pragma unroll
-        for (int k = 0; k < 16; k++) sc[u][k] *= mul;
-        if (a.softcap > 0.f) {
+          for (int k = 0; k < 16; k++) sc[u][k] = capped(sc[u][k], f);
+      }
+      if (a.d_slope) {
 #pragma unroll
-          for (int k = 0; k < 16; k++) sc[u][k] = cap - 2.f * cap * __builtin_amdgcn_rcpf(ex2(sc[u][k]) + 1.f);
-        }
-        const int j0 = t0 + 32 * u;
-        if (a.d_slope) {
+        for (int u = 0; u < KT; u++)
 #pragma unroll
           for (int k = 0; k < 16; k++) {
-            int j = j0 + (k & 3) + 8 * (k >> 2) + 4 * half;
-            if (drafts && j >= q.base) j = q.base + depths[min(j - q.base, RKC_MAX_TREE_ROWS - 1)];
+            int j = t0 + 32 * u + (k & 3) + 8 * (k >> 2) + 4 * half;
+            if (drafts && t0 + BK > q.base) {
+              const int d = depths[max(0, min(j - q.base, RKC_MAX_TREE_ROWS - 1))];
+              j = j >= q.base ? q.base + d : j;
+            }
             sc[u][k] -= slope * fabsf((float)(row.pos - j));
           }
-        }
-        if (!whole) {
+      }
+#pragma unroll
+      for (int u = 0; u < KT; u++) seen[u] = 0xffff;
+      if (!whole) {
+#pragma unroll
+        for (int u = 0; u < KT; u++) {
+          const int j0 = t0 + 32 * u;
           const uint32_t line = drafts ? line_window(lines[qi], 4, j0 - q.base) : 0;
           uint32_t bits = 0;
 #pragma unroll
@@ -170,10 +192,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
           }
           seen[u] = bits;
         }
+      }
+      float most = -kInf;
+#pragma unroll
+      for (int u = 0; u < KT; u++)
 #pragma unroll
         for (int k = 0; k < 16; k++) most = fmaxf(most, sc[u][k]);
-      }
-      most = max32(most);
+      most = max32(most) * f.post;
       // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
       if (__any(most > top + 8.f)) {
         const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
@@ -181,6 +206,36 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
 #pragma unroll
         for (int d = 0; d < DB; d++) o[d] *= by;
       }
+    }
+    if (hurt) {  // the same for the whole workgroup
+      if (sees) {
+#pragma unroll
+        for (int d = 0; d < DB; d++) {
+          f32x16 n;
+#pragma unroll
+          for (int k = 0; k < 16; k++) n[k] = 0.f;
+#pragma unroll
+          for (int u = 0; u < KT; u++)
+#pragma unroll
+            for (int v = 0; v < 2; v++) {
+              V8 by, vt = read_tr2<T>(vt_ + tile_at<D>(32 * u + 16 * v + vr, 4 * d + vc) + ve, vt_ + tile_at<D>(32 * u + 16 * v + vr + 8, 4 * d + vc) + ve);
+#pragma unroll
+              for (int k = 0; k < 8; k++) by[k] = (T)(seen[u] >> (8 * v + k) & 1 ? 1.f : 0.f);
+              n = mma32(strip<T>(vt), by, n);
+            }
+#pragma unroll
+          for (int k = 0; k < 16; k++) o[d][k] += hurt_by(n[k]);
+        }
+      }
+      __syncthreads();
+      for (int k = tid; k < kTile / 8; k += kThreads) {
+        V8 v = *(const V8*)(vt_ + 8 * k);
+        strip<T>(v);
+        *(V8*)(vt_ + 8 * k) = v;
+      }
+      __syncthreads();
+    }
+    if (sees) {
       const float mx = top == -kInf ? 0.f : top;
 #pragma unroll
       for (int u = 0; u < KT; u++) {
@@ -188,35 +243,23 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
         for (int v = 0; v < 2; v++) {
           f32x8 p;
 #pragma unroll
-          for (int k = 0; k < 8; k++) p[k] = ex2(sc[u][8 * v + k] - mx);
+          for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[u][8 * v + k], f.post, -mx));
           sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
           // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
           const V8 pb = __builtin_convertvector(p, V8);
-          const int i = lane & 15, r = 32 * u + 16 * v + 4 * half + (i >> 2), ch = (lane >> 4 & 1) * 2 + ((i & 3) >> 1), e = (i & 1) * 4;
+          const int r = 32 * u + 16 * v + vr;
 #pragma unroll
-          for (int d = 0; d < DB; d++) {
-            V8 vt = read_tr2<T>(vt_ + tile_at<D>(r, 4 * d + ch) + e, vt_ + tile_at<D>(r + 8, 4 * d + ch) + e);
-            if (hurt && !whole) {
-              V8 by;
-#pragma unroll
-              for (int k = 0; k < 8; k++) by[k] = (T)(seen[u] >> (8 * v + k) & 1 ? 1.f : 0.f);
-              f32x16 n;
-#pragma unroll
-              for (int k = 0; k < 16; k++) n[k] = 0.f;
-              n = mma32(strip<T>(vt), by, n);
-#pragma unroll
-              for (int k = 0; k < 16; k++) o[d][k] += hurt_by(n[k]);
-            }
-            o[d] = mma32(vt, pb, o[d]);
-          }
+          for (int d = 0; d < DB; d++)
+            o[d] = mma32(read_tr2<T>(vt_ + tile_at<D>(r, 4 * d + vc) + ve, vt_ + tile_at<D>(r + 8, 4 * d + vc) + ve), pb, o[d]);
         }
       }
     }
     buf ^= 1;
     if (next < end) store(next, buf);
     __syncthreads();
-    t0 = next;
+    t0 = next, next = then;
   }
+  if (bad) flag(c, s, RKC_CS_BLOCK);
 
   sum = sum32(sum);
   if (!mine) return;

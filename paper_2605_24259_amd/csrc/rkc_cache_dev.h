@@ -208,14 +208,40 @@ __device__ __forceinline__ int rows_end(const rkc_attention& a, const Seq& q, in
   return max(pre, q.base + last + 1);
 }
 
-// Block of the page that slot t lies in (block 0 for an id outside the pool, which sets the status).
-__device__ __forceinline__ int64_t page_of(const rkc_cache& c, const int32_t* table, int shift, int t, int s) {
+// Block of the page that slot t lies in; block 0 for an id outside the pool, which `bad` remembers.
+__device__ __forceinline__ int page_of(const rkc_cache& c, const int32_t* table, int shift, int t, bool& bad) {
   const int id = table[t >> shift];
-  if ((uint32_t)id >= (uint32_t)c.n_blocks) {
-    flag(c, s, RKC_CS_BLOCK);
-    return 0;
-  }
-  return id;
+  const bool out = (uint32_t)id >= (uint32_t)c.n_blocks;
+  bad |= out;
+  return out ? 0 : id;
+}
+
+// The factors of a score: x = raw * pre, or capped; then x - slope * distance; weights are exp2(x * post - maximum).
+// Without a cap the scale stays out of the scores until the exponent takes it up; a negative scale goes into
+// the queries' signs, so that the maximum of the scores is that of the products.
+struct Scale {
+  float pre, cap, post;
+  bool negate;
+};
+
+__device__ __forceinline__ Scale load_scale(const rkc_attention& a) {
+  Scale s;
+  s.cap = a.softcap * kLog2e;
+  s.negate = a.scale < 0.f;
+  const float by = fabsf(a.scale);
+  s.pre = a.softcap > 0.f ? by / a.softcap * 2.f * kLog2e : 1.f;
+  s.post = a.softcap > 0.f ? 1.f : fmaxf(by * kLog2e, 1e-30f);  // above 0: what is masked stays -inf
+  return s;
+}
+
+// softcap tanh(x / softcap) in units of log2, of x with `pre` in it: 1 - 2 / (exp(2 y) + 1)
+__device__ __forceinline__ float capped(float x, const Scale& s) {
+  return s.cap - 2.f * s.cap * __builtin_amdgcn_rcpf(ex2(x * s.pre) + 1.f);
+}
+
+template <typename V> __device__ __forceinline__ V negated(V v) {
+  u32x4 b = __builtin_bit_cast(u32x4, v);
+  return __builtin_bit_cast(V, b ^ 0x80008000u);
 }
 
 }  // namespace

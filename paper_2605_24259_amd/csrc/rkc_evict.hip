@@ -204,7 +204,9 @@ __global__ __launch_bounds__(256) void evict_move(const evict_args g, int chunks
   const int32_t* from = g.from + (int64_t)row * g.most + first;
   for (int x = threadIdx.x; x < n * per; x += 256) {
     const int i = x / per, e = x % per * 8, to = gaps[i], at = from[i];
-    const int64_t pt = page_of(c, table, shift, to, s), pf = page_of(c, table, shift, at, s);
+    bool bad = false;
+    const int64_t pt = page_of(c, table, shift, to, bad), pf = page_of(c, table, shift, at, bad);
+    if (bad) flag(c, s, RKC_CS_BLOCK);
     const int in_page = c.page_tokens - 1;
     uint16_t* k = (uint16_t*)c.d_k + h * c.k_head_stride + e;
     uint16_t* v = (uint16_t*)c.d_v + h * c.v_head_stride + e;

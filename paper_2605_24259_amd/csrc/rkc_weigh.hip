@@ -37,20 +37,21 @@ __global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_a
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
   V8 kf[NS][KC];
+  bool bad = false;
   const T* kp = (const T*)c.d_k + h * c.k_head_stride;
 #pragma unroll
   for (int u = 0; u < NS; u++) {
     const int at = min(t0 + 16 * u, (q.len - 1) & ~15);
-    const T* kb = kp + page_of(c, table, shift, at, s) * c.k_block_stride + (at & in_page) * c.k_slot_stride + (int)(col * (int)c.k_slot_stride) + quad * 8;
+    const T* kb = kp + (int64_t)page_of(c, table, shift, at, bad) * c.k_block_stride + (at & in_page) * c.k_slot_stride + (int)(col * (int)c.k_slot_stride) + quad * 8;
 #pragma unroll
     for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + 32 * k);
   }
+  if (bad) flag(c, s, RKC_CS_BLOCK);
   const bool tree = a.d_parent != nullptr;
   const bool drafts = tree && w0 + 4 * kSlots > q.base;
   if (drafts || (tree && a.d_slope)) tree_lines(c, a, q, s, part == 0 && h == 0, lines, depths);
   const int pre = a.d_prefix ? max(0, min(a.d_prefix[s], tree ? q.base : q.len)) : 0;
-  const float mul = a.softcap > 0.f ? a.scale / a.softcap * 2.f * kLog2e : a.scale * kLog2e;
-  const float cap = a.softcap * kLog2e;
+  const Scale sc = load_scale(a);
   float acc[NS] = {};
 
   for (int mb = 0; mb < M; mb += kBlock) {
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_a
         const Row w = load_row(a, q, s, qi);
         const float lse = a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh];
         r.lse2 = lse == -kInf ? kInf : lse * kLog2e;  // a row that saw nothing gave nothing
-        r.slope = a.d_slope ? a.d_slope[qh] * kLog2e : 0.f;
+        r.slope = a.d_slope ? a.d_slope[qh] * kLog2e / sc.post : 0.f;
         r.start = w.start, r.end = w.end, r.line = qi;
         r.pos = tree && a.d_slope ? q.base + depths[qi] : w.pos;
       }
@@ -82,7 +83,10 @@ __global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_a
       const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + quad * 8;
       V8 qf[KC];
 #pragma unroll
-      for (int k = 0; k < KC; k++) qf[k] = *(const V8*)(p + 32 * k);
+      for (int k = 0; k < KC; k++) {
+        qf[k] = *(const V8*)(p + 32 * k);
+        if (sc.negate) qf[k] = negated(qf[k]);
+      }
 #pragma unroll
       for (int u = 0; u < NS; u++) {
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -92,13 +96,13 @@ __global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_a
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const RowIn& r = in[m0 + quad * 4 + e];  // rows behind the last one have a sum of infinity
-          float y = x[e] * mul;
-          if (a.softcap > 0.f) y = cap - 2.f * cap * __builtin_amdgcn_rcpf(ex2(y) + 1.f);
+          float y = x[e];
+          if (a.softcap > 0.f) y = capped(y, sc);
           if (a.d_slope) {
             const int at = drafts && j >= q.base ? q.base + depths[min(j - q.base, RKC_MAX_TREE_ROWS - 1)] : j;
             y -= r.slope * fabsf((float)(r.pos - at));
           }
-          y = ex2(y - r.lse2);
+          y = ex2(y * sc.post - r.lse2);
           if (!whole) {
             bool see = (j >= r.start && j < r.end) || j < pre;
             if (drafts && j >= q.base) {
