@@ -1,8 +1,8 @@
 // rkc_evict.hip -- eviction from a paged cache by the account of its slots.
 //
-// One workgroup decides for a head of a sequence: the account of the last slot to be kept is found by bisection
-// of its 32-bit order (two bits a round: three counts by ballots, no atomics), ties go to the lowest slots, and
-// two prefix sums pair the gaps in front of the new end with the kept slots behind it.  A second kernel moves their
+// One workgroup decides for a head of a sequence: the account of the last slot to be kept is found 8 bits of its
+// 32-bit order at a time, by counts of the digits in LDS (whole numbers: their order does not matter); ties go to the
+// lowest slots, and prefix sums pair the gaps in front of the new end with the kept slots behind it.  A second kernel moves their
 // keys and values.  Sources lie behind the new end and targets before it, so that the moves need no order among
 // each other, and what is kept in place is not touched: the least that can be moved.
 #include "rkc_cache_dev.h"
@@ -25,7 +25,8 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {  // inclusive
+// Sum over the lower lanes and this one.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -35,10 +36,16 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {  // inclusive
   return x;
 }
 
+// Number of the lower lanes whose bit is set.
+__device__ __forceinline__ int lower(uint64_t m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); }
+
 __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
   const rkc_cache& c = g.c;
   const rkc_eviction& e = g.e;
-  __shared__ uint32_t part[2][4][kWaves];
+  // counts of 256 digits, one copy per lane: no two lanes of an addition meet in a bank, whatever the digits
+  __shared__ __attribute__((aligned(16))) uint32_t hist[256 * 64];
+  __shared__ uint32_t table[2][kItems * kWaves + 1];  // counts per run of 64 slots, then what lies before each
+  __shared__ uint32_t found[3];
   const int H = c.kv_heads, s = blockIdx.x / H, h = blockIdx.x % H;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int len = e.d_length[s];
@@ -65,129 +72,166 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
     if (tid == 0) g.count[blockIdx.x] = 0;
     return;
   }
+  // A thread's slots of a tile: tid, tid + 1024, ...  Their accounts and positions stay in registers where a
+  // sequence is one tile; of a longer one they are read again for each pass.
   const int tiles = (len + kTile - 1) / kTile;
-  int turn = 0;
-  // sums of up to four counts of this wave over the workgroup
-  auto total = [&](uint32_t a0, uint32_t a1, uint32_t a2, uint32_t* out) {
-    if (lane == 0) part[turn][0][wave] = a0, part[turn][1][wave] = a1, part[turn][2][wave] = a2;
-    __syncthreads();
-    for (int k = 0; k < 3; k++) {
-      uint32_t x = 0;
-#pragma unroll
-      for (int i = 0; i < kWaves; i++) x += part[turn][k][i];
-      out[k] = x;
-    }
-    turn ^= 1;
-  };
-  uint32_t sums[3];
-  int K = now - held;  // to be kept of the slots behind the protected ones
-  bool among_recent = false;
-  if (recents) {
-    uint32_t n = 0;
-    for (int j = held + tid; j - tid < len; j += kThreads) n += __popcll(__ballot(j < len && pos_at(j) >= recent_from));
-    total(n, 0, 0, sums);
-    among_recent = (int)sums[0] >= K;
-    if (!among_recent) K -= sums[0];
-  }
-  // the slots the choice is among: their order, the others 0.  A thread has 16 neighbouring slots of a tile.
-  uint32_t key[kItems], sure = 0;
+  float wt[kItems];
+  int ps[kItems];
   auto load = [&](int tile) {
-    const int j0 = tile * kTile + tid * kItems;
-    sure = 0;
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
-      const int j = j0 + i;
-      const bool in = j >= held && j < len;
-      const bool recent = recents && in && pos_at(j) >= recent_from;
-      key[i] = in && recent == among_recent ? order_of(w[j]) : 0;
-      if (j < held || (recent && !among_recent)) sure |= 1u << i;
+      const int j = tile * kTile + i * kThreads + tid;
+      wt[i] = 0.f, ps[i] = j;
+      if (j < len) {
+        wt[i] = w[j];
+        if (pos) ps[i] = pos[j];
+      }
     }
   };
-  if (tiles == 1) load(0);
-  uint32_t T = 0;  // the order of the last slot to be kept
-  if (K > 0) {
-    for (int b = 30; b >= 0; b -= 2) {
-      uint32_t n1 = 0, n2 = 0, n3 = 0;
-      const uint32_t t1 = T | 1u << b, t2 = T | 2u << b, t3 = T | 3u << b;
-      for (int t = 0; t < tiles; t++) {
-        if (tiles > 1) load(t);
+  // bit i: slot i of the thread is behind the protected ones; is recent
+  auto slots_of = [&](int tile, uint32_t& open, uint32_t& recent) {
+    open = recent = 0;
 #pragma unroll
-        for (int i = 0; i < kItems; i++) {
-          n1 += __popcll(__ballot(key[i] >= t1));
-          n2 += __popcll(__ballot(key[i] >= t2));
-          n3 += __popcll(__ballot(key[i] >= t3));
-        }
-      }
-      total(n1, n2, n3, sums);
-      T = (int)sums[2] >= K ? t3 : (int)sums[1] >= K ? t2 : (int)sums[0] >= K ? t1 : T;
+    for (int i = 0; i < kItems; i++) {
+      const int j = tile * kTile + i * kThreads + tid;
+      const bool in = j >= held && j < len;
+      open |= (in ? 1u : 0u) << i;
+      recent |= (in && recents && ps[i] >= recent_from ? 1u : 0u) << i;
     }
-  } else {
-    T = 0xffffffffu;
-  }
-  int ties = 0;  // slots of that order to be kept, the lowest first
-  if (K > 0) {
+  };
+  uint32_t open, recent;
+  load(0);
+  slots_of(0, open, recent);
+  int K = now - held;  // to be kept of the slots behind the protected ones
+  bool among_recent = false;  // the choice is among the recent ones; else they stay, and it is among the others
+  if (recents) {
+    if (tid == 0) found[0] = 0;
+    __syncthreads();
     uint32_t n = 0;
     for (int t = 0; t < tiles; t++) {
-      if (tiles > 1) load(t);
-#pragma unroll
-      for (int i = 0; i < kItems; i++) n += __popcll(__ballot(key[i] > T));
+      if (t) load(t), slots_of(t, open, recent);
+      n += __popc(recent);
     }
-    total(n, 0, 0, sums);
-    ties = K - sums[0];
+    n = wave_scan(n);
+    if (lane == 63 && n) atomicAdd(&found[0], n);
+    __syncthreads();
+    among_recent = (int)found[0] >= K;
+    if (!among_recent) K -= found[0];
+    __syncthreads();
   }
+  // The order of the last slot to be kept, 8 bits at a time from the top; `left`: how many of those that agree with
+  // it so far are to be kept.
+  uint32_t T = 0, left = K, same = 0;
+  if (K > 0) {
+    for (int b = 24; b >= 0; b -= 8) {
+      for (int k = tid; k < 256 * 64 / 4; k += kThreads) ((u32x4*)hist)[k] = u32x4{0, 0, 0, 0};
+      __syncthreads();
+      for (int t = 0; t < tiles; t++) {
+        if (tiles > 1) load(t), slots_of(t, open, recent);
+        const uint32_t in = among_recent ? recent : open & ~recent;
+#pragma unroll
+        for (int i = 0; i < kItems; i++) {
+          if (t * kTile + i * kThreads >= len) break;
+          const uint32_t key = order_of(wt[i]);
+          if ((in >> i & 1) && (b == 24 || (key ^ T) >> b >> 8 == 0)) atomicAdd(&hist[(key >> b & 255) * 64 + lane], 1u);
+        }
+      }
+      __syncthreads();
+      // a quarter of a digit's copies per thread
+      uint32_t n = 0;
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        const u32x4 x = ((const u32x4*)hist)[tid * 4 + (k + tid & 3)];
+        n += x[0] + x[1] + x[2] + x[3];
+      }
+      n += __shfl_xor(n, 1);
+      n += __shfl_xor(n, 2);
+      __syncthreads();
+      if ((tid & 3) == 0) hist[tid >> 2] = n;
+      __syncthreads();
+      if (wave == 0) {  // lane l: digits 255 - 4 l and the three below
+        const u32x4 x = ((const u32x4*)hist)[63 - lane];
+        const uint32_t mine = x[0] + x[1] + x[2] + x[3], to = wave_scan(mine);
+        uint32_t above = to - mine;
+        if (above < left && left <= to) {
+          int d = 3;
+          while (above + x[d] < left) above += x[d--];
+          found[0] = (63 - lane) * 4 + d, found[1] = left - above, found[2] = x[d];
+        }
+      }
+      __syncthreads();
+      T |= found[0] << b, left = found[1], same = found[2];
+    }
+  }
+  // prefix sums over the runs of 64 slots of a tile, of two counts at once; returns the tile's totals
+  auto runs_before = [&](uint32_t& all0, uint32_t& all1) {
+    __syncthreads();
+    if (wave < 2) {
+      uint32_t x[kItems * kWaves / 64], sum = 0;
+#pragma unroll
+      for (int k = 0; k < kItems * kWaves / 64; k++) x[k] = sum, sum += table[wave][lane * (kItems * kWaves / 64) + k];
+      const uint32_t to = wave_scan(sum);
+#pragma unroll
+      for (int k = 0; k < kItems * kWaves / 64; k++) table[wave][lane * (kItems * kWaves / 64) + k] = to - sum + x[k];
+      if (lane == 63) table[wave][kItems * kWaves] = to;
+    }
+    __syncthreads();
+    all0 = table[0][kItems * kWaves], all1 = table[1][kItems * kWaves];
+  };
   int32_t* gaps = g.gaps + (int64_t)blockIdx.x * g.most;
   int32_t* from = g.from + (int64_t)blockIdx.x * g.most;
-  int tie0 = 0, gap0 = 0, from0 = 0;
-  // exclusive sum over the threads; *all: the total
-  auto scan = [&](uint32_t x, uint32_t* all) {
-    const uint32_t inc = wave_scan(x);
-    if (lane == 63) part[turn][0][wave] = inc;
-    __syncthreads();
-    uint32_t before = 0, sum = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; i++) {
-      const uint32_t y = part[turn][0][i];
-      before += i < wave ? y : 0, sum += y;
-    }
-    turn ^= 1;
-    *all = sum;
-    return before + inc - x;
-  };
+  uint32_t tie0 = 0, gap0 = 0, from0 = 0, all0, all1;
   for (int t = 0; t < tiles; t++) {
-    if (tiles > 1) load(t);
-    uint32_t all, keep = sure, eq = 0;
+    if (tiles > 1) load(t), slots_of(t, open, recent);
+    const uint32_t in = among_recent ? recent : open & ~recent;
+    uint32_t keep = among_recent ? 0 : recent, tie = 0;
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
-      if (K > 0 && key[i] > T) keep |= 1u << i;
-      if (K > 0 && key[i] == T) eq |= 1u << i;
+      const uint32_t key = order_of(wt[i]);
+      if (t * kTile + i * kThreads + tid < held) keep |= 1u << i;
+      if (K > 0 && (in >> i & 1)) {
+        if (key > T) keep |= 1u << i;
+        if (key == T) tie |= 1u << i;
+      }
     }
-    int left = ties - tie0 - (int)scan(__popc(eq), &all);
-    tie0 += all;
+    if (left == same) {  // all of the last order stay
+      keep |= tie;
+    } else {  // the lowest `left` of them
 #pragma unroll
-    for (int i = 0; i < kItems; i++)
-      if (eq >> i & 1 && left-- > 0) keep |= 1u << i;
-    const int j0 = t * kTile + tid * kItems;
-    uint32_t before = 0, behind = 0;  // slots in front of the new end, slots behind it
+      for (int i = 0; i < kItems; i++) {
+        const uint64_t m = __ballot(tie >> i & 1);
+        if (lane == 0) table[0][i * kWaves + wave] = __popcll(m), table[1][i * kWaves + wave] = 0;
+      }
+      runs_before(all0, all1);
+#pragma unroll
+      for (int i = 0; i < kItems; i++) {
+        const uint64_t m = __ballot(tie >> i & 1);
+        if ((tie >> i & 1) && tie0 + table[0][i * kWaves + wave] + lower(m) < left) keep |= 1u << i;
+      }
+      tie0 += all0;
+      __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
-      before |= (j0 + i < now ? 1u : 0u) << i;
-      behind |= (j0 + i >= now && j0 + i < len ? 1u : 0u) << i;
+      const int j = t * kTile + i * kThreads + tid;
+      const uint64_t gap = __ballot(j < now && !(keep >> i & 1)), src = __ballot(j >= now && j < len && (keep >> i & 1));
+      if (lane == 0) table[0][i * kWaves + wave] = __popcll(gap), table[1][i * kWaves + wave] = __popcll(src);
     }
-    const uint32_t gap = before & ~keep, src = behind & keep;
-    const uint32_t mine = scan(__popc(gap) << 16 | __popc(src), &all);
-    int gi = gap0 + (mine >> 16), fi = from0 + (mine & 0xffff);
-    gap0 += all >> 16, from0 += all & 0xffff;
+    runs_before(all0, all1);
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
-      const int j = j0 + i;
-      if (gap >> i & 1) gaps[gi++] = j;
-      if (src >> i & 1) from[fi++] = j;
-      if (before & keep & 1u << i) w_out[j] = w[j], pos_out[j] = pos_at(j);
+      const int j = t * kTile + i * kThreads + tid;
+      const bool kept = keep >> i & 1, is_gap = j < now && !kept, is_src = j >= now && j < len && kept;
+      const uint64_t gap = __ballot(is_gap), src = __ballot(is_src);
+      if (is_gap) gaps[gap0 + table[0][i * kWaves + wave] + lower(gap)] = j;
+      if (is_src) from[from0 + table[1][i * kWaves + wave] + lower(src)] = j;
+      if (j < now && kept) w_out[j] = wt[i], pos_out[j] = ps[i];
     }
+    gap0 += all0, from0 += all1;
+    __syncthreads();
   }
-  __syncthreads();
   if (tid == 0) g.count[blockIdx.x] = gap0;
-  for (int i = tid; i < gap0; i += kThreads) {
+  for (int i = tid; i < (int)gap0; i += kThreads) {
     const int j = from[i], to = gaps[i];
     w_out[to] = w[j], pos_out[to] = pos_at(j);
   }
