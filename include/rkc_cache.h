@@ -37,7 +37,8 @@ enum rkc_cache_status {
 };
 
 /* The cache: host struct.  K and V are [block][slot][head][dim] in any order of the first three (strides in
- * elements, multiples of 8; the last dimension is contiguous); 16-byte aligned. */
+ * elements, multiples of 8, below 2^31 between blocks and 2^30 within one; the last dimension is contiguous); 16-byte
+ * aligned. */
 typedef struct rkc_cache {
   int32_t n_seqs;
   int32_t n_blocks;    /* blocks of the pool; table entries are < this                               */

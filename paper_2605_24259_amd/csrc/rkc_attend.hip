@@ -69,7 +69,9 @@ rkc_status rkc_cache_check(const rkc_cache* c) {
   if (c->page_tokens < 16 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1))) return RKC_E_UNSUPPORTED;
   for (int64_t x : {c->k_slot_stride, c->v_slot_stride})
     if (bad_stride(x, c->page_tokens)) return RKC_E_RANGE;
-  for (int64_t x : {c->k_block_stride, c->v_block_stride, c->k_head_stride, c->v_head_stride})
+  for (int64_t x : {c->k_block_stride, c->v_block_stride})
+    if (x < 0 || x % 8 || x >= (int64_t)1 << 31) return RKC_E_RANGE;
+  for (int64_t x : {c->k_head_stride, c->v_head_stride})
     if (x < 0 || x % 8 || x > kFar) return RKC_E_RANGE;
   if (c->n_seqs == 0) return RKC_OK;
   if (!c->d_k || !c->d_v || !c->d_block_table) return RKC_E_NULL;

@@ -105,8 +105,7 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
   if (a.d_parent) any_to = q.len;
   const int end = min(c1, any_to);  // of what is looked at here: a chunk is a multiple of 32 slots
 
-  const T* kp = (const T*)c.d_k + h * c.k_head_stride;
-  const T* vp = (const T*)c.d_v + h * c.v_head_stride;
+  const Pool kp = k_pool(c, h), vp = v_pool(c, h);
   T* tile = (T*)(lds + wave * kLds);
 
   float top[NT], sum[NT];
@@ -126,15 +125,15 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
 #pragma unroll
     for (int u = 0; u < 2; u++) {
       const int at = u && t0 + 16 >= end ? t0 : t0 + 16 * u;
-      const int64_t page = page_of(c, table, shift, at, bad);
-      const T* kb = kp + page * c.k_block_stride + (at & in_page) * c.k_slot_stride;
-      const T* vb = vp + page * c.v_block_stride + (at & in_page) * c.v_slot_stride;
+      const int page = page_of(c, table, shift, at, bad);
+      const char* kb = run_at(kp, page, at & in_page);
+      const char* vb = run_at(vp, page, at & in_page);
 #pragma unroll
-      for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + (int)(col * (int)c.k_slot_stride) + quad * 8 + 32 * k);
+      for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + (col * kp.slot + quad * 16u) + 64 * k);
 #pragma unroll
       for (int p = 0; p < VP / 2; p++) {
-        const int piece = p * 64 + lane, r = piece / (D / 8), e = piece % (D / 8) * 8;
-        vf[u * (VP / 2) + p] = *(const u32x4*)(vb + (int)(r * (int)c.v_slot_stride) + e);
+        const uint32_t piece = p * 64 + lane, r = piece / (D / 8), e = piece % (D / 8) * 16;
+        vf[u * (VP / 2) + p] = *(const u32x4*)(vb + (r * vp.slot + e));
       }
     }
   };
@@ -189,18 +188,13 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
           sc[t][e >> 2][e & 3] -= slope[t] * fabsf((float)(row[t].pos - j));
         }
       }
-      seen[t] = 0xff;
+      seen[t] = 0xffffffff;
       if (!whole) {
         const int from = t0 - q.base;
         const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line[t] >> from : line[t] << -from;
-        seen[t] = 0;
+        seen[t] = seen_of(row[t], t0, drafted) >> 4 * quad;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const int off = quad * 4 + (e >> 2) * 16 + (e & 3), j = t0 + off;
-          const bool see = (j >= row[t].start && j < row[t].end) || j < row[t].prefix || (drafted >> off & 1);
-          sc[t][e >> 2][e & 3] = see ? sc[t][e >> 2][e & 3] : -kInf;
-          seen[t] |= (see ? 1u : 0u) << e;
-        }
+        for (int e = 0; e < 8; e++) sc[t][e >> 2][e & 3] = masked(sc[t][e >> 2][e & 3], seen[t], 16 * (e >> 2) + (e & 3));
       }
     }
     const int vr = quad * 4 + (col >> 2), vc = (col & 3) >> 1, ve = (col & 1) * 4;
@@ -230,7 +224,7 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
       for (int t = 0; t < NT; t++) {
         V8 by;
 #pragma unroll
-        for (int e = 0; e < 8; e++) by[e] = (T)(seen[t] >> e & 1 ? 1.f : 0.f);
+        for (int e = 0; e < 8; e++) by[e] = (T)(seen[t] >> (16 * (e >> 2) + (e & 3)) & 1 ? 1.f : 0.f);
 #pragma unroll
         for (int d = 0; d < DB; d++) {
           V8 vt = read_tr2<T>(tile + tile_at<D>(vr, d * 2 + vc) + ve, tile + tile_at<D>(vr + 16, d * 2 + vc) + ve);

@@ -13,7 +13,7 @@ constexpr int kRows = 128, kThreads = 256;
 static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int BK = D == 256 ? 32 : 64, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
   constexpr int P = BK * CH / kThreads;  // 16-byte pieces of K, and of V, per thread
@@ -63,8 +63,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
     row.pos = q.base + depths[qi];
   }
   // slots that all of the wave's rows see, and slots that any of them, and of the workgroup's, sees
-  const int all_from = wave_max(row.start), all_to = wave_min(row.end), pre = uni(row.prefix);
-  const int any_from = wave_min(row.start), any_to = tree ? q.len : max(pre, wave_max(row.end));
+  int all_from = 0, any_from = 0;
+  if (a.d_row_start) all_from = wave_max(row.start), any_from = wave_min(row.start);
+  const int all_to = uni(row.end), pre = uni(row.prefix);  // a wave's first lane has its first row
+  const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, 31));
   if (lane == 0) lim[wave][0] = all_from, lim[wave][1] = all_to, lim[wave][2] = any_from, lim[wave][3] = any_to;
   if (tid < 2) hurt_at[tid] = -1;
   __syncthreads();
@@ -74,8 +76,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   const int g_any_to = max(max(lim[0][3], lim[1][3]), max(lim[2][3], lim[3][3]));
   const int end = min(c1, g_any_to);
 
-  const T* kp = (const T*)c.d_k + h * c.k_head_stride;
-  const T* vp = (const T*)c.d_v + h * c.v_head_stride;
+  const Pool kp = k_pool(c, h), vp = v_pool(c, h);
 
   float top = -kInf, sum = 0.f;
   f32x16 o[DB];
@@ -98,9 +99,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   auto load = [&](int t0) {
 #pragma unroll
     for (int p = 0; p < P; p++) {
-      const int piece = p * kThreads + tid, r = piece / CH, e = piece % CH * 8, at = run_of(t0, p) & in_page;
-      ks[p] = *(const u32x4*)(kp + page[p] * c.k_block_stride + at * c.k_slot_stride + (int)((r & 15) * (int)c.k_slot_stride) + e);
-      vs[p] = *(const u32x4*)(vp + page[p] * c.v_block_stride + at * c.v_slot_stride + (int)((r & 15) * (int)c.v_slot_stride) + e);
+      const uint32_t piece = p * kThreads + tid, r = piece / CH & 15, e = piece % CH * 16;
+      const int at = run_of(t0, p) & in_page;
+      ks[p] = *(const u32x4*)(run_at(kp, page[p], at) + (r * kp.slot + e));
+      vs[p] = *(const u32x4*)(run_at(vp, page[p], at) + (r * vp.slot + e));
     }
   };
   auto store = [&](int t0, int buf) {
@@ -176,21 +178,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
           }
       }
 #pragma unroll
-      for (int u = 0; u < KT; u++) seen[u] = 0xffff;
+      for (int u = 0; u < KT; u++) seen[u] = 0xffffffff;
       if (!whole) {
 #pragma unroll
         for (int u = 0; u < KT; u++) {
           const int j0 = t0 + 32 * u;
-          const uint32_t line = drafts ? line_window(lines[qi], 4, j0 - q.base) : 0;
-          uint32_t bits = 0;
+          seen[u] = seen_of(row, j0, drafts ? line_window(lines[qi], 4, j0 - q.base) : 0) >> 4 * half;
 #pragma unroll
-          for (int k = 0; k < 16; k++) {
-            const int off = (k & 3) + 8 * (k >> 2) + 4 * half, j = j0 + off;
-            const bool see = (j >= row.start && j < row.end) || j < row.prefix || (line >> off & 1);
-            sc[u][k] = see ? sc[u][k] : -kInf;
-            bits |= (see ? 1u : 0u) << k;
-          }
-          seen[u] = bits;
+          for (int k = 0; k < 16; k++) sc[u][k] = masked(sc[u][k], seen[u], (k & 3) + 8 * (k >> 2));
         }
       }
       float most = -kInf;
@@ -220,7 +215,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
             for (int v = 0; v < 2; v++) {
               V8 by, vt = read_tr2<T>(vt_ + tile_at<D>(32 * u + 16 * v + vr, 4 * d + vc) + ve, vt_ + tile_at<D>(32 * u + 16 * v + vr + 8, 4 * d + vc) + ve);
 #pragma unroll
-              for (int k = 0; k < 8; k++) by[k] = (T)(seen[u] >> (8 * v + k) & 1 ? 1.f : 0.f);
+              for (int k = 0; k < 8; k++) by[k] = (T)(seen[u] >> (16 * v + (k & 3) + 8 * (k >> 2)) & 1 ? 1.f : 0.f);
               n = mma32(strip<T>(vt), by, n);
             }
 #pragma unroll

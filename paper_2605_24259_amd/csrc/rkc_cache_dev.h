@@ -56,14 +56,20 @@ __device__ __forceinline__ float sum16(float x) { float a, b; pair16(x, a, b); r
 __device__ __forceinline__ float sum32(float x) { float a, b; pair32(x, a, b); return a + b; }
 
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int wave_min(int x) {
-  for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d));
-  return uni(x);
+// Minimum and maximum over the wave, by row permutations and swaps of rows.
+template <int CTRL> __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true); }
+template <typename Op> __device__ __forceinline__ int wave_all(int x, Op op) {
+  x = op(x, dpp<0xb1>(x));   // quad_perm [1,0,3,2]
+  x = op(x, dpp<0x4e>(x));   // quad_perm [2,3,0,1]
+  x = op(x, dpp<0x141>(x));  // row_half_mirror
+  x = op(x, dpp<0x140>(x));  // row_mirror
+  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op((int)r[0], (int)r[1]);
+  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return uni(op((int)r[0], (int)r[1]));
 }
-__device__ __forceinline__ int wave_max(int x) {
-  for (int d = 32; d; d >>= 1) x = max(x, __shfl_xor(x, d));
-  return uni(x);
-}
+__device__ __forceinline__ int wave_min(int x) { return wave_all(x, [](int a, int b) { return min(a, b); }); }
+__device__ __forceinline__ int wave_max(int x) { return wave_all(x, [](int a, int b) { return max(a, b); }); }
 
 // A tile of slots in LDS: rows of D elements in 16-byte chunks, the chunk's number xored with a number of
 // the row so that neither a column of chunks over 16 rows (keys) nor 32 bytes of 4, 8 or 16 neighbouring rows
@@ -206,6 +212,35 @@ __device__ __forceinline__ int rows_end(const rkc_attention& a, const Seq& q, in
   if (a.d_parent) return q.len;
   const int pre = a.d_prefix ? max(0, min(a.d_prefix[s], q.len)) : 0;
   return max(pre, q.base + last + 1);
+}
+
+// Bits of 32 slots from number `lo` of them on.
+__device__ __forceinline__ uint32_t bits_from(int lo) { return (uint32_t)(0xffffffffull << max(0, min(lo, 32))); }
+
+// Which of the 32 slots from j0 on a row sees, `line` being what it sees of drafted ones.
+__device__ __forceinline__ uint32_t seen_of(const Row& r, int j0, uint32_t line) {
+  return (bits_from(r.start - j0) & ~bits_from(r.end - j0)) | ~bits_from(r.prefix - j0) | line;
+}
+
+// x where bit k of m is set, else -inf: two instructions.
+__device__ __forceinline__ float masked(float x, uint32_t m, int k) {
+  const uint32_t all = (uint32_t)((int32_t)(m << (31 - k)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & all) | (0xff800000u & ~all));
+}
+
+// Memory of slot t's 16 neighbours: base + page x block + (t in its page) x slot, all in bytes; uniform.
+struct Pool {
+  const char* base;
+  uint32_t block, slot;
+};
+__device__ __forceinline__ Pool k_pool(const rkc_cache& c, int h) {
+  return {(const char*)c.d_k + 2 * h * c.k_head_stride, 2 * (uint32_t)c.k_block_stride, 2 * (uint32_t)c.k_slot_stride};
+}
+__device__ __forceinline__ Pool v_pool(const rkc_cache& c, int h) {
+  return {(const char*)c.d_v + 2 * h * c.v_head_stride, 2 * (uint32_t)c.v_block_stride, 2 * (uint32_t)c.v_slot_stride};
+}
+__device__ __forceinline__ const char* run_at(const Pool& p, int page, int in_page) {
+  return p.base + (uint64_t)(uint32_t)page * p.block + (uint32_t)in_page * p.slot;
 }
 
 // Block of the page that slot t lies in; block 0 for an id outside the pool, which `bad` remembers.
