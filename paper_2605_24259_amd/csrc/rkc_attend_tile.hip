@@ -2,9 +2,11 @@
 //
 // A workgroup holds 128 packed rows (rows x query heads of one key/value head), 32 of them in each of its four
 // waves as columns of 32x32x16 matrix products, and goes over the slots that any of them sees in tiles of 64 (32
-// at 256 elements a head).  K and V of the next tile travel through registers into the other half of LDS while this
-// one is worked on; one barrier a tile.  Tiles that every row sees skip the masks, waves whose rows see nothing of a
+// at 256 elements a head).  K and V of the next tile go from memory into the other half of LDS while this one is
+// worked on, past the registers; one barrier a tile.  Tiles that every row sees skip the masks, waves whose rows see nothing of a
 // tile skip it.  What bounds it: matrix products and the exponentials between them, which take about as long.
+#include <type_traits>
+
 #include "rkc_cache_dev.h"
 
 namespace {
@@ -13,14 +15,14 @@ constexpr int kRows = 128, kThreads = 256;
 static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int BK = D == 256 ? 32 : 64, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
   constexpr int P = BK * CH / kThreads;  // 16-byte pieces of K, and of V, per thread
   constexpr int kTile = BK * D;
   __shared__ __attribute__((aligned(16))) T lds[4 * kTile];  // K, V of two tiles
   __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
-  __shared__ int depths[RKC_MAX_TREE_ROWS], lim[4][4], hurt_at[2];
+  __shared__ int depths[RKC_MAX_TREE_ROWS], lim[4][2];
 
   const int H = c.kv_heads, G = a.q_heads / H;
   int b = blockIdx.x;
@@ -67,13 +69,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
   if (a.d_row_start) all_from = wave_max(row.start), any_from = wave_min(row.start);
   const int all_to = uni(row.end), pre = uni(row.prefix);  // a wave's first lane has its first row
   const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, 31));
-  if (lane == 0) lim[wave][0] = all_from, lim[wave][1] = all_to, lim[wave][2] = any_from, lim[wave][3] = any_to;
-  if (tid < 2) hurt_at[tid] = -1;
+  if (lane == 0) lim[wave][0] = any_from, lim[wave][1] = any_to;
   __syncthreads();
-  const int g_all_from = max(max(lim[0][0], lim[1][0]), max(lim[2][0], lim[3][0]));
-  const int g_all_to = min(min(lim[0][1], lim[1][1]), min(lim[2][1], lim[3][1]));
-  const int g_any_from = min(min(lim[0][2], lim[1][2]), min(lim[2][2], lim[3][2]));
-  const int g_any_to = max(max(lim[0][3], lim[1][3]), max(lim[2][3], lim[3][3]));
+  const int g_any_from = min(min(lim[0][0], lim[1][0]), min(lim[2][0], lim[3][0]));
+  const int g_any_to = max(max(lim[0][1], lim[1][1]), max(lim[2][1], lim[3][1]));
   const int end = min(c1, g_any_to);
 
   const Pool kp = k_pool(c, h), vp = v_pool(c, h);
@@ -85,7 +84,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
 #pragma unroll
     for (int k = 0; k < 16; k++) o[d][k] = 0.f;
 
-  u32x4 ks[P], vs[P];
   int page[P];  // of this thread's pieces of the tile after the next: a wave's pieces lie in rows of one page
   bool bad = false;
   auto run_of = [&](int t0, int p) {  // first slot of the 16 that piece p lies in; one behind the end stands for the first
@@ -96,58 +94,61 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
 #pragma unroll
     for (int p = 0; p < P; p++) page[p] = page_of(c, table, shift, run_of(t0, p), bad);
   };
-  auto load = [&](int t0) {
+  // the pieces go where the tile's layout has them: the chunk that belongs there is the lane's to fetch
+  auto load = [&](int t0, int buf) {
+    T* to = lds + buf * 2 * kTile + wave * 64 * 8;
 #pragma unroll
     for (int p = 0; p < P; p++) {
-      const uint32_t piece = p * kThreads + tid, r = piece / CH & 15, e = piece % CH * 16;
+      const uint32_t piece = p * kThreads + tid, r = piece / CH, e = (tile_at<D>(r, piece % CH) - r * D) * 2, in_run = r & 15;
       const int at = run_of(t0, p) & in_page;
-      ks[p] = *(const u32x4*)(run_at(kp, page[p], at) + (r * kp.slot + e));
-      vs[p] = *(const u32x4*)(run_at(vp, page[p], at) + (r * vp.slot + e));
+      dma(run_at(kp, page[p], at) + (in_run * kp.slot + e), to + p * kThreads * 8);
+      dma(run_at(vp, page[p], at) + (in_run * vp.slot + e), to + kTile + p * kThreads * 8);
     }
   };
-  auto store = [&](int t0, int buf) {
-    T* to = lds + buf * 2 * kTile;
-    const bool whole = t0 + BK <= pre || (t0 >= g_all_from && t0 + BK <= g_all_to);
-    bool hurt = false;
-#pragma unroll
-    for (int p = 0; p < P; p++) {
-      const int piece = p * kThreads + tid, r = piece / CH, j = t0 + r;
-      u32x4 x = vs[p];
-      if (!whole) {
-        if (j >= end || (j < g_any_from && j >= pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
-        hurt |= any_hurt<T>(x);
-      }
-      *(u32x4*)(to + tile_at<D>(r, piece % CH)) = ks[p];
-      *(u32x4*)(to + kTile + tile_at<D>(r, piece % CH)) = x;
-    }
-    if (hurt) hurt_at[buf] = t0;
-  };
+  const int vi = lane & 15, vr = 4 * half + (vi >> 2), vc = (lane >> 4 & 1) * 2 + ((vi & 3) >> 1), ve = (vi & 1) * 4;
+  const int key_at = 2 * tile_at<D>(col, half), val_at = 2 * (kTile + tile_at<D>(vr, vc) + ve);
   auto skip = [&](int t) { return t + BK <= g_any_from && t >= pre; };
-
   auto after = [&](int t) {
     while (t < end && skip(t)) t += BK;
     return t;
   };
-  int t0 = after(c0), next = end, buf = 0;
+  const int first = after(c0);
+  auto go_over = [&](auto with_care) {
+  constexpr bool careful = decltype(with_care)::value;
+  int t0 = first, next = end, buf = 0;
   if (t0 < end) {
     look_up(t0);
-    load(t0);
+    load(t0, 0);
     next = after(t0 + BK);
     if (next < end) look_up(next);
-    store(t0, 0);
   }
-  __syncthreads();
   while (t0 < end) {
+    dma_barrier();
+    if (next < end) load(next, buf ^ 1);
     const int then = next < end ? after(next + BK) : end;
-    if (next < end) load(next);
     if (then < end) look_up(then);
-    T* kt_ = lds + buf * 2 * kTile;
-    T* vt_ = kt_ + kTile;
-    const int vi = lane & 15, vr = 4 * half + (vi >> 2), vc = (lane >> 4 & 1) * 2 + ((vi & 3) >> 1), ve = (vi & 1) * 4;
+    T* vt_ = lds + buf * 2 * kTile + kTile;
+    // byte offsets of this lane's first key and first values of the tile; the others differ by an exclusive or
+    // (chunks along a row) and by whole rows
+    const int ka = here(buf * 4 * kTile + key_at), va = here(buf * 4 * kTile + val_at);
+    auto keys = [&](int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k << 5) + 64 * D * u); };
+    auto vals = [&](int u, int v, int d) {
+      return read_tr2<T>((const char*)lds + (va ^ d << 6) + 32 * D * (2 * u + v), (const char*)lds + (va ^ d << 6 ^ 32) + 32 * D * (2 * u + v) + 16 * D);
+    };
+    bool hurt = false;
+    if (t0 + BK > end || careful) {  // what lies behind the last slot that a row sees must not enter a product
+      for (int k = tid; k < BK * CH; k += kThreads) {
+        const int j = t0 + k / CH;
+        V8* v = (V8*)(vt_ + 8 * k);
+        if (j >= end || (j < g_any_from && j >= pre)) *v = __builtin_bit_cast(V8, u32x4{0, 0, 0, 0});
+        else if constexpr (careful) hurt |= any_hurt<T>(__builtin_bit_cast(u32x4, *v));
+      }
+      if constexpr (careful) hurt = __syncthreads_or(hurt);
+      else __syncthreads();
+    }
     // whether any of the wave's rows sees anything of the tile, and whether all see all of it
     const bool sees = (t0 + BK > any_from && t0 < any_to) || t0 < pre;
     const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
-    const bool hurt = hurt_at[buf] == t0;
     f32x16 sc[KT];
     uint32_t seen[KT];
     if (sees) {
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
 #pragma unroll
         for (int k = 0; k < 16; k++) sc[u][k] = 0.f;
 #pragma unroll
-        for (int k = 0; k < KC; k++) sc[u] = mma32(*(const V8*)(kt_ + tile_at<D>(32 * u + col, 2 * k + half)), qf[k], sc[u]);
+        for (int k = 0; k < KC; k++) sc[u] = mma32(keys(u, k), qf[k], sc[u]);
       }
       if (a.softcap > 0.f) {
 #pragma unroll
@@ -165,16 +166,19 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
           for (int k = 0; k < 16; k++) sc[u][k] = capped(sc[u][k], f);
       }
       if (a.d_slope) {
+        const int base_at = here(q.base - t0 - 4 * half);
+        const float far = (float)(here(row.pos - t0) - 4 * half);
 #pragma unroll
         for (int u = 0; u < KT; u++)
 #pragma unroll
           for (int k = 0; k < 16; k++) {
-            int j = t0 + 32 * u + (k & 3) + 8 * (k >> 2) + 4 * half;
+            const int j = 32 * u + (k & 3) + 8 * (k >> 2);
+            float gap = far - (float)j;
             if (drafts && t0 + BK > q.base) {
-              const int d = depths[max(0, min(j - q.base, RKC_MAX_TREE_ROWS - 1))];
-              j = j >= q.base ? q.base + d : j;
+              const int i = j - base_at, d = depths[max(0, min(i, RKC_MAX_TREE_ROWS - 1))];
+              gap = i >= 0 ? (float)(row.pos - q.base - d) : gap;
             }
-            sc[u][k] -= slope * fabsf((float)(row.pos - j));
+            sc[u][k] = __builtin_fmaf(-slope, fabsf(gap), sc[u][k]);
           }
       }
 #pragma unroll
@@ -202,20 +206,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
         for (int d = 0; d < DB; d++) o[d] *= by;
       }
     }
-    if (hurt) {  // the same for the whole workgroup
+    if constexpr (careful) if (hurt) {  // the same for the whole workgroup
       if (sees) {
 #pragma unroll
         for (int d = 0; d < DB; d++) {
           f32x16 n;
 #pragma unroll
           for (int k = 0; k < 16; k++) n[k] = 0.f;
+#pragma unroll 1
+          for (int x = 0; x < 2 * KT; x++) {
+              const int u = x >> 1, v = x & 1;
+              const uint32_t bits = KT > 1 && u ? seen[KT - 1] : seen[0];
+              V8 by, vt = vals(u, v, d);
 #pragma unroll
-          for (int u = 0; u < KT; u++)
-#pragma unroll
-            for (int v = 0; v < 2; v++) {
-              V8 by, vt = read_tr2<T>(vt_ + tile_at<D>(32 * u + 16 * v + vr, 4 * d + vc) + ve, vt_ + tile_at<D>(32 * u + 16 * v + vr + 8, 4 * d + vc) + ve);
-#pragma unroll
-              for (int k = 0; k < 8; k++) by[k] = (T)(seen[u] >> (16 * v + (k & 3) + 8 * (k >> 2)) & 1 ? 1.f : 0.f);
+              for (int k = 0; k < 8; k++) by[k] = (T)(bits >> (16 * v + (k & 3) + 8 * (k >> 2)) & 1 ? 1.f : 0.f);
               n = mma32(strip<T>(vt), by, n);
             }
 #pragma unroll
@@ -242,17 +246,31 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 128 ? 2 : 3) void att
           sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
           // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
           const V8 pb = __builtin_convertvector(p, V8);
-          const int r = 32 * u + 16 * v + vr;
 #pragma unroll
           for (int d = 0; d < DB; d++)
-            o[d] = mma32(read_tr2<T>(vt_ + tile_at<D>(r, 4 * d + vc) + ve, vt_ + tile_at<D>(r + 8, 4 * d + vc) + ve), pb, o[d]);
+            o[d] = mma32(vals(u, v, d), pb, o[d]);
         }
       }
     }
     buf ^= 1;
-    if (next < end) store(next, buf);
-    __syncthreads();
     t0 = next, next = then;
+  }
+  };
+  go_over(std::false_type());
+  // A value that is not finite reaches rows that do not see its slot, through a weight of zero.  That shows in the
+  // outputs, and then all is done once more with care.
+  float odd = 0.f;  // stays 0 unless an output is not finite
+#pragma unroll
+  for (int d = 0; d < DB; d++)
+#pragma unroll
+    for (int k = 0; k < 16; k++) odd = __builtin_fmaf(o[d][k], 0.f, odd);
+  if (__syncthreads_or(odd != 0.f)) {
+    top = -kInf, sum = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+      for (int k = 0; k < 16; k++) o[d][k] = 0.f;
+    go_over(std::true_type());
   }
   if (bad) flag(c, s, RKC_CS_BLOCK);
 

@@ -79,13 +79,33 @@ template <int D> __device__ __forceinline__ int tile_at(int r, int c) {
   return r * D + ((c ^ x) << 3);
 }
 
+// Keeps the compiler from moving what follows from x out of a loop, where every element of a tile would cost a register.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// 16 bytes a lane from memory into LDS, past the registers: lane l's go to `to` + 16 l.  The loads of a wave are done
+// when its vector memory count says so (dma_barrier); what other waves loaded, behind the next barrier.
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void glb_void;
+__device__ __forceinline__ void dma(const char* from, void* to) {
+  __builtin_amdgcn_global_load_lds((glb_void*)from, (lds_void*)to, 16, 0, 0);
+}
+// Waits for this wave's loads and its LDS accesses, then for the workgroup.
+__device__ __forceinline__ void dma_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // 4 slots x 16 columns, transposed within each 16 lanes: lane i gets column i of the 4 slots whose addresses
 // lanes 4 s .. 4 s + 3 give (8 bytes each).
 __device__ __forceinline__ s16x4 read_tr(const void* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
 
-template <typename T> __device__ __forceinline__ typename Vec8<T>::t read_tr2(const T* a, const T* b) {
+template <typename T> __device__ __forceinline__ typename Vec8<T>::t read_tr2(const void* a, const void* b) {
   const s16x4 x = read_tr(a), y = read_tr(b);
   const s16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
   return __builtin_bit_cast(typename Vec8<T>::t, z);
