@@ -17,10 +17,10 @@ static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
-  constexpr int BK = D == 256 ? 32 : 64, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
+  constexpr int BK = D == 256 ? 32 : 64, kAhead = D == 256 ? 3 : 1, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
   constexpr int P = BK * CH / kThreads;  // 16-byte pieces of K, and of V, per thread
   constexpr int kTile = BK * D;
-  __shared__ __attribute__((aligned(16))) T lds[4 * kTile];  // K, V of two tiles
+  __shared__ __attribute__((aligned(16))) T lds[(kAhead + 1) * 2 * kTile];  // K and V of each tile
   __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
   __shared__ int depths[RKC_MAX_TREE_ROWS], lim[4][2];
 
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
   const int m = min(m0 + 32 * wave + col, M - 1), qi = m / G, qh = h * G + m % G;
-  const bool mine = m0 + 32 * wave + col < M;
+  const bool mine = m0 + 32 * wave + col < M, rows = m0 + 32 * wave < M;
   const Scale f = load_scale(a);
   Row row = load_row(a, q, s, qi);
   const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
@@ -71,8 +71,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, 31));
   if (lane == 0) lim[wave][0] = any_from, lim[wave][1] = any_to;
   __syncthreads();
-  const int g_any_from = min(min(lim[0][0], lim[1][0]), min(lim[2][0], lim[3][0]));
-  const int g_any_to = max(max(lim[0][1], lim[1][1]), max(lim[2][1], lim[3][1]));
+  const int g_any_from = uni(min(min(lim[0][0], lim[1][0]), min(lim[2][0], lim[3][0])));
+  const int g_any_to = uni(max(max(lim[0][1], lim[1][1]), max(lim[2][1], lim[3][1])));
   const int end = min(c1, g_any_to);
 
   const Pool kp = k_pool(c, h), vp = v_pool(c, h);
@@ -84,49 +84,61 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
 #pragma unroll
     for (int k = 0; k < 16; k++) o[d][k] = 0.f;
 
-  int page[P];  // of this thread's pieces of the tile after the next: a wave's pieces lie in rows of one page
+  // The tiles that any row sees, in order: from c0 on, less those between the prefix and the first document.
+  const int end_up = c0 + (max(0, end - c0) + BK - 1) / BK * BK;
+  const int gap_from = min(max((pre + BK - 1) / BK * BK, c0), end_up), gap_to = min(max(g_any_from / BK * BK, gap_from), end_up);
+  const int n_tiles = (end_up - c0 - (gap_to - gap_from)) / BK;
+  auto slot_of = [&](int i) {
+    const int t = c0 + i * BK;
+    return t >= gap_from ? t + (gap_to - gap_from) : t;
+  };
   bool bad = false;
-  auto run_of = [&](int t0, int p) {  // first slot of the 16 that piece p lies in; one behind the end stands for the first
-    const int at = t0 + uni((p * kThreads + tid) / CH & ~15);
+  // this thread's pieces of a tile: a wave's pieces of one load lie in 16 slots of one page
+  const int lane_run = uni(tid / CH & ~15);
+  uint32_t k_off[2], v_off[2];  // of a piece in its run; the chunk is the one that the tile's layout has at its place
+#pragma unroll
+  for (int p = 0; p < 2; p++) {
+    const uint32_t r = (p * kThreads + tid) / CH, e = (tile_at<D>(r, tid % CH) - r * D) * 2;
+    k_off[p] = (r & 15) * kp.slot + e, v_off[p] = (r & 15) * vp.slot + e;
+  }
+  int page[P];  // of the next tile to be loaded
+  auto run_of = [&](int t0, int p) {  // a run behind the end stands for the first one
+    const int at = t0 + lane_run + (p * kThreads / CH & ~15);
     return at < end ? at : t0;
   };
-  auto look_up = [&](int t0) {
+  auto look_up = [&](int i) {
+    const int t0 = slot_of(i);
 #pragma unroll
     for (int p = 0; p < P; p++) page[p] = page_of(c, table, shift, run_of(t0, p), bad);
   };
-  // the pieces go where the tile's layout has them: the chunk that belongs there is the lane's to fetch
-  auto load = [&](int t0, int buf) {
+  auto load = [&](int i, int buf) {
+    const int t0 = slot_of(i);
     T* to = lds + buf * 2 * kTile + wave * 64 * 8;
 #pragma unroll
     for (int p = 0; p < P; p++) {
-      const uint32_t piece = p * kThreads + tid, r = piece / CH, e = (tile_at<D>(r, piece % CH) - r * D) * 2, in_run = r & 15;
-      const int at = run_of(t0, p) & in_page;
-      dma(run_at(kp, page[p], at) + (in_run * kp.slot + e), to + p * kThreads * 8);
-      dma(run_at(vp, page[p], at) + (in_run * vp.slot + e), to + kTile + p * kThreads * 8);
+      const int at = run_of(t0, p) & in_page, o = kThreads / CH >= 16 ? 0 : p & 1;
+      dma(fixed(run_at(kp, page[p], at)) + k_off[o], to + p * kThreads * 8);
+      dma(fixed(run_at(vp, page[p], at)) + v_off[o], to + kTile + p * kThreads * 8);
     }
   };
   const int vi = lane & 15, vr = 4 * half + (vi >> 2), vc = (lane >> 4 & 1) * 2 + ((vi & 3) >> 1), ve = (vi & 1) * 4;
   const int key_at = 2 * tile_at<D>(col, half), val_at = 2 * (kTile + tile_at<D>(vr, vc) + ve);
-  auto skip = [&](int t) { return t + BK <= g_any_from && t >= pre; };
-  auto after = [&](int t) {
-    while (t < end && skip(t)) t += BK;
-    return t;
-  };
-  const int first = after(c0);
   auto go_over = [&](auto with_care) {
   constexpr bool careful = decltype(with_care)::value;
-  int t0 = first, next = end, buf = 0;
-  if (t0 < end) {
-    look_up(t0);
-    load(t0, 0);
-    next = after(t0 + BK);
-    if (next < end) look_up(next);
+  // kAhead tiles are on their way while one is worked on
+  look_up(0);
+#pragma unroll
+  for (int i = 0; i < kAhead; i++) {
+    if (i < n_tiles) load(i, i);
+    if (i + 1 < n_tiles) look_up(i + 1);
   }
-  while (t0 < end) {
-    dma_barrier();
-    if (next < end) load(next, buf ^ 1);
-    const int then = next < end ? after(next + BK) : end;
-    if (then < end) look_up(then);
+  int buf = 0;
+  for (int i = 0; i < n_tiles; i++) {
+    const int t0 = slot_of(i);
+    if (i + kAhead <= n_tiles) dma_barrier<2 * P * (kAhead - 1)>();
+    else dma_barrier<0>();
+    if (i + kAhead < n_tiles) load(i + kAhead, buf ? buf - 1 : kAhead);
+    if (i + kAhead + 1 < n_tiles) look_up(i + kAhead + 1);
     T* vt_ = lds + buf * 2 * kTile + kTile;
     // byte offsets of this lane's first key and first values of the tile; the others differ by an exclusive or
     // (chunks along a row) and by whole rows
@@ -147,7 +159,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
       else __syncthreads();
     }
     // whether any of the wave's rows sees anything of the tile, and whether all see all of it
-    const bool sees = (t0 + BK > any_from && t0 < any_to) || t0 < pre;
+    const bool sees = rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre);
     const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
     f32x16 sc[KT];
     uint32_t seen[KT];
@@ -252,8 +264,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
         }
       }
     }
-    buf ^= 1;
-    t0 = next, next = then;
+    buf = buf == kAhead ? 0 : buf + 1;
   }
   };
   go_over(std::false_type());

@@ -85,6 +85,12 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
+// The same for a pointer in scalar registers, so that a load takes it from there with the lane's 32-bit offset.
+__device__ __forceinline__ const char* fixed(const char* p) {
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
 // 16 bytes a lane from memory into LDS, past the registers: lane l's go to `to` + 16 l.  The loads of a wave are done
 // when its vector memory count says so (dma_barrier); what other waves loaded, behind the next barrier.
 typedef __attribute__((address_space(3))) void lds_void;
@@ -92,9 +98,9 @@ typedef const __attribute__((address_space(1))) void glb_void;
 __device__ __forceinline__ void dma(const char* from, void* to) {
   __builtin_amdgcn_global_load_lds((glb_void*)from, (lds_void*)to, 16, 0, 0);
 }
-// Waits for this wave's loads and its LDS accesses, then for the workgroup.
-__device__ __forceinline__ void dma_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+// Waits for this wave's loads but the last N, and its LDS accesses, then for the workgroup.
+template <int N> __device__ __forceinline__ void dma_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -151,6 +157,12 @@ __device__ __forceinline__ float hurt_by(float codes) {
   return x;
 }
 
+// A word that no kernel of the call writes, at an address that is the same for the wave: loaded as a scalar, also behind
+// barriers, where the compiler must otherwise expect it to have changed.
+template <typename T> __device__ __forceinline__ T word(const T* p, int64_t i) {
+  return ((const __attribute__((address_space(4))) T*)p)[i];
+}
+
 // ------------------------------------------------------------------------------------------------------------
 // What a row sees.  Slots [start, end) and [0, prefix), and of a tree's drafted slots those of `line`.
 struct Row {
@@ -166,8 +178,8 @@ struct Seq {
 // Reads and checks a sequence's row range and length.
 __device__ __forceinline__ Seq load_seq(const rkc_cache& c, const rkc_attention& a, int s) {
   Seq q;
-  const int r0 = a.d_row_offset[s], r1 = a.d_row_offset[s + 1];
-  q.row0 = r0, q.n = r1 - r0, q.len = a.d_length[s], q.base = q.len - q.n;
+  const int r0 = word(a.d_row_offset, s), r1 = word(a.d_row_offset, s + 1);
+  q.row0 = r0, q.n = r1 - r0, q.len = word(a.d_length, s), q.base = q.len - q.n;
   q.ok = r0 >= 0 && r1 >= r0 && r1 <= a.n_rows && q.n <= a.max_rows && q.len >= 0 && q.len <= a.max_len && q.n <= q.len;
   return q;
 }
@@ -180,7 +192,7 @@ __device__ __forceinline__ Row load_row(const rkc_attention& a, const Seq& q, in
   Row r;
   r.start = a.d_row_start ? max(0, a.d_row_start[q.row0 + i]) : 0;
   r.end = a.d_parent ? q.base : q.base + i + 1;
-  r.prefix = a.d_prefix ? max(0, min(a.d_prefix[s], a.d_parent ? q.base : q.len)) : 0;
+  r.prefix = a.d_prefix ? max(0, min(word(a.d_prefix, s), a.d_parent ? q.base : q.len)) : 0;
   r.pos = q.base + i;
   return r;
 }
@@ -230,7 +242,7 @@ __device__ __forceinline__ uint32_t line_window(const uint64_t* line, int words,
 // The end of the slots that the tile's rows up to `last` see.
 __device__ __forceinline__ int rows_end(const rkc_attention& a, const Seq& q, int s, int last) {
   if (a.d_parent) return q.len;
-  const int pre = a.d_prefix ? max(0, min(a.d_prefix[s], q.len)) : 0;
+  const int pre = a.d_prefix ? max(0, min(word(a.d_prefix, s), q.len)) : 0;
   return max(pre, q.base + last + 1);
 }
 
@@ -263,9 +275,10 @@ __device__ __forceinline__ const char* run_at(const Pool& p, int page, int in_pa
   return p.base + (uint64_t)(uint32_t)page * p.block + (uint32_t)in_page * p.slot;
 }
 
-// Block of the page that slot t lies in; block 0 for an id outside the pool, which `bad` remembers.
+// Block of the page that slot t, the same for the wave, lies in; block 0 for an id outside the pool, which `bad`
+// remembers.
 __device__ __forceinline__ int page_of(const rkc_cache& c, const int32_t* table, int shift, int t, bool& bad) {
-  const int id = table[t >> shift];
+  const int id = word(table, t >> shift);
   const bool out = (uint32_t)id >= (uint32_t)c.n_blocks;
   bad |= out;
   return out ? 0 : id;

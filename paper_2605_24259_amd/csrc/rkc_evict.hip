@@ -249,7 +249,13 @@ __global__ __launch_bounds__(256) void evict_move(const evict_args g, int chunks
   for (int x = threadIdx.x; x < n * per; x += 256) {
     const int i = x / per, e = x % per * 8, to = gaps[i], at = from[i];
     bool bad = false;
-    const int64_t pt = page_of(c, table, shift, to, bad), pf = page_of(c, table, shift, at, bad);
+    auto page = [&](int t) {
+      const int id = table[t >> shift];
+      const bool out = (uint32_t)id >= (uint32_t)c.n_blocks;
+      bad |= out;
+      return (int64_t)(out ? 0 : id);
+    };
+    const int64_t pt = page(to), pf = page(at);
     if (bad) flag(c, s, RKC_CS_BLOCK);
     const int in_page = c.page_tokens - 1;
     uint16_t* k = (uint16_t*)c.d_k + h * c.k_head_stride + e;

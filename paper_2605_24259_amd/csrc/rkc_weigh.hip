@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_a
   const bool tree = a.d_parent != nullptr;
   const bool drafts = tree && w0 + 4 * kSlots > q.base;
   if (drafts || (tree && a.d_slope)) tree_lines(c, a, q, s, part == 0 && h == 0, lines, depths);
-  const int pre = a.d_prefix ? max(0, min(a.d_prefix[s], tree ? q.base : q.len)) : 0;
+  const int pre = a.d_prefix ? max(0, min(word(a.d_prefix, s), tree ? q.base : q.len)) : 0;
   const Scale sc = load_scale(a);
   float acc[NS] = {};
 
