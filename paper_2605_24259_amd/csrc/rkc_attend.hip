@@ -42,6 +42,37 @@ __global__ __launch_bounds__(256) void attend_join(const rkc_cache c, const rkc_
   if (lane == 0) a.d_lse[row * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
 }
 
+// The account from kept scores: one slot of four a thread.
+__global__ __launch_bounds__(256) void attend_account(const rkc_cache c, const rkc_attention a, const rkc_plan pl, int parts) {
+  const int H = c.kv_heads, G = a.q_heads / H, part = blockIdx.x % parts, unit = blockIdx.x / parts, s = unit / H, h = unit % H;
+  const Seq q = load_seq(c, a, s);
+  if (!q.ok || part * 1024 >= q.len) return;
+  const int M = q.n * G;
+  const float* sc = (const float*)((const char*)a.d_scratch + pl.score_at) + (int64_t)unit * (a.max_rows * G) * pl.wide;
+  const int64_t at = s * a.weight_seq_stride + h * a.weight_head_stride;
+  float got[4] = {}, in[4] = {};
+#pragma unroll
+  for (int k = 0; k < 4; k++) {
+    const int j = part * 1024 + k * 256 + threadIdx.x;
+    if (a.d_weight_in && j < q.len) in[k] = a.decay * a.d_weight_in[at + j];
+  }
+  for (int m = 0; m < M; m++) {
+    const float lse = a.d_lse[(int64_t)(q.row0 + m / G) * a.q_heads + h * G + m % G];
+    const float z = lse == -kInf ? kInf : lse * kLog2e;  // a row that saw nothing gave nothing
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const int j = part * 1024 + k * 256 + threadIdx.x;
+      const float x = j < q.len ? sc[(int64_t)m * pl.wide + j] : -kInf;
+      got[k] += x == -kInf ? 0.f : ex2(x - z);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; k++) {
+    const int j = part * 1024 + k * 256 + threadIdx.x;
+    if (j < q.len) a.d_weight[at + j] = in[k] + got[k];
+  }
+}
+
 template <typename T>
 rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
   const int64_t waves = (int64_t)c->n_seqs * c->kv_heads * p->tiles * p->rows;
@@ -125,7 +156,16 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
     const size_t rows = (size_t)units * p.splits * p.rows;
     p.part_at = 0;
     p.stat_at = rows * c->head_dim * 4;
-    p.bytes = p.stat_at + rows * 8;
+    p.bytes = (p.stat_at + rows * 8 + 255) & ~(size_t)255;
+  }
+  // The account by scores kept (written and read: 8 bytes per slot and packed row) where that is at most half of what
+  // reading the keys again would be (2 bytes per slot and element of a head).
+  // (Not with documents: slots that no row sees are passed over, and would keep no score.)
+  p.keep = a->d_weight && !a->d_row_start && p.few && M <= c->head_dim / 8 && M <= 16;
+  if (p.keep) {
+    p.wide = (a->max_len + 31) & ~31;
+    p.score_at = p.bytes;
+    p.bytes += (size_t)units * M * p.wide * 4;
   }
   return p;
 }
@@ -150,8 +190,12 @@ rkc_status rkc_attend(const rkc_cache* c, const rkc_attention* a, void* stream) 
   }
   rkc_status st = p.few ? rkc_attend_few(c, a, &p, s) : rkc_attend_tile(c, a, &p, s);
   if (st == RKC_OK && p.splits > 1) st = c->dtype == RKC_BF16 ? join<__bf16>(c, a, &p, s) : join<_Float16>(c, a, &p, s);
-  if (st == RKC_OK && a->d_weight) st = rkc_weigh(c, a, stream);
-  return st;
+  if (st != RKC_OK || !a->d_weight) return st;
+  if (!p.keep) return rkc_weigh(c, a, stream);
+  const int parts = (a->max_len + 1023) / 1024;
+  if ((int64_t)p.units * parts > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  attend_account<<<dim3(p.units * parts), dim3(256), 0, s>>>(*c, *a, p, parts);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 }  // extern "C"

@@ -117,33 +117,51 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
     for (int d = 0; d < DB; d++) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // The tiles of 32 slots that any row sees, in order: from c0 on, less those between the prefix and the first document.
+  const int end_up = c0 + (max(0, end - c0) + 31) / 32 * 32;
+  const int gap_from = min(max((all_pre + 31) / 32 * 32, c0), end_up), gap_to = min(max(any_from / 32 * 32, gap_from), end_up);
+  const int n_tiles = (end_up - c0 - (gap_to - gap_from)) / 32;
+  auto slot_of = [&](int i) {
+    const int t = c0 + i * 32;
+    return t >= gap_from ? t + (gap_to - gap_from) : t;
+  };
   V8 kf[2][KC];
   u32x4 vf[VP];
   bool bad = false;
-  // the 32 slots from t0 on: two runs of 16, each within a page; a run behind the chunk repeats the first
-  auto load = [&](int t0) {
+  int page[2];  // of the next tile to be loaded: two runs of 16 slots, each within a page
+  auto run_of = [&](int t0, int u) { return u && t0 + 16 >= end ? t0 : t0 + 16 * u; };  // one behind the end repeats the first
+  auto look_up = [&](int i) {
+    const int t0 = slot_of(i);
+#pragma unroll
+    for (int u = 0; u < 2; u++) page[u] = page_of(c, table, shift, run_of(t0, u), bad);
+  };
+  constexpr int RP = 512 / D;  // rows of a piece of V: 64 lanes of 16 bytes
+  const uint32_t k_off = col * kp.slot + quad * 16, v_off = lane / (D / 8) * vp.slot + lane % (D / 8) * 16;
+  auto load = [&](int i) {
+    const int t0 = slot_of(i);
 #pragma unroll
     for (int u = 0; u < 2; u++) {
-      const int at = u && t0 + 16 >= end ? t0 : t0 + 16 * u;
-      const int page = page_of(c, table, shift, at, bad);
-      const char* kb = run_at(kp, page, at & in_page);
-      const char* vb = run_at(vp, page, at & in_page);
+      const int at = run_of(t0, u) & in_page;
+      const char* kb = fixed(run_at(kp, page[u], at));
+      const char* vb = run_at(vp, page[u], at);
 #pragma unroll
-      for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + (col * kp.slot + quad * 16u) + 64 * k);
+      for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + k_off + 64 * k);
 #pragma unroll
-      for (int p = 0; p < VP / 2; p++) {
-        const uint32_t piece = p * 64 + lane, r = piece / (D / 8), e = piece % (D / 8) * 16;
-        vf[u * (VP / 2) + p] = *(const u32x4*)(vb + (r * vp.slot + e));
-      }
+      for (int p = 0; p < VP / 2; p++) vf[u * (VP / 2) + p] = *(const u32x4*)(fixed(vb + p * RP * vp.slot) + v_off);
     }
   };
+  // byte offsets in the tile: of this lane's piece of V, and of its first values for a product
+  const int put_at = 2 * tile_at<D>(lane / (D / 8), lane % (D / 8));
+  const int val_at = 2 * (tile_at<D>(quad * 4 + (col >> 2), (col & 3) >> 1) + (col & 1) * 4);
 
-  const int step = 32 * kWaves;
-  int t0 = c0 + 32 * wave;
-  auto skip = [&](int t) { return t + 32 <= any_from && t >= all_pre; };  // no row sees anything there
-  while (t0 < end && skip(t0)) t0 += step;
-  if (t0 < end) load(t0);
-  while (t0 < end) {
+  int i = wave;
+  if (i < n_tiles) {
+    look_up(i);
+    load(i);
+    if (i + kWaves < n_tiles) look_up(i + kWaves);
+  }
+  for (; i < n_tiles; i += kWaves) {
+    const int t0 = slot_of(i);
     f32x4 sc[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; t++)
@@ -155,21 +173,22 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
       }
     const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
     bool hurt = false;
+    const int pa = here(put_at), va = here(val_at);
+    auto put = [&](int p, u32x4 x) { *(u32x4*)((char*)tile + ((pa ^ tile_x<D>(p * RP) << 4) + p * RP * 2 * D)) = x; };
+    if (whole) {
 #pragma unroll
-    for (int p = 0; p < VP; p++) {
-      const int piece = (p % (VP / 2)) * 64 + lane, r = p / (VP / 2) * 16 + piece / (D / 8), j = t0 + r;
-      u32x4 x = vf[p];
-      if (!whole) {
+      for (int p = 0; p < VP; p++) put(p, vf[p]);
+    } else {
+#pragma unroll
+      for (int p = 0; p < VP; p++) {
+        const int j = t0 + p * RP + lane / (D / 8);
+        u32x4 x = vf[p];
         if (j >= end || (j < any_from && j >= all_pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
         hurt |= any_hurt<T>(x);
+        put(p, x);
       }
-      *(u32x4*)(tile + tile_at<D>(r, piece % (D / 8))) = x;
+      hurt = __any(hurt);
     }
-    hurt = __any(hurt);
-    int next = t0 + step;
-    while (next < end && skip(next)) next += step;
-    if (next < end) load(next);
-
     uint32_t seen[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
@@ -178,14 +197,15 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
         for (int e = 0; e < 8; e++) sc[t][e >> 2][e & 3] = capped(sc[t][e >> 2][e & 3], f);
       }
       if (a.d_slope) {
+        const float far = (float)(here(row[t].pos - t0) - quad * 4);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          int j = t0 + quad * 4 + (e >> 2) * 16 + (e & 3);
+          float gap = far - (float)(16 * (e >> 2) + (e & 3));
           if (a.d_parent && t0 + 32 > q.base) {
-            const int d = __shfl(depth_of, (j - q.base) & 63);
-            j = j >= q.base ? q.base + d : j;
+            const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
+            gap = at >= 0 ? (float)(row[t].pos - q.base - d) : gap;
           }
-          sc[t][e >> 2][e & 3] -= slope[t] * fabsf((float)(row[t].pos - j));
+          sc[t][e >> 2][e & 3] = __builtin_fmaf(-slope[t], fabsf(gap), sc[t][e >> 2][e & 3]);
         }
       }
       seen[t] = 0xffffffff;
@@ -197,7 +217,15 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
         for (int e = 0; e < 8; e++) sc[t][e >> 2][e & 3] = masked(sc[t][e >> 2][e & 3], seen[t], 16 * (e >> 2) + (e & 3));
       }
     }
-    const int vr = quad * 4 + (col >> 2), vc = (col & 3) >> 1, ve = (col & 1) * 4;
+    auto vals = [&](int d) { return read_tr2<T>((const char*)tile + (va ^ d << 5), (const char*)tile + (va ^ d << 5) + 32 * D); };
+    if (pl.keep) {  // one column tile
+      float* to = (float*)((char*)a.d_scratch + pl.score_at) + ((int64_t)(s * H + h) * (a.max_rows * G) + col) * pl.wide + t0 + quad * 4;
+      if (col < M) *(f32x4*)to = sc[0][0] * f.post, *(f32x4*)(to + 16) = sc[0][1] * f.post;
+    }
+    if (i + kWaves < n_tiles) {
+      load(i + kWaves);
+      if (i + 2 * kWaves < n_tiles) look_up(i + 2 * kWaves);
+    }
     V8 pb[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
@@ -227,7 +255,7 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
         for (int e = 0; e < 8; e++) by[e] = (T)(seen[t] >> (16 * (e >> 2) + (e & 3)) & 1 ? 1.f : 0.f);
 #pragma unroll
         for (int d = 0; d < DB; d++) {
-          V8 vt = read_tr2<T>(tile + tile_at<D>(vr, d * 2 + vc) + ve, tile + tile_at<D>(vr + 16, d * 2 + vc) + ve);
+          V8 vt = vals(d);
           const f32x4 n = mma16(strip<T>(vt), by, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int k = 0; k < 4; k++) o[t][d][k] += hurt_by(n[k]);
@@ -241,11 +269,10 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
     }
 #pragma unroll
     for (int d = 0; d < DB; d++) {
-      const V8 vt = read_tr2<T>(tile + tile_at<D>(vr, d * 2 + vc) + ve, tile + tile_at<D>(vr + 16, d * 2 + vc) + ve);
+      const V8 vt = vals(d);
 #pragma unroll
       for (int t = 0; t < NT; t++) o[t][d] = mma16(vt, pb[t], o[t][d]);
     }
-    t0 = next;
   }
 
   if (bad) flag(c, s, RKC_CS_BLOCK);

@@ -74,10 +74,9 @@ __device__ __forceinline__ int wave_max(int x) { return wave_all(x, [](int a, in
 // A tile of slots in LDS: rows of D elements in 16-byte chunks, the chunk's number xored with a number of
 // the row so that neither a column of chunks over 16 rows (keys) nor 32 bytes of 4, 8 or 16 neighbouring rows
 // (transposing reads of values) share banks.  Element offset of chunk `c` of row `r`.
-template <int D> __device__ __forceinline__ int tile_at(int r, int c) {
-  const int x = D == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
-  return r * D + ((c ^ x) << 3);
-}
+// (The number is linear in the row's bits: of a sum of rows without a carry it is the exclusive or of theirs.)
+template <int D> __device__ __forceinline__ constexpr int tile_x(int r) { return D == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3); }
+template <int D> __device__ __forceinline__ constexpr int tile_at(int r, int c) { return r * D + ((c ^ tile_x<D>(r)) << 3); }
 
 // Keeps the compiler from moving what follows from x out of a loop, where every element of a tile would cost a register.
 __device__ __forceinline__ int here(int x) {
@@ -327,6 +326,9 @@ struct rkc_plan {
   int rows;    // packed rows of a tile
   int chunk, splits;
   size_t part_at, stat_at, bytes;  // scratch: partial outputs, their maxima and sums, in all
+  bool keep;        // scores are kept for the account: [unit][packed row][slot], in units of log2
+  int wide;         // slots of a row of them
+  size_t score_at;
 };
 rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a);
 rkc_status rkc_attend_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);

@@ -1,24 +1,27 @@
 // rkc_weigh.hip -- the account of a cache: how much attention each of its slots received.
 //
-// Softmax sums are given, so slots are independent: a wave holds the keys of 64 slots (32 at 256 elements a head) in
-// registers as columns of 16x16x32 products and goes over the packed rows 16 at a time; a lane adds up the
-// weights of its slot's column in 32 bits, in a fixed order.  One read of the keys; no atomics.
+// Softmax sums are given, so slots are independent: a wave holds the keys of 32 slots in registers as columns of
+// 16x16x32 products, with those of its next 32 on their way, and goes over the packed rows, whose queries lie in
+// LDS, 16 at a time; a lane adds up the weights of its slot's column in 32 bits, in a fixed order.  One read of the
+// keys; no atomics.
 #include "rkc_cache_dev.h"
 
 namespace {
 
-constexpr int kThreads = 256, kBlock = 128;  // packed rows whose masks and sums lie in LDS at a time
+constexpr int kThreads = 256, kRuns = 2, kSlots = 16 * kRuns, kTurn = kThreads / 64 * kSlots;
+constexpr int kBlock = 128;  // packed rows whose queries, masks and sums lie in LDS at a time
 static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
 
 struct RowIn {
-  float lse2, slope;
   int start, end, pos, line;
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_attention a, int chunks) {
+__global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rkc_attention a, int chunks, int turns) {
   typedef typename Vec8<T>::t V8;
-  constexpr int KC = D / 32, NS = D == 256 ? 2 : 4, kSlots = 16 * NS;
+  constexpr int KC = D / 32;
+  __shared__ __attribute__((aligned(16))) T rows_q[kBlock * D];
+  __shared__ __attribute__((aligned(16))) float lse2[kBlock], slopes[kBlock];
   __shared__ RowIn in[kBlock];
   __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
   __shared__ int depths[RKC_MAX_TREE_ROWS];
@@ -31,110 +34,161 @@ __global__ __launch_bounds__(kThreads) void weigh(const rkc_cache c, const rkc_a
     if (part == 0 && h == 0 && tid == 0) flag(c, s, RKC_CS_LENGTH);
     return;
   }
-  const int w0 = part * 4 * kSlots, t0 = w0 + wave * kSlots;
+  const int w0 = part * turns * kTurn;
   if (w0 >= q.len) return;
-  const int M = q.n * G;
+  const int n_turns = min(turns, (q.len - w0 + kTurn - 1) / kTurn), M = q.n * G;
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
-  V8 kf[NS][KC];
+  const Pool kp = k_pool(c, h);
+  const uint32_t k_off = col * kp.slot + quad * 16;
   bool bad = false;
-  const T* kp = (const T*)c.d_k + h * c.k_head_stride;
+  V8 next[kRuns][KC];
+  auto load = [&](int turn) {
 #pragma unroll
-  for (int u = 0; u < NS; u++) {
-    const int at = min(t0 + 16 * u, (q.len - 1) & ~15);
-    const T* kb = kp + (int64_t)page_of(c, table, shift, at, bad) * c.k_block_stride + (at & in_page) * c.k_slot_stride + (int)(col * (int)c.k_slot_stride) + quad * 8;
+    for (int u = 0; u < kRuns; u++) {
+      const int at = min(w0 + turn * kTurn + wave * kSlots + 16 * u, (q.len - 1) & ~15);
+      const char* kb = run_at(kp, page_of(c, table, shift, at, bad), at & in_page);
 #pragma unroll
-    for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + 32 * k);
-  }
-  if (bad) flag(c, s, RKC_CS_BLOCK);
+      for (int k = 0; k < KC; k++) next[u][k] = *(const V8*)(kb + k_off + 64 * k);
+    }
+  };
+  load(0);
   const bool tree = a.d_parent != nullptr;
-  const bool drafts = tree && w0 + 4 * kSlots > q.base;
+  const bool drafts = tree && w0 + n_turns * kTurn > q.base;
   if (drafts || (tree && a.d_slope)) tree_lines(c, a, q, s, part == 0 && h == 0, lines, depths);
   const int pre = a.d_prefix ? max(0, min(word(a.d_prefix, s), tree ? q.base : q.len)) : 0;
   const Scale sc = load_scale(a);
-  float acc[NS] = {};
 
-  for (int mb = 0; mb < M; mb += kBlock) {
+  // queries, sums and masks of up to kBlock packed rows from row mb on
+  int rows = 0, all_from = 0, all_to = 0, any_from = 0, any_to = 0;  // what all of them see, and what any sees
+  auto stage = [&](int mb) {
     __syncthreads();
-    if (tid < kBlock) {
+    rows = min(kBlock, M - mb);
+    const int rows_up = (rows + 15) & ~15;
+    for (int x = tid; x < rows_up * (D / 8); x += kThreads) {
+      const int r = x / (D / 8), m = min(mb + r, M - 1), qi = m / G;
+      V8 v = *(const V8*)((const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + (h * G + m - qi * G) * a.q_head_stride + x % (D / 8) * 8);
+      *(V8*)(rows_q + tile_at<D>(r, x % (D / 8))) = sc.negate ? negated(v) : v;
+    }
+    if (tid < rows_up) {
       const int m = mb + tid;
-      RowIn r = {kInf, 0.f, 0x7fffffff, 0, 0, 0};
+      RowIn r = {0x7fffffff, 0, 0, 0};
+      float z = kInf, sl = 0.f;
       if (m < M) {
-        const int qi = m / G, qh = h * G + m % G;
+        const int qi = m / G, qh = h * G + m - qi * G;
         const Row w = load_row(a, q, s, qi);
         const float lse = a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh];
-        r.lse2 = lse == -kInf ? kInf : lse * kLog2e;  // a row that saw nothing gave nothing
-        r.slope = a.d_slope ? a.d_slope[qh] * kLog2e / sc.post : 0.f;
+        z = lse == -kInf ? kInf : lse * kLog2e;  // a row that saw nothing gave nothing
+        if (a.d_slope) sl = a.d_slope[qh] * kLog2e / sc.post;
         r.start = w.start, r.end = w.end, r.line = qi;
         r.pos = tree && a.d_slope ? q.base + depths[qi] : w.pos;
       }
-      in[tid] = r;
+      in[tid] = r, lse2[tid] = z, slopes[tid] = sl;
     }
     __syncthreads();
-    const int rows = min(kBlock, M - mb);
-    // what all rows of the block see, and what any sees
-    const int e0 = lane < rows ? lane : 0, e1 = lane + 64 < rows ? lane + 64 : 0;
-    const int all_from = wave_max(max(in[e0].start, in[e1].start)), all_to = wave_min(min(in[e0].end, in[e1].end));
-    const int any_from = wave_min(min(in[e0].start, in[e1].start)), any_to = tree ? q.len : wave_max(max(in[e0].end, in[e1].end));
-    if (!((t0 + kSlots > any_from && t0 < any_to) || t0 < pre) || t0 >= q.len) continue;
-    const bool whole = t0 + kSlots <= pre || (t0 >= all_from && t0 + kSlots <= all_to);
-    for (int m0 = 0; m0 < rows; m0 += 16) {
-      const int m = min(mb + m0 + col, M - 1), qi = m / G, qh = h * G + m % G;
-      const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + quad * 8;
-      V8 qf[KC];
+    all_from = any_from = 0;
+    if (a.d_row_start) {
+      const int e0 = lane < rows ? lane : 0, e1 = lane + 64 < rows ? lane + 64 : 0;
+      all_from = wave_max(max(in[e0].start, in[e1].start)), any_from = wave_min(min(in[e0].start, in[e1].start));
+    }
+    all_to = uni(in[0].end), any_to = tree ? q.len : uni(in[rows - 1].end);
+  };
+  if (M > 0 && M <= kBlock) stage(0);
+
+  for (int turn = 0; turn < n_turns; turn++) {
+    const int t0 = w0 + turn * kTurn + wave * kSlots;
+    V8 kf[kRuns][KC];
 #pragma unroll
-      for (int k = 0; k < KC; k++) {
-        qf[k] = *(const V8*)(p + 32 * k);
-        if (sc.negate) qf[k] = negated(qf[k]);
-      }
+    for (int u = 0; u < kRuns; u++)
 #pragma unroll
-      for (int u = 0; u < NS; u++) {
-        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < KC; k++) kf[u][k] = next[u][k];
+    if (turn + 1 < n_turns) load(turn + 1);
+    float acc[kRuns] = {};
+    for (int mb = 0; mb < M; mb += kBlock) {
+      if (M > kBlock) stage(mb);
+      if (!((t0 + kSlots > any_from && t0 < any_to) || t0 < pre) || t0 >= q.len) continue;
+      const bool whole = t0 + kSlots <= pre || (t0 >= all_from && t0 + kSlots <= all_to);
+      for (int m0 = 0; m0 < rows; m0 += 16) {
+        const int rm = m0 + quad * 4;  // rows of this lane's four elements of a product
+        V8 qf[KC];
 #pragma unroll
-        for (int k = 0; k < KC; k++) x = mma16(qf[k], kf[u][k], x);
-        const int j = t0 + 16 * u + col;
+        for (int k = 0; k < KC; k++) qf[k] = *(const V8*)(rows_q + tile_at<D>(m0 + col, 4 * k + quad));
+        const f32x4 z = *(const f32x4*)(lse2 + rm);  // rows behind the last one have a sum of infinity
+        f32x4 x[kRuns];
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const RowIn& r = in[m0 + quad * 4 + e];  // rows behind the last one have a sum of infinity
-          float y = x[e];
-          if (a.softcap > 0.f) y = capped(y, sc);
-          if (a.d_slope) {
-            const int at = drafts && j >= q.base ? q.base + depths[min(j - q.base, RKC_MAX_TREE_ROWS - 1)] : j;
-            y -= r.slope * fabsf((float)(r.pos - at));
-          }
-          y = ex2(y * sc.post - r.lse2);
-          if (!whole) {
-            bool see = (j >= r.start && j < r.end) || j < pre;
-            if (drafts && j >= q.base) {
-              const int d = min(j - q.base, RKC_MAX_TREE_ROWS - 1);
-              see |= lines[r.line][d >> 6] >> (d & 63) & 1;
-            }
-            y = see && r.lse2 != kInf ? y : 0.f;
-          }
-          acc[u] += y;
+        for (int u = 0; u < kRuns; u++) {
+          x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < KC; k++) x[u] = mma16(qf[k], kf[u][k], x[u]);
         }
+        if (a.softcap > 0.f) {
+#pragma unroll
+          for (int u = 0; u < kRuns; u++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[u][e] = capped(x[u][e], sc);
+        }
+        if (a.d_slope) {
+          const f32x4 sl = *(const f32x4*)(slopes + rm);
+#pragma unroll
+          for (int u = 0; u < kRuns; u++) {
+            int j = t0 + 16 * u + col;
+            if (drafts && j >= q.base) j = q.base + depths[min(j - q.base, RKC_MAX_TREE_ROWS - 1)];
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[u][e] = __builtin_fmaf(-sl[e], fabsf((float)(in[rm + e].pos - j)), x[u][e]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kRuns; u++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) x[u][e] = ex2(__builtin_fmaf(x[u][e], sc.post, -z[e]));
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const RowIn r = in[rm + e];
+#pragma unroll
+            for (int u = 0; u < kRuns; u++) {
+              const int j = t0 + 16 * u + col;
+              bool see = (j >= r.start && j < r.end) || j < pre;
+              if (drafts && j >= q.base) {
+                const int d = min(j - q.base, RKC_MAX_TREE_ROWS - 1);
+                see |= lines[r.line][d >> 6] >> (d & 63) & 1;
+              }
+              x[u][e] = see && z[e] != kInf ? x[u][e] : 0.f;
+            }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kRuns; u++) acc[u] += (x[u][0] + x[u][1]) + (x[u][2] + x[u][3]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kRuns; u++) {
+      const float got = sum32(sum16(acc[u]));
+      const int j = t0 + 16 * u + col;
+      if (quad == 0 && j < q.len) {
+        const int64_t at = s * a.weight_seq_stride + h * a.weight_head_stride + j;
+        a.d_weight[at] = (a.d_weight_in ? a.decay * a.d_weight_in[at] : 0.f) + got;
       }
     }
   }
-#pragma unroll
-  for (int u = 0; u < NS; u++) {
-    const float got = sum32(sum16(acc[u]));
-    const int j = t0 + 16 * u + col;
-    if (quad == 0 && j < q.len) {
-      const int64_t at = s * a.weight_seq_stride + h * a.weight_head_stride + j;
-      a.d_weight[at] = (a.d_weight_in ? a.decay * a.d_weight_in[at] : 0.f) + got;
-    }
-  }
+  if (bad) flag(c, s, RKC_CS_BLOCK);
 }
 
 template <typename T>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, hipStream_t s) {
-  const int slots = c->head_dim == 256 ? 128 : 256, chunks = (a->max_len + slots - 1) / slots;
+  // A workgroup keeps its queries for as many turns as leave three workgroups a CU, at most for one turn per 8 packed
+  // rows: few rows are staged quickly, and short turns even out sequences of unlike length.
+  const int64_t all = (int64_t)c->n_seqs * c->kv_heads * ((a->max_len + kTurn - 1) / kTurn);
+  const int64_t most = (int64_t)a->max_rows * (a->q_heads / c->kv_heads) / 8;
+  int64_t turns = all / (3 * 256);
+  turns = turns > most ? most : turns;
+  turns = turns > 16 ? 16 : turns < 2 ? 2 : turns;
+  const int chunks = (int)((a->max_len + turns * kTurn - 1) / (turns * kTurn));
   if ((int64_t)c->n_seqs * c->kv_heads * chunks > 0x7fffffff) return RKC_E_UNSUPPORTED;
   const dim3 grid(c->n_seqs * c->kv_heads * chunks), block(kThreads);
-  if (c->head_dim == 64) weigh<T, 64><<<grid, block, 0, s>>>(*c, *a, chunks);
-  else if (c->head_dim == 128) weigh<T, 128><<<grid, block, 0, s>>>(*c, *a, chunks);
-  else weigh<T, 256><<<grid, block, 0, s>>>(*c, *a, chunks);
+  if (c->head_dim == 64) weigh<T, 64><<<grid, block, 0, s>>>(*c, *a, chunks, (int)turns);
+  else if (c->head_dim == 128) weigh<T, 128><<<grid, block, 0, s>>>(*c, *a, chunks, (int)turns);
+  else weigh<T, 256><<<grid, block, 0, s>>>(*c, *a, chunks, (int)turns);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
