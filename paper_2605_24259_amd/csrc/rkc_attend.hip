@@ -3,43 +3,47 @@
 
 namespace {
 
-// Joins the chunks of a row: one wave per packed row, D / 64 elements a lane.
+// Joins the chunks of a packed row: a workgroup for each, D / 4 lanes for a chunk, as many chunks at a time as that
+// leaves room for.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
-  constexpr int E = D / 64;
-  const int H = c.kv_heads, G = a.q_heads / H, per = pl.tiles * pl.rows;
-  const int64_t id = (int64_t)blockIdx.x * 4 + uni(threadIdx.x >> 6);
-  const int64_t unit = id / per;
-  const int m = (int)(id % per), s = (int)(unit / H), h = (int)(unit % H), lane = threadIdx.x & 63;
-  if (s >= c.n_seqs) return;
+  constexpr int L = D / 4, N = 256 / L;
+  __shared__ __attribute__((aligned(16))) float part_o[N][D];
+  __shared__ float part_l[N];
+  const int H = c.kv_heads, G = a.q_heads / H, per = a.max_rows * G;
+  const int m = blockIdx.x % per, unit = blockIdx.x / per, s = unit / H, h = unit % H;
+  const int lane = threadIdx.x & 63, group = threadIdx.x / L, d = threadIdx.x % L * 4;
   const Seq q = load_seq(c, a, s);
   if (!q.ok || m >= q.n * G) return;
   const int qt = m / pl.rows, last = (min(q.n * G, (qt + 1) * pl.rows) - 1) / G;
   const int n = max(1, (rows_end(a, q, s, last) + pl.chunk - 1) / pl.chunk);
-  const int64_t at = (unit * pl.tiles + qt) * pl.splits * pl.rows + m % pl.rows;
+  const int64_t at = ((int64_t)unit * pl.tiles + qt) * pl.splits * pl.rows + m % pl.rows;
   const float* st = (const float*)((const char*)a.d_scratch + pl.stat_at) + at * 2;
-  const float* part = (const float*)((const char*)a.d_scratch + pl.part_at) + at * D + lane * E;
+  const float* part = (const float*)((const char*)a.d_scratch + pl.part_at) + at * D + d;
   float top = -kInf;
   for (int k = lane; k < n; k += 64) top = fmaxf(top, st[(int64_t)k * pl.rows * 2]);
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float sum = 0.f, o[E] = {};
+  for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+  float sum = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int k = 0; k < n; k++) {
+  for (int k = group; k < n; k += N) {
     const float m_k = st[(int64_t)k * pl.rows * 2], l_k = st[(int64_t)k * pl.rows * 2 + 1];
-    const float by = m_k == -kInf ? 0.f : ex2(m_k - top);
-    sum += l_k * by;
-#pragma unroll
-    for (int e = 0; e < E; e++) {
-      const float x = part[(int64_t)k * pl.rows * D + e];
-      o[e] += m_k == -kInf ? 0.f : x * by;
+    const f32x4 x = *(const f32x4*)(part + (int64_t)k * pl.rows * D);
+    if (m_k != -kInf) {
+      const float by = ex2(m_k - top);
+      sum += l_k * by, o += x * by;
     }
   }
+  *(f32x4*)&part_o[group][d] = o;
+  if (d == 0) part_l[group] = sum;
+  __syncthreads();
+  if (group) return;
+  for (int k = 1; k < N && k < n; k++) o += *(const f32x4*)&part_o[k][d], sum += part_l[k];
   const float by = sum == 0.f ? 0.f : 1.f / sum;
   const int64_t row = q.row0 + m / G, qh = h * G + m % G;
-  T* to = (T*)a.d_out + row * a.out_row_stride + qh * a.out_head_stride + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; e++) to[e] = (T)(o[e] * by);
-  if (lane == 0) a.d_lse[row * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  *(T4*)((T*)a.d_out + row * a.out_row_stride + qh * a.out_head_stride + d) = __builtin_convertvector(o * by, T4);
+  if (d == 0) a.d_lse[row * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
 }
 
 // The account from kept scores: one slot of four a thread.
@@ -47,7 +51,7 @@ __global__ __launch_bounds__(256) void attend_account(const rkc_cache c, const r
   const int H = c.kv_heads, G = a.q_heads / H, part = blockIdx.x % parts, unit = blockIdx.x / parts, s = unit / H, h = unit % H;
   const Seq q = load_seq(c, a, s);
   if (!q.ok || part * 1024 >= q.len) return;
-  const int M = q.n * G;
+  const int M = q.n * G, per = 32 * a.max_rows * G;
   const float* sc = (const float*)((const char*)a.d_scratch + pl.score_at) + (int64_t)unit * (a.max_rows * G) * pl.wide;
   const int64_t at = s * a.weight_seq_stride + h * a.weight_head_stride;
   float got[4] = {}, in[4] = {};
@@ -62,7 +66,7 @@ __global__ __launch_bounds__(256) void attend_account(const rkc_cache c, const r
 #pragma unroll
     for (int k = 0; k < 4; k++) {
       const int j = part * 1024 + k * 256 + threadIdx.x;
-      const float x = j < q.len ? sc[(int64_t)m * pl.wide + j] : -kInf;
+      const float x = j < q.len ? sc[(int64_t)(j >> 5) * per + m * 32 + (j & 31)] : -kInf;
       got[k] += x == -kInf ? 0.f : ex2(x - z);
     }
   }
@@ -75,8 +79,7 @@ __global__ __launch_bounds__(256) void attend_account(const rkc_cache c, const r
 
 template <typename T>
 rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  const int64_t waves = (int64_t)c->n_seqs * c->kv_heads * p->tiles * p->rows;
-  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+  const dim3 grid((unsigned)((int64_t)c->n_seqs * c->kv_heads * a->max_rows * (a->q_heads / c->kv_heads))), block(256);
   if (c->head_dim == 64) attend_join<T, 64><<<grid, block, 0, s>>>(*c, *a, *p);
   else if (c->head_dim == 128) attend_join<T, 128><<<grid, block, 0, s>>>(*c, *a, *p);
   else attend_join<T, 256><<<grid, block, 0, s>>>(*c, *a, *p);
@@ -144,7 +147,7 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
-  const int64_t want = p.few ? 6 * 256 : 2 * 256, grain = p.few ? 128 : 256;
+  const int64_t want = p.few ? 12 * 256 : c->head_dim == 256 ? 256 : 2 * 256, grain = p.few || c->head_dim == 256 ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;  // workgroups along a sequence
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;
@@ -183,7 +186,7 @@ rkc_status rkc_attend(const rkc_cache* c, const rkc_attention* a, void* stream) 
   if (a->n_rows == 0 || a->max_rows == 0) return a->d_weight ? rkc_weigh(c, a, stream) : RKC_OK;
   hipStream_t s = (hipStream_t)stream;
   const rkc_plan p = rkc_attend_plan(c, a);
-  if ((int64_t)p.units * p.splits > 0x7fffffff || (int64_t)c->n_seqs * c->kv_heads * p.tiles > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  if ((int64_t)p.units * p.splits > 0x7fffffff || (int64_t)c->n_seqs * c->kv_heads * p.tiles * p.rows > 0x7fffffff) return RKC_E_UNSUPPORTED;
   if (p.bytes) {
     if (!a->d_scratch || a->scratch_bytes < p.bytes) return RKC_E_SCRATCH;
     if ((uintptr_t)a->d_scratch & 255) return RKC_E_ALIGN;

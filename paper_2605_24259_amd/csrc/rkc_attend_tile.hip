@@ -25,16 +25,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   __shared__ int depths[RKC_MAX_TREE_ROWS], lim[4][2];
 
   const int H = c.kv_heads, G = a.q_heads / H;
-  int b = blockIdx.x;
-  const int h = b % H;
-  b /= H;
-  const int split = b % pl.splits;
-  b /= pl.splits;
-  const int qt = pl.tiles - 1 - b % pl.tiles, s = b / pl.tiles;  // the rows that see most go first
+  // Heads first: with 8 of them each XCD has one, and its cache that head's keys and values for the row tiles of a
+  // sequence, which are neighbours; the rows that see most go first.  (All heads on each XCD: trees 397 us instead of
+  // 334, documents 57 instead of 49; sequences before row tiles: 455 and 62.)
+  const int h = blockIdx.x % H, split = blockIdx.x / H % pl.splits, b = blockIdx.x / (H * pl.splits);
+  const int qt = pl.tiles - 1 - b % pl.tiles, s = b / pl.tiles;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5, col = lane & 31;
   const Seq q = load_seq(c, a, s);
   if (!q.ok) {
-    if (split == 0 && h == 0 && b % pl.tiles == 0 && tid == 0) flag(c, s, RKC_CS_LENGTH);
+    if (split == 0 && h == 0 && qt == 0 && tid == 0) flag(c, s, RKC_CS_LENGTH);
     return;
   }
   const int M = q.n * G, m0 = qt * kRows;

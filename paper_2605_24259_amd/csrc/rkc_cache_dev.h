@@ -326,8 +326,8 @@ struct rkc_plan {
   int rows;    // packed rows of a tile
   int chunk, splits;
   size_t part_at, stat_at, bytes;  // scratch: partial outputs, their maxima and sums, in all
-  bool keep;        // scores are kept for the account: [unit][packed row][slot], in units of log2
-  int wide;         // slots of a row of them
+  bool keep;        // scores are kept for the account: [unit][32 slots][packed row][slot], in units of log2
+  int wide;         // slots of a unit
   size_t score_at;
 };
 rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a);
