@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
   auto look_up = [&](int i) {
     const int t0 = slot_of(i);
 #pragma unroll
-    for (int u = 0; u < 2; u++) page[u] = page_of(c, table, shift, run_of(t0, u), bad);
+    for (int u = 0; u < 2; u++) page[u] = page_of(table, shift, run_of(t0, u));
   };
   constexpr int RP = 512 / D;  // rows of a piece of V: 64 lanes of 16 bytes
   const uint32_t k_off = col * kp.slot + quad * 16, v_off = lane / (D / 8) * vp.slot + lane % (D / 8) * 16;
@@ -145,8 +145,9 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
 #pragma unroll
     for (int u = 0; u < 2; u++) {
       const int at = run_of(t0, u) & in_page;
-      const char* kb = fixed(run_at(kp, page[u], at));
-      const char* vb = run_at(vp, page[u], at);
+      const int block = block_of(c, page[u], bad);
+      const char* kb = fixed(run_at(kp, block, at));
+      const char* vb = run_at(vp, block, at);
 #pragma unroll
       for (int k = 0; k < KC; k++) kf[u][k] = *(const V8*)(kb + k_off + 64 * k);
 #pragma unroll

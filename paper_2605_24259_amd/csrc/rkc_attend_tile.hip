@@ -11,18 +11,17 @@
 
 namespace {
 
-constexpr int kRows = 128, kThreads = 256;
-static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
 
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+template <typename T, int D, int W>
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
-  constexpr int BK = D == 256 ? 32 : 64, kAhead = D == 256 ? 3 : 1, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
+  constexpr int kRows = 32 * W, kThreads = 64 * W;
+  constexpr int BK = D == 256 ? 32 : 64, kAhead = D == 256 || W == 8 ? 3 : 1, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
   constexpr int P = BK * CH / kThreads;  // 16-byte pieces of K, and of V, per thread
   constexpr int kTile = BK * D;
   __shared__ __attribute__((aligned(16))) T lds[(kAhead + 1) * 2 * kTile];  // K and V of each tile
   __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
-  __shared__ int depths[RKC_MAX_TREE_ROWS], lim[4][2];
+  __shared__ int depths[RKC_MAX_TREE_ROWS], lim[W][2];
 
   const int H = c.kv_heads, G = a.q_heads / H;
   // Heads first: with 8 of them each XCD has one, and its cache that head's keys and values for the row tiles of a
@@ -70,8 +69,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, 31));
   if (lane == 0) lim[wave][0] = any_from, lim[wave][1] = any_to;
   __syncthreads();
-  const int g_any_from = uni(min(min(lim[0][0], lim[1][0]), min(lim[2][0], lim[3][0])));
-  const int g_any_to = uni(max(max(lim[0][1], lim[1][1]), max(lim[2][1], lim[3][1])));
+  int g_any_from = lim[0][0], g_any_to = lim[0][1];
+#pragma unroll
+  for (int k = 1; k < W; k++) g_any_from = min(g_any_from, lim[k][0]), g_any_to = max(g_any_to, lim[k][1]);
+  g_any_from = uni(g_any_from), g_any_to = uni(g_any_to);
   const int end = min(c1, g_any_to);
 
   const Pool kp = k_pool(c, h), vp = v_pool(c, h);
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   auto look_up = [&](int i) {
     const int t0 = slot_of(i);
 #pragma unroll
-    for (int p = 0; p < P; p++) page[p] = page_of(c, table, shift, run_of(t0, p), bad);
+    for (int p = 0; p < P; p++) page[p] = page_of(table, shift, run_of(t0, p));
   };
   auto load = [&](int i, int buf) {
     const int t0 = slot_of(i);
@@ -116,157 +117,258 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
 #pragma unroll
     for (int p = 0; p < P; p++) {
       const int at = run_of(t0, p) & in_page, o = kThreads / CH >= 16 ? 0 : p & 1;
-      dma(fixed(run_at(kp, page[p], at)) + k_off[o], to + p * kThreads * 8);
-      dma(fixed(run_at(vp, page[p], at)) + v_off[o], to + kTile + p * kThreads * 8);
+      const int block = block_of(c, page[p], bad);
+      dma(fixed(run_at(kp, block, at)) + k_off[o], to + p * kThreads * 8);
+      dma(fixed(run_at(vp, block, at)) + v_off[o], to + kTile + p * kThreads * 8);
     }
   };
   const int vi = lane & 15, vr = 4 * half + (vi >> 2), vc = (lane >> 4 & 1) * 2 + ((vi & 3) >> 1), ve = (vi & 1) * 4;
   const int key_at = 2 * tile_at<D>(col, half), val_at = 2 * (kTile + tile_at<D>(vr, vc) + ve);
-  auto go_over = [&](auto with_care) {
-  constexpr bool careful = decltype(with_care)::value;
-  // kAhead tiles are on their way while one is worked on
-  look_up(0);
+  // whether any of the wave's rows sees anything of a tile, and whether all see all of it
+  auto sees = [&](int t0) { return rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre); };
+  // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
+  // a row) and by whole rows
+  auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k << 5) + 64 * D * u); };
+  auto vals = [&](int va, int u, int v, int d) {
+    return read_tr2<T>((const char*)lds + (va ^ d << 6) + 32 * D * (2 * u + v), (const char*)lds + (va ^ d << 6 ^ 32) + 32 * D * (2 * u + v) + 16 * D);
+  };
+  auto scores = [&](f32x16(&sc)[KT], int buf) {
+    const int ka = here(buf * 4 * kTile + key_at);
 #pragma unroll
-  for (int i = 0; i < kAhead; i++) {
-    if (i < n_tiles) load(i, i);
-    if (i + 1 < n_tiles) look_up(i + 1);
-  }
-  int buf = 0;
-  for (int i = 0; i < n_tiles; i++) {
-    const int t0 = slot_of(i);
-    if (i + kAhead <= n_tiles) dma_barrier<2 * P * (kAhead - 1)>();
-    else dma_barrier<0>();
-    if (i + kAhead < n_tiles) load(i + kAhead, buf ? buf - 1 : kAhead);
-    if (i + kAhead + 1 < n_tiles) look_up(i + kAhead + 1);
-    T* vt_ = lds + buf * 2 * kTile + kTile;
-    // byte offsets of this lane's first key and first values of the tile; the others differ by an exclusive or
-    // (chunks along a row) and by whole rows
-    const int ka = here(buf * 4 * kTile + key_at), va = here(buf * 4 * kTile + val_at);
-    auto keys = [&](int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k << 5) + 64 * D * u); };
-    auto vals = [&](int u, int v, int d) {
-      return read_tr2<T>((const char*)lds + (va ^ d << 6) + 32 * D * (2 * u + v), (const char*)lds + (va ^ d << 6 ^ 32) + 32 * D * (2 * u + v) + 16 * D);
-    };
-    bool hurt = false;
-    if (t0 + BK > end || careful) {  // what lies behind the last slot that a row sees must not enter a product
-      for (int k = tid; k < BK * CH; k += kThreads) {
-        const int j = t0 + k / CH;
-        V8* v = (V8*)(vt_ + 8 * k);
-        if (j >= end || (j < g_any_from && j >= pre)) *v = __builtin_bit_cast(V8, u32x4{0, 0, 0, 0});
-        else if constexpr (careful) hurt |= any_hurt<T>(__builtin_bit_cast(u32x4, *v));
-      }
-      if constexpr (careful) hurt = __syncthreads_or(hurt);
-      else __syncthreads();
+    for (int u = 0; u < KT; u++) {
+#pragma unroll
+      for (int k = 0; k < 16; k++) sc[u][k] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KC; k++) sc[u] = mma32(keys(ka, u, k), qf[k], sc[u]);
     }
-    // whether any of the wave's rows sees anything of the tile, and whether all see all of it
-    const bool sees = rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre);
+  };
+  // cap, distance, masks, and the maximum that the weights refer to
+  auto fold = [&](f32x16(&sc)[KT], uint32_t(&seen)[KT], int t0) {
     const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
-    f32x16 sc[KT];
-    uint32_t seen[KT];
-    if (sees) {
-#pragma unroll
-      for (int u = 0; u < KT; u++) {
-#pragma unroll
-        for (int k = 0; k < 16; k++) sc[u][k] = 0.f;
-#pragma unroll
-        for (int k = 0; k < KC; k++) sc[u] = mma32(keys(u, k), qf[k], sc[u]);
-      }
-      if (a.softcap > 0.f) {
-#pragma unroll
-        for (int u = 0; u < KT; u++)
-#pragma unroll
-          for (int k = 0; k < 16; k++) sc[u][k] = capped(sc[u][k], f);
-      }
-      if (a.d_slope) {
-        const int base_at = here(q.base - t0 - 4 * half);
-        const float far = (float)(here(row.pos - t0) - 4 * half);
-#pragma unroll
-        for (int u = 0; u < KT; u++)
-#pragma unroll
-          for (int k = 0; k < 16; k++) {
-            const int j = 32 * u + (k & 3) + 8 * (k >> 2);
-            float gap = far - (float)j;
-            if (drafts && t0 + BK > q.base) {
-              const int i = j - base_at, d = depths[max(0, min(i, RKC_MAX_TREE_ROWS - 1))];
-              gap = i >= 0 ? (float)(row.pos - q.base - d) : gap;
-            }
-            sc[u][k] = __builtin_fmaf(-slope, fabsf(gap), sc[u][k]);
-          }
-      }
-#pragma unroll
-      for (int u = 0; u < KT; u++) seen[u] = 0xffffffff;
-      if (!whole) {
-#pragma unroll
-        for (int u = 0; u < KT; u++) {
-          const int j0 = t0 + 32 * u;
-          seen[u] = seen_of(row, j0, drafts ? line_window(lines[qi], 4, j0 - q.base) : 0) >> 4 * half;
-#pragma unroll
-          for (int k = 0; k < 16; k++) sc[u][k] = masked(sc[u][k], seen[u], (k & 3) + 8 * (k >> 2));
-        }
-      }
-      float most = -kInf;
+    if (a.softcap > 0.f) {
 #pragma unroll
       for (int u = 0; u < KT; u++)
 #pragma unroll
-        for (int k = 0; k < 16; k++) most = fmaxf(most, sc[u][k]);
-      most = max32(most) * f.post;
-      // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
-      if (__any(most > top + 8.f)) {
-        const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
-        top = now, sum *= by;
+        for (int k = 0; k < 16; k++) sc[u][k] = capped(sc[u][k], f);
+    }
+    if (a.d_slope) {
+      const int base_at = here(q.base - t0 - 4 * half);
+      const float far = (float)(here(row.pos - t0) - 4 * half);
 #pragma unroll
-        for (int d = 0; d < DB; d++) o[d] *= by;
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+          const int j = 32 * u + (k & 3) + 8 * (k >> 2);
+          float gap = far - (float)j;
+          if (drafts && t0 + BK > q.base) {
+            const int i = j - base_at, d = depths[max(0, min(i, RKC_MAX_TREE_ROWS - 1))];
+            gap = i >= 0 ? (float)(row.pos - q.base - d) : gap;
+          }
+          sc[u][k] = __builtin_fmaf(-slope, fabsf(gap), sc[u][k]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < KT; u++) seen[u] = 0xffffffff;
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < KT; u++) {
+        const int j0 = t0 + 32 * u;
+        seen[u] = seen_of(row, j0, drafts ? line_window(lines[qi], 4, j0 - q.base) : 0) >> 4 * half;
+#pragma unroll
+        for (int k = 0; k < 16; k++) sc[u][k] = masked(sc[u][k], seen[u], (k & 3) + 8 * (k >> 2));
       }
     }
-    if constexpr (careful) if (hurt) {  // the same for the whole workgroup
-      if (sees) {
+    float most = -kInf;
 #pragma unroll
-        for (int d = 0; d < DB; d++) {
-          f32x16 n;
+    for (int u = 0; u < KT; u++)
 #pragma unroll
-          for (int k = 0; k < 16; k++) n[k] = 0.f;
+      for (int k = 0; k < 16; k++) most = fmaxf(most, sc[u][k]);
+    most = max32(most) * f.post;
+    // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+    if (__any(most > top + 8.f)) {
+      const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
+      top = now, sum *= by;
+#pragma unroll
+      for (int d = 0; d < DB; d++) o[d] *= by;
+    }
+  };
+  // The products' operands have the cache's type: the weights are rounded to it here, their sum is not.
+  auto weights = [&](const f32x16& sc, int v) {
+    const float mx = top == -kInf ? 0.f : top;
+    f32x8 p;
+#pragma unroll
+    for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[8 * v + k], f.post, -mx));
+    sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    return __builtin_convertvector(p, V8);
+  };
+
+  // One tile after the other: all waves take the same step of it.
+  auto go_over = [&](auto with_care) {
+    constexpr bool careful = decltype(with_care)::value;
+    // kAhead tiles are on their way while one is worked on
+    look_up(0);
+#pragma unroll
+    for (int i = 0; i < kAhead; i++) {
+      if (i < n_tiles) load(i, i);
+      if (i + 1 < n_tiles) look_up(i + 1);
+    }
+    int buf = 0;
+    for (int i = 0; i < n_tiles; i++) {
+      const int t0 = slot_of(i);
+      if (i + kAhead <= n_tiles) dma_barrier<2 * P * (kAhead - 1)>();
+      else dma_barrier<0>();
+      if (i + kAhead < n_tiles) load(i + kAhead, buf ? buf - 1 : kAhead);
+      if (i + kAhead + 1 < n_tiles) look_up(i + kAhead + 1);
+      T* tile_v = lds + buf * 2 * kTile + kTile;
+      const int va = here(buf * 4 * kTile + val_at);
+      bool hurt = false;
+      if (t0 + BK > end || careful) {  // what lies behind the last slot that a row sees must not enter a product
+        for (int k = tid; k < BK * CH; k += kThreads) {
+          const int j = t0 + k / CH;
+          V8* v = (V8*)(tile_v + 8 * k);
+          if (j >= end || (j < g_any_from && j >= pre)) *v = __builtin_bit_cast(V8, u32x4{0, 0, 0, 0});
+          else if constexpr (careful) hurt |= any_hurt<T>(__builtin_bit_cast(u32x4, *v));
+        }
+        if constexpr (careful) hurt = __syncthreads_or(hurt);
+        else __syncthreads();
+      }
+      f32x16 sc[KT];
+      uint32_t seen[KT];
+      if (sees(t0)) {
+        scores(sc, buf);
+        fold(sc, seen, t0);
+      }
+      if constexpr (careful) if (hurt) {  // the same for the whole workgroup
+        if (sees(t0)) {
+#pragma unroll
+          for (int d = 0; d < DB; d++) {
+            f32x16 n;
+#pragma unroll
+            for (int k = 0; k < 16; k++) n[k] = 0.f;
 #pragma unroll 1
-          for (int x = 0; x < 2 * KT; x++) {
-              const int u = x >> 1, v = x & 1;
-              const uint32_t bits = KT > 1 && u ? seen[KT - 1] : seen[0];
-              V8 by, vt = vals(u, v, d);
+            for (int x = 0; x < 2 * KT; x++) {
+              const uint32_t bits = (KT > 1 && x >> 1 ? seen[KT - 1] : seen[0]) >> 16 * (x & 1);
+              V8 by, vt = vals(va, x >> 1, x & 1, d);
 #pragma unroll
-              for (int k = 0; k < 8; k++) by[k] = (T)(bits >> (16 * v + (k & 3) + 8 * (k >> 2)) & 1 ? 1.f : 0.f);
+              for (int k = 0; k < 8; k++) by[k] = (T)(bits >> ((k & 3) + 8 * (k >> 2)) & 1 ? 1.f : 0.f);
               n = mma32(strip<T>(vt), by, n);
             }
 #pragma unroll
-          for (int k = 0; k < 16; k++) o[d][k] += hurt_by(n[k]);
+            for (int k = 0; k < 16; k++) o[d][k] += hurt_by(n[k]);
+          }
         }
-      }
-      __syncthreads();
-      for (int k = tid; k < kTile / 8; k += kThreads) {
-        V8 v = *(const V8*)(vt_ + 8 * k);
-        strip<T>(v);
-        *(V8*)(vt_ + 8 * k) = v;
-      }
-      __syncthreads();
-    }
-    if (sees) {
-      const float mx = top == -kInf ? 0.f : top;
-#pragma unroll
-      for (int u = 0; u < KT; u++) {
-#pragma unroll
-        for (int v = 0; v < 2; v++) {
-          f32x8 p;
-#pragma unroll
-          for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[u][8 * v + k], f.post, -mx));
-          sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-          // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
-          const V8 pb = __builtin_convertvector(p, V8);
-#pragma unroll
-          for (int d = 0; d < DB; d++)
-            o[d] = mma32(vals(u, v, d), pb, o[d]);
+        __syncthreads();
+        for (int k = tid; k < kTile / 8; k += kThreads) {
+          V8 v = *(const V8*)(tile_v + 8 * k);
+          strip<T>(v);
+          *(V8*)(tile_v + 8 * k) = v;
         }
+        __syncthreads();
       }
+      if (sees(t0)) {
+#pragma unroll
+        for (int u = 0; u < KT; u++)
+#pragma unroll
+          for (int v = 0; v < 2; v++) {
+            const V8 pb = weights(sc[u], v);
+#pragma unroll
+            for (int d = 0; d < DB; d++) o[d] = mma32(vals(va, u, v, d), pb, o[d]);
+          }
+      }
+      buf = buf == kAhead ? 0 : buf + 1;
     }
-    buf = buf == kAhead ? 0 : buf + 1;
-  }
   };
-  go_over(std::false_type());
+
+  // Two waves to a SIMD in turns: while one multiplies (the next tile's scores and this one's outputs), the other
+  // works on its scores.  Steps are numbered over the workgroup; the second four waves are one step behind.  Step
+  // 2 i needs tile i and leaves the place of tile i - 2 to tile i + 2.
+  auto in_turns = [&] {
+    static_assert(W != 8 || kAhead == 3, "four places");
+    const bool behind = wave >= 4;
+    look_up(0);
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      if (i < n_tiles) load(i, i);
+      if (i + 1 < n_tiles) look_up(i + 1);
+    }
+    auto even = [&](int i) {
+      if (i + 1 < n_tiles) dma_barrier<2 * P>();
+      else dma_barrier<0>();
+      if (i + 2 < n_tiles) load(i + 2, i + 2 & 3);
+      if (i + 3 < n_tiles) look_up(i + 3);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto odd = [&] {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    f32x16 sc[KT];
+    V8 pb[2 * KT];
+    bool had = false;  // weights of the tile before are there
+    auto multiply = [&](int i) {
+      const bool has = i < n_tiles && sees(slot_of(i));
+      if (has) scores(sc, i & 3);
+      if (had) {
+        const int va = here((i - 1 & 3) * 4 * kTile + val_at);
+#pragma unroll
+        for (int u = 0; u < KT; u++)
+#pragma unroll
+          for (int v = 0; v < 2; v++)
+#pragma unroll
+            for (int d = 0; d < DB; d++) o[d] = mma32(vals(va, u, v, d), pb[2 * u + v], o[d]);
+      }
+      had = has;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto weigh = [&](int i) {
+      const int t0 = slot_of(i);
+      if (had) {
+        uint32_t seen[KT];
+        fold(sc, seen, t0);
+#pragma unroll
+        for (int u = 0; u < KT; u++)
+#pragma unroll
+          for (int v = 0; v < 2; v++) pb[2 * u + v] = weights(sc[u], v);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // What lies behind the last slot that a row sees must not enter a product: zeroed by the second waves at step 2 i,
+    // the first ones multiply with it from step 2 i + 2 on.
+    auto blank = [&](int i) {
+      const int t0 = slot_of(i);
+      if (t0 + BK <= end) return;
+      T* tile_v = lds + (i & 3) * 2 * kTile + kTile;
+      for (int k = tid - kThreads / 2; k < BK * CH; k += kThreads / 2) {
+        const int j = t0 + k / CH;
+        if (j >= end || (j < g_any_from && j >= pre)) *(u32x4*)(tile_v + 8 * k) = u32x4{0, 0, 0, 0};
+      }
+    };
+    if (!behind) {
+      for (int i = 0; i <= n_tiles; i++) {
+        even(i);
+        multiply(i);
+        odd();
+        if (i < n_tiles) weigh(i);
+      }
+    } else {
+      even(0);
+      if (n_tiles) blank(0);
+      for (int i = 0; i <= n_tiles; i++) {
+        odd();
+        multiply(i);
+        if (i < n_tiles) {
+          even(i + 1);
+          if (i + 1 < n_tiles) blank(i + 1);
+          weigh(i);
+        }
+      }
+    }
+    __syncthreads();
+  };
+  if constexpr (W == 8) in_turns();
+  else go_over(std::false_type());
   // A value that is not finite reaches rows that do not see its slot, through a weight of zero.  That shows in the
   // outputs, and then all is done once more with care.
   float odd = 0.f;  // stays 0 unless an output is not finite
@@ -310,13 +412,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tile(const 
   }
 }
 
+template <typename T, int D, int W>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  attend_tile<T, D, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
 template <typename T>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  const dim3 grid(p->units * p->splits), block(kThreads);
-  if (c->head_dim == 64) attend_tile<T, 64><<<grid, block, 0, s>>>(*c, *a, *p);
-  else if (c->head_dim == 128) attend_tile<T, 128><<<grid, block, 0, s>>>(*c, *a, *p);
-  else attend_tile<T, 256><<<grid, block, 0, s>>>(*c, *a, *p);
-  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+  if (c->head_dim == 256) return go<T, 256, 4>(c, a, p, s);
+  if (c->head_dim == 128) return p->rows == 256 ? go<T, 128, 8>(c, a, p, s) : go<T, 128, 4>(c, a, p, s);
+  return p->rows == 256 ? go<T, 64, 8>(c, a, p, s) : go<T, 64, 4>(c, a, p, s);
 }
 
 }  // namespace

@@ -196,7 +196,7 @@ __device__ __forceinline__ Row load_row(const rkc_attention& a, const Seq& q, in
   return r;
 }
 
-// Lines of a tree of at most RKC_MAX_TREE_ROWS rows, by a workgroup of as many threads: every row joins the line
+// Lines of a tree of at most RKC_MAX_TREE_ROWS rows, by a workgroup of as many threads or more: every row joins the line
 // of the row that its own line ends at, until all end at a root.  On return depths holds the rows' depths.
 __device__ __forceinline__ void tree_lines(const rkc_cache& c, const rkc_attention& a, const Seq& q, int s, bool tell, uint64_t (*lines)[4], int* depths) {
   const int tid = threadIdx.x;
@@ -212,9 +212,11 @@ __device__ __forceinline__ void tree_lines(const rkc_cache& c, const rkc_attenti
     for (int k = 0; k < 4; k++) w[k] = tid >> 6 == k ? 1ull << (tid & 63) : 0;
   }
   for (int reach = 1;; reach *= 2) {
+    if (tid < RKC_MAX_TREE_ROWS) {
 #pragma unroll
-    for (int k = 0; k < 4; k++) lines[tid][k] = w[k];
-    depths[tid] = up;
+      for (int k = 0; k < 4; k++) lines[tid][k] = w[k];
+      depths[tid] = up;
+    }
     __syncthreads();
     if (reach >= q.n) break;
     if (up >= 0) {
@@ -224,7 +226,7 @@ __device__ __forceinline__ void tree_lines(const rkc_cache& c, const rkc_attenti
     }
     __syncthreads();
   }
-  depths[tid] = __popcll(w[0]) + __popcll(w[1]) + __popcll(w[2]) + __popcll(w[3]) - 1;
+  if (tid < RKC_MAX_TREE_ROWS) depths[tid] = __popcll(w[0]) + __popcll(w[1]) + __popcll(w[2]) + __popcll(w[3]) - 1;
   __syncthreads();
 }
 
@@ -274,10 +276,10 @@ __device__ __forceinline__ const char* run_at(const Pool& p, int page, int in_pa
   return p.base + (uint64_t)(uint32_t)page * p.block + (uint32_t)in_page * p.slot;
 }
 
-// Block of the page that slot t, the same for the wave, lies in; block 0 for an id outside the pool, which `bad`
-// remembers.
-__device__ __forceinline__ int page_of(const rkc_cache& c, const int32_t* table, int shift, int t, bool& bad) {
-  const int id = word(table, t >> shift);
+// Block of the page that slot t, the same for the wave, lies in, as the table has it: to be looked up ahead of its use.
+__device__ __forceinline__ int page_of(const int32_t* table, int shift, int t) { return word(table, t >> shift); }
+// The block itself; 0 for an id outside the pool, which `bad` remembers.
+__device__ __forceinline__ int block_of(const rkc_cache& c, int id, bool& bad) {
   const bool out = (uint32_t)id >= (uint32_t)c.n_blocks;
   bad |= out;
   return out ? 0 : id;

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rk
 #pragma unroll
     for (int u = 0; u < kRuns; u++) {
       const int at = min(w0 + turn * kTurn + wave * kSlots + 16 * u, (q.len - 1) & ~15);
-      const char* kb = run_at(kp, page_of(c, table, shift, at, bad), at & in_page);
+      const char* kb = run_at(kp, block_of(c, page_of(table, shift, at), bad), at & in_page);
 #pragma unroll
       for (int k = 0; k < KC; k++) next[u][k] = *(const V8*)(kb + k_off + 64 * k);
     }
