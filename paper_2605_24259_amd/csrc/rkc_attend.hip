@@ -155,6 +155,9 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   p.chunk = (int)chunk;
   p.splits = (int)((a->max_len + chunk - 1) / chunk);
   if (p.splits < 1) p.splits = 1;
+  // More workgroups than the card holds at once: the longest go first, so that none starts late.  (Each finds its
+  // sequence by comparing lengths, less than 1 us; 48 trees of 700 to 8,192 slots: 310 us instead of 365.)
+  p.sorted = !p.few && c->n_seqs > 1 && c->n_seqs <= 64 && units * p.splits > want;
   if (p.splits > 1) {
     const size_t rows = (size_t)units * p.splits * p.rows;
     p.part_at = 0;

@@ -28,8 +28,10 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rk
   // sequence, which are neighbours; the rows that see most go first.  (All heads on each XCD: trees 397 us instead of
   // 334, documents 57 instead of 49; sequences before row tiles: 455 and 62.)
   const int h = blockIdx.x % H, split = blockIdx.x / H % pl.splits, b = blockIdx.x / (H * pl.splits);
-  const int qt = pl.tiles - 1 - b % pl.tiles, s = b / pl.tiles;
+  const int qt = pl.tiles - 1 - b % pl.tiles, s = pl.sorted ? seq_of_rank(c, a, b / pl.tiles) : b / pl.tiles;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5, col = lane & 31;
+  // which 32 rows are the wave's: neighbours work in turns on one SIMD, also where a tile is not full
+  const int part = W == 8 ? (wave & 3) * 2 + (wave >> 2) : wave;
   const Seq q = load_seq(c, a, s);
   if (!q.ok) {
     if (split == 0 && h == 0 && qt == 0 && tid == 0) flag(c, s, RKC_CS_LENGTH);
@@ -43,8 +45,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rk
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
-  const int m = min(m0 + 32 * wave + col, M - 1), qi = m / G, qh = h * G + m % G;
-  const bool mine = m0 + 32 * wave + col < M, rows = m0 + 32 * wave < M;
+  const int m = min(m0 + 32 * part + col, M - 1), qi = m / G, qh = h * G + m % G;
+  const bool mine = m0 + 32 * part + col < M, rows = m0 + 32 * part < M;
   const Scale f = load_scale(a);
   Row row = load_row(a, q, s, qi);
   const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
@@ -135,12 +137,13 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rk
   auto scores = [&](f32x16(&sc)[KT], int buf) {
     const int ka = here(buf * 4 * kTile + key_at);
 #pragma unroll
-    for (int u = 0; u < KT; u++) {
+    for (int u = 0; u < KT; u++)
 #pragma unroll
       for (int k = 0; k < 16; k++) sc[u][k] = 0.f;
 #pragma unroll
-      for (int k = 0; k < KC; k++) sc[u] = mma32(keys(ka, u, k), qf[k], sc[u]);
-    }
+    for (int k = 0; k < KC; k++)
+#pragma unroll
+      for (int u = 0; u < KT; u++) sc[u] = mma32(keys(ka, u, k), qf[k], sc[u]);
   };
   // cap, distance, masks, and the maximum that the weights refer to
   auto fold = [&](f32x16(&sc)[KT], uint32_t(&seen)[KT], int t0) {
@@ -307,17 +310,33 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rk
     f32x16 sc[KT];
     V8 pb[2 * KT];
     bool had = false;  // weights of the tile before are there
+    auto outputs = [&](int i) {
+      const int va = here((i & 3) * 4 * kTile + val_at);
+#pragma unroll
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int v = 0; v < 2; v++)
+#pragma unroll
+          for (int d = 0; d < DB; d++) o[d] = mma32(vals(va, u, v, d), pb[2 * u + v], o[d]);
+    };
     auto multiply = [&](int i) {
       const bool has = i < n_tiles && sees(slot_of(i));
-      if (has) scores(sc, i & 3);
-      if (had) {
-        const int va = here((i - 1 & 3) * 4 * kTile + val_at);
+      if (has && had) {
+        scores(sc, i & 3);
+        outputs(i - 1);
+        // operands a few products ahead of their use
+        if constexpr (D == 128) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
-        for (int u = 0; u < KT; u++)
-#pragma unroll
-          for (int v = 0; v < 2; v++)
-#pragma unroll
-            for (int d = 0; d < DB; d++) o[d] = mma32(vals(va, u, v, d), pb[2 * u + v], o[d]);
+          for (int k = 0; k < KT * (KC + 2 * DB); k++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          }
+        }
+      } else if (has) {
+        scores(sc, i & 3);
+      } else if (had) {
+        outputs(i - 1);
       }
       had = has;
       __builtin_amdgcn_sched_barrier(0);
@@ -401,7 +420,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rk
       }
     if (half == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
   } else {
-    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + 32 * wave + col;
+    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + 32 * part + col;
     float* to = (float*)((char*)a.d_scratch + pl.part_at) + at * D + 4 * half;
 #pragma unroll
     for (int d = 0; d < DB; d++)

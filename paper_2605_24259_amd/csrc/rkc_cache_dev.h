@@ -196,6 +196,17 @@ __device__ __forceinline__ Row load_row(const rkc_attention& a, const Seq& q, in
   return r;
 }
 
+// The sequence of rank r by length, the longest first, of at most 64: found by each wave for itself.
+__device__ __forceinline__ int seq_of_rank(const rkc_cache& c, const rkc_attention& a, int r) {
+  const int lane = threadIdx.x & 63, len = lane < c.n_seqs ? a.d_length[lane] : (int)0x80000000;
+  int rank = 0;
+  for (int k = 0; k < c.n_seqs; k++) {
+    const int other = __builtin_amdgcn_readlane(len, k);
+    rank += other > len || (other == len && k < lane);
+  }
+  return uni(__builtin_ctzll(__ballot(lane < c.n_seqs && rank == r)));
+}
+
 // Lines of a tree of at most RKC_MAX_TREE_ROWS rows, by a workgroup of as many threads or more: every row joins the line
 // of the row that its own line ends at, until all end at a root.  On return depths holds the rows' depths.
 __device__ __forceinline__ void tree_lines(const rkc_cache& c, const rkc_attention& a, const Seq& q, int s, bool tell, uint64_t (*lines)[4], int* depths) {
@@ -327,6 +338,7 @@ struct rkc_plan {
   int tiles;   // row tiles per sequence and head
   int rows;    // packed rows of a tile
   int chunk, splits;
+  bool sorted;  // long sequences first
   size_t part_at, stat_at, bytes;  // scratch: partial outputs, their maxima and sums, in all
   bool keep;        // scores are kept for the account: [unit][32 slots][packed row][slot], in units of log2
   int wide;         // slots of a unit
