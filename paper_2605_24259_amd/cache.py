@@ -13,8 +13,11 @@ Nothing is copied to the host and no call waits for the GPU.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
+
+from . import RkcError, _stream_ptr
 
 MAX_TREE_ROWS = 256
 HEAD_DIMS = (64, 128, 256)
@@ -64,6 +67,9 @@ def declare(lib):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ctypes.c_int
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _ptr(t):
     return t.data_ptr() if t is not None else None
 
@@ -93,6 +99,7 @@ class PagedCache:
             raise TypeError(f"k and v are bfloat16 or float16, alike: {k.dtype}, {v.dtype}")
         if k.stride(3) != 1 or v.stride(3) != 1:
             raise ValueError("the last dimension of k and v must be contiguous")
+        self._int32 = torch.int32
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         if not k.is_cuda or v.device != k.device:
             raise ValueError("k and v must be on one GPU")
@@ -105,15 +112,16 @@ class PagedCache:
         c.k_block_stride, c.k_slot_stride, c.k_head_stride = k.stride()[:3]
         c.v_block_stride, c.v_slot_stride, c.v_head_stride = v.stride()[:3]
         c.d_k, c.d_v, c.d_block_table, c.d_status = k.data_ptr(), v.data_ptr(), _ptr(self.block_table), _ptr(self.status)
-        self._c = c
+        self._c, self._c_ref = c, ctypes.byref(c)
+        self._torch, self._raw_stream = torch, torch._C._cuda_getCurrentRawStream
+        self._index = k.device.index
         self.n_seqs, self.kv_heads, self.head_dim = int(c.n_seqs), int(c.kv_heads), int(c.head_dim)
         self.max_len = int(c.max_pages) * int(c.page_tokens)
 
     def _ints(self, t, name, dim=1, n=None, optional=False):
-        import torch
         if t is None and optional:
             return None
-        if t.dtype != torch.int32 or t.device != self.device or t.dim() != dim or not t.is_contiguous():
+        if t.dtype != self._int32 or t.device != self.device or t.dim() != dim or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous int32 tensor of {dim} dimension(s) on {self.device} is wanted")
         if n is not None and t.shape[0] != n:
             raise ValueError(f"{name}: {n} values are wanted, got {t.shape[0]}")
@@ -127,7 +135,7 @@ class PagedCache:
         return t
 
     def _attention(self, q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent):
-        import torch
+        torch = self._torch
         if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype != self.dtype or q.device != self.device or q.stride(2) != 1:
             raise ValueError(f"q: [rows, heads, {self.head_dim}] of {self.dtype} on {self.device}, the last dimension "
                              "contiguous, is wanted")
@@ -153,7 +161,7 @@ class PagedCache:
         return a
 
     def _weights(self, a, weight, weight_out, decay):
-        import torch
+        torch = self._torch
         n = int(a.max_len)
         if weight is not None:
             self._account(weight, "weight", torch.float32, n)
@@ -169,17 +177,15 @@ class PagedCache:
         return weight_out
 
     def _call(self, name, args, stream):
-        from . import RkcError, _stream_ptr
-        st = getattr(self._lib, name)(ctypes.byref(self._c), ctypes.byref(args), _stream_ptr(stream))
+        # the current stream of the cache's device; looked up by number, a twentieth of the cost of a Stream object
+        at = self._raw_stream(self._index) if stream is None else _stream_ptr(stream)
+        st = getattr(self._lib, name)(self._c_ref, ctypes.byref(args), at)
         if st != 0:
             raise RkcError(st, name)
 
     def _on(self, stream):
         """Tensors made in a call belong to the stream that the call runs on."""
-        import contextlib
-
-        import torch
-        return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+        return self._torch.cuda.stream(stream) if stream is not None else _HERE
 
     def attend(self, q, row_offset, length, *, max_rows, max_len=None, scale=None, softcap=0.0, slope=None, prefix=None,
                row_start=None, parent=None, out=None, weight=None, decay=1.0, weight_out=None, stream=None):
@@ -200,7 +206,7 @@ class PagedCache:
         Returns (out, lse), or (out, lse, weight_out): out as q, lse [rows, heads] float32, the natural logarithm
         of the softmax sums.  A row that sees nothing gets zeros and -inf.
         """
-        import torch
+        torch = self._torch
         a = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
         with self._on(stream):
             if out is None:
@@ -213,7 +219,7 @@ class PagedCache:
             weigh = weight is not None or weight_out is not None
             if weigh:
                 weight_out = self._weights(a, weight, weight_out, decay)
-            need = self._lib.rkc_attend_scratch_bytes(ctypes.byref(self._c), ctypes.byref(a))
+            need = self._lib.rkc_attend_scratch_bytes(self._c_ref, ctypes.byref(a))
             if need:
                 scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
                 a.d_scratch, a.scratch_bytes = scratch.data_ptr(), need
@@ -228,7 +234,7 @@ class PagedCache:
         gets  decay * weight[s, h, j] + sum of exp(score - lse)  over the rows and the head's queries; slots behind
         the length are left alone.  weight_out may be weight; by default it is new and zero behind the length.
         """
-        import torch
+        torch = self._torch
         a = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
         if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.device != self.device or not lse.is_contiguous():
             raise ValueError(f"lse: a contiguous float32 tensor {tuple(q.shape[:2])} on {self.device} is wanted")
@@ -252,7 +258,7 @@ class PagedCache:
         the blocks behind the new length are free.  Returns (length, weight_out, pos_out) as new tensors (or the
         ones given), valid up to the new lengths.
         """
-        import torch
+        torch = self._torch
         n = (min(self.max_len, weight.shape[-1]) if max_len is None else max_len)
         self._account(weight, "weight", torch.float32, n)
         e = _Eviction()
@@ -277,7 +283,7 @@ class PagedCache:
             e.d_weight, e.d_pos = weight.data_ptr(), _ptr(pos)
             length_out = torch.empty_like(length)
             e.d_weight_out, e.d_pos_out, e.d_length_out = weight_out.data_ptr(), pos_out.data_ptr(), length_out.data_ptr()
-            need = self._lib.rkc_evict_scratch_bytes(ctypes.byref(self._c), ctypes.byref(e))
+            need = self._lib.rkc_evict_scratch_bytes(self._c_ref, ctypes.byref(e))
             scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             e.d_scratch, e.scratch_bytes = scratch.data_ptr(), scratch.numel()
             self._call("rkc_evict", e, stream)

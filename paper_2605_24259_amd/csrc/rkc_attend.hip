@@ -143,7 +143,7 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   rkc_plan p = {};
   const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
   p.few = M <= 16 || (M <= 32 && c->head_dim <= 128);
-  p.rows = p.few ? (M <= 16 ? 16 : 32) : M <= 128 || c->head_dim == 256 ? 128 : 256;
+  p.rows = p.few ? (M <= 16 ? 16 : 32) : M <= 128 || c->head_dim != 128 ? 128 : 256;
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;

@@ -13,7 +13,7 @@ namespace {
 
 
 template <typename T, int D, int W>
-__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int kRows = 32 * W, kThreads = 64 * W;
   constexpr int BK = D == 256 ? 32 : 64, kAhead = D == 256 || W == 8 ? 3 : 1, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void attend_tile(const rk
         scores(sc, i & 3);
         outputs(i - 1);
         // operands a few products ahead of their use
-        if constexpr (D == 128) {
+        {
           __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
           for (int k = 0; k < KT * (KC + 2 * DB); k++) {
@@ -441,7 +441,7 @@ template <typename T>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
   if (c->head_dim == 256) return go<T, 256, 4>(c, a, p, s);
   if (c->head_dim == 128) return p->rows == 256 ? go<T, 128, 8>(c, a, p, s) : go<T, 128, 4>(c, a, p, s);
-  return p->rows == 256 ? go<T, 64, 8>(c, a, p, s) : go<T, 64, 4>(c, a, p, s);
+  return go<T, 64, 4>(c, a, p, s);
 }
 
 }  // namespace

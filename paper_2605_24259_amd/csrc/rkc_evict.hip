@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kItems = 16, kTile = kThreads * kItems, kMoves = 128;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kItems = 16, kTile = kThreads * kItems, kMoves = 128, kCopies = 16;
 
 struct evict_args {
   rkc_cache c;
@@ -25,14 +25,17 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-// Sum over the lower lanes and this one.
+// Sum over the lower lanes and this one, by shifts within rows of 16 and broadcasts of rows' last lanes.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+  x += moved<0x111, 0xf>(x);  // row_shr:1
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);  // row_bcast:15
+  x += moved<0x143, 0xc>(x);  // row_bcast:31
   return x;
 }
 
@@ -42,8 +45,10 @@ __device__ __forceinline__ int lower(uint64_t m) { return __builtin_amdgcn_mbcnt
 __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
   const rkc_cache& c = g.c;
   const rkc_eviction& e = g.e;
-  // counts of 256 digits, one copy per lane: no two lanes of an addition meet in a bank, whatever the digits
-  __shared__ __attribute__((aligned(16))) uint32_t hist[256 * 64];
+  // counts of 256 digits, a copy for each of 16 lanes: at most 4 lanes of an addition meet in a word, whatever the digits
+  __shared__ __attribute__((aligned(16))) uint32_t hist[256 * kCopies];
+  uint16_t* const gap_at = (uint16_t*)hist;  // later: the gaps of a sequence of one tile
+  static_assert(sizeof(hist) >= kTile / 2 * sizeof(uint16_t), "gaps");
   __shared__ uint32_t table[2][kItems * kWaves + 1];  // counts per run of 64 slots, then what lies before each
   __shared__ uint32_t found[3];
   const int H = c.kv_heads, s = blockIdx.x / H, h = blockIdx.x % H;
@@ -124,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
   uint32_t T = 0, left = K, same = 0;
   if (K > 0) {
     for (int b = 24; b >= 0; b -= 8) {
-      for (int k = tid; k < 256 * 64 / 4; k += kThreads) ((u32x4*)hist)[k] = u32x4{0, 0, 0, 0};
+      ((u32x4*)hist)[tid] = u32x4{0, 0, 0, 0};
       __syncthreads();
       for (int t = 0; t < tiles; t++) {
         if (tiles > 1) load(t), slots_of(t, open, recent);
@@ -133,19 +138,14 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
         for (int i = 0; i < kItems; i++) {
           if (t * kTile + i * kThreads >= len) break;
           const uint32_t key = order_of(wt[i]);
-          if ((in >> i & 1) && (b == 24 || (key ^ T) >> b >> 8 == 0)) atomicAdd(&hist[(key >> b & 255) * 64 + lane], 1u);
+          if ((in >> i & 1) && (b == 24 || (key ^ T) >> b >> 8 == 0)) atomicAdd(&hist[(key >> b & 255) * kCopies + (lane & (kCopies - 1))], 1u);
         }
       }
       __syncthreads();
-      // a quarter of a digit's copies per thread
-      uint32_t n = 0;
-#pragma unroll
-      for (int k = 0; k < 4; k++) {
-        const u32x4 x = ((const u32x4*)hist)[tid * 4 + (k + tid & 3)];
-        n += x[0] + x[1] + x[2] + x[3];
-      }
-      n += __shfl_xor(n, 1);
-      n += __shfl_xor(n, 2);
+      const u32x4 x4 = ((const u32x4*)hist)[tid];  // a quarter of a digit's copies
+      uint32_t n = x4[0] + x4[1] + x4[2] + x4[3];
+      n += (uint32_t)dpp<0xb1>((int)n);  // quad_perm [1,0,3,2]
+      n += (uint32_t)dpp<0x4e>((int)n);  // quad_perm [2,3,0,1]
       __syncthreads();
       if ((tid & 3) == 0) hist[tid >> 2] = n;
       __syncthreads();
@@ -221,20 +221,37 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
       const int j = t * kTile + i * kThreads + tid;
-      const bool kept = keep >> i & 1, is_gap = j < now && !kept, is_src = j >= now && j < len && kept;
-      const uint64_t gap = __ballot(is_gap), src = __ballot(is_src);
-      if (is_gap) gaps[gap0 + table[0][i * kWaves + wave] + lower(gap)] = j;
-      if (is_src) from[from0 + table[1][i * kWaves + wave] + lower(src)] = j;
+      if (t * kTile + i * kThreads >= now) break;
+      const bool kept = keep >> i & 1, is_gap = j < now && !kept;
+      const uint64_t gap = __ballot(is_gap);
+      const int at_gap = gap0 + table[0][i * kWaves + wave] + lower(gap);
+      if (is_gap) gaps[at_gap] = j;
+      if (is_gap && tiles == 1) gap_at[at_gap] = (uint16_t)j;
       if (j < now && kept) w_out[j] = wt[i], pos_out[j] = ps[i];
+    }
+    if (tiles == 1) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; i++) {
+      const int j = t * kTile + i * kThreads + tid;
+      if (t * kTile + i * kThreads >= len) break;
+      const bool is_src = j >= now && j < len && (keep >> i & 1);
+      const uint64_t src = __ballot(is_src);
+      const int at_src = from0 + table[1][i * kWaves + wave] + lower(src);
+      if (is_src) from[at_src] = j;
+      if (is_src && tiles == 1) {
+        const int to = gap_at[at_src];
+        w_out[to] = wt[i], pos_out[to] = ps[i];
+      }
     }
     gap0 += all0, from0 += all1;
     __syncthreads();
   }
   if (tid == 0) g.count[blockIdx.x] = gap0;
-  for (int i = tid; i < (int)gap0; i += kThreads) {
-    const int j = from[i], to = gaps[i];
-    w_out[to] = w[j], pos_out[to] = pos_at(j);
-  }
+  if (tiles > 1)
+    for (int i = tid; i < (int)gap0; i += kThreads) {
+      const int j = from[i], to = gaps[i];
+      w_out[to] = w[j], pos_out[to] = pos_at(j);
+    }
 }
 
 // Moves the keys and values of up to kMoves slots of a head of a sequence, 16 bytes a lane.
