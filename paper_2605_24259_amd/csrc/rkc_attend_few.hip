@@ -2,7 +2,7 @@
 //
 // Up to 32 packed rows (rows x query heads of one key/value head) make one or two column tiles of a 16x16x32
 // matrix product, so every key and value is read once for all of them; what bounds the kernel is that read.
-// A workgroup takes a chunk of one sequence's slots for one head, its four waves take 32 slots at a time:
+// A workgroup takes a chunk of one sequence's slots for one head, its four waves (eight, see rkc_attend_plan) take 32 slots at a time:
 //   K goes from memory straight into the product's operand (a lane holds 8 elements of its slot's key),
 //   V goes through the wave's own 32-slot tile in LDS, from where it is read transposed (no barriers),
 //   both for the next 32 slots are in flight while these are worked on.
@@ -12,9 +12,7 @@
 
 namespace {
 
-constexpr int kWaves = 4;
-
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int KC = D / 32, DB = D / 16, VP = D / 16;  // key operands, output blocks, 16-byte pieces of V per lane
@@ -342,14 +340,19 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
   }
 }
 
+template <typename T, int D, int NT, int W>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  attend_few<T, D, NT, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
 template <typename T, int D>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  const dim3 grid(p->units * p->splits), block(64 * kWaves);
   if constexpr (D <= 128) {
-    if (p->rows == 32) attend_few<T, D, 2><<<grid, block, 0, s>>>(*c, *a, *p);
+    if (p->rows == 32) return go<T, D, 2, 4>(c, a, p, s);
+    if (p->waves == 8) return go<T, D, 1, 8>(c, a, p, s);
   }
-  if (p->rows == 16) attend_few<T, D, 1><<<grid, block, 0, s>>>(*c, *a, *p);
-  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+  return go<T, D, 1, 4>(c, a, p, s);
 }
 
 template <typename T>

@@ -337,6 +337,7 @@ struct rkc_plan {
   int units;   // sequences x key/value heads x row tiles
   int tiles;   // row tiles per sequence and head
   int rows;    // packed rows of a tile
+  int waves;   // of a workgroup, where few
   int chunk, splits;
   bool sorted;  // long sequences first
   size_t part_at, stat_at, bytes;  // scratch: partial outputs, their maxima and sums, in all
