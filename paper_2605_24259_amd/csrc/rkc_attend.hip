@@ -142,8 +142,8 @@ rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool 
 rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   rkc_plan p = {};
   const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
-  p.few = M <= 16 || (M <= 32 && c->head_dim <= 128);
-  p.rows = p.few ? (M <= 16 ? 16 : 32) : M <= 128 || c->head_dim != 128 ? 128 : 256;
+  p.few = M <= 16;
+  p.rows = p.few ? 16 : M <= 128 || c->head_dim != 128 ? 128 : 256;
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
@@ -153,7 +153,7 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   chunk = (chunk + grain - 1) / grain * grain;
   if (chunk < grain) chunk = grain;
   // Short sequences whole, by eight waves: no second kernel for the join (four pools of 80 blocks: xx us instead of yy).
-  p.waves = p.few && p.rows == 16 && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
+  p.waves = p.few && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
   if (p.waves == 8) chunk = a->max_len < 32 ? 32 : (a->max_len + 31) / 32 * 32;
   p.chunk = (int)chunk;
   p.splits = (int)((a->max_len + chunk - 1) / chunk);

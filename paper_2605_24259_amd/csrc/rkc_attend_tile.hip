@@ -11,12 +11,19 @@
 
 namespace {
 
+template <int R> struct Acc;
+template <> struct Acc<32> { typedef f32x16 t; };
+template <> struct Acc<16> { typedef f32x4 t; };
 
-template <typename T, int D, int W>
-__global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+
+template <typename T, int D, int W, int R>
+__global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
-  constexpr int kRows = 32 * W, kThreads = 64 * W;
-  constexpr int BK = D == 256 ? 32 : 64, kAhead = D == 256 || W == 8 ? 3 : 1, KT = BK / 32, KC = D / 16, DB = D / 32, CH = D / 8;
+  // R rows a wave: products of R x R, A elements a lane; tiles of BK slots, kAhead of them on their way
+  typedef typename Acc<R>::t acc;
+  constexpr int A = R * R / 64, kRows = R * W, kThreads = 64 * W;
+  constexpr int BK = D == 256 ? 32 : 64, kAhead = W == 8 ? 3 : 1, CH = D / 8;
+  constexpr int KT = BK / R, KC = D * R / 512, DB = D / R, NP = KT * A / 8;  // score blocks, key operands, output blocks, weight operands
   constexpr int P = BK * CH / kThreads;  // 16-byte pieces of K, and of V, per thread
   constexpr int kTile = BK * D;
   __shared__ __attribute__((aligned(16))) T lds[(kAhead + 1) * 2 * kTile];  // K and V of each tile
@@ -29,8 +36,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
   // 334, documents 57 instead of 49; sequences before row tiles: 455 and 62.)
   const int h = blockIdx.x % H, split = blockIdx.x / H % pl.splits, b = blockIdx.x / (H * pl.splits);
   const int qt = pl.tiles - 1 - b % pl.tiles, s = pl.sorted ? seq_of_rank(c, a, b / pl.tiles) : b / pl.tiles;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), half = lane >> 5, col = lane & 31;
-  // which 32 rows are the wave's: neighbours work in turns on one SIMD, also where a tile is not full
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), grp = lane / R, col = lane % R;
+  // which rows are the wave's: neighbours work in turns on one SIMD, also where a tile is not full
   const int part = W == 8 ? (wave & 3) * 2 + (wave >> 2) : wave;
   const Seq q = load_seq(c, a, s);
   if (!q.ok) {
@@ -45,17 +52,17 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
-  const int m = min(m0 + 32 * part + col, M - 1), qi = m / G, qh = h * G + m % G;
-  const bool mine = m0 + 32 * part + col < M, rows = m0 + 32 * part < M;
+  const int m = min(m0 + R * part + col, M - 1), qi = m / G, qh = h * G + m % G;
+  const bool mine = m0 + R * part + col < M, rows = m0 + R * part < M;
   const Scale f = load_scale(a);
   Row row = load_row(a, q, s, qi);
   const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
   V8 qf[KC];
   {
-    const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + half * 8;
+    const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + grp * 8;
 #pragma unroll
     for (int k = 0; k < KC; k++) {
-      qf[k] = *(const V8*)(p + 16 * k);
+      qf[k] = *(const V8*)(p + 512 / R * k);
       if (f.negate) qf[k] = negated(qf[k]);
     }
   }
@@ -68,7 +75,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
   int all_from = 0, any_from = 0;
   if (a.d_row_start) all_from = wave_max(row.start), any_from = wave_min(row.start);
   const int all_to = uni(row.end), pre = uni(row.prefix);  // a wave's first lane has its first row
-  const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, 31));
+  const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, R - 1));
   if (lane == 0) lim[wave][0] = any_from, lim[wave][1] = any_to;
   __syncthreads();
   int g_any_from = lim[0][0], g_any_to = lim[0][1];
@@ -80,11 +87,11 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
   const Pool kp = k_pool(c, h), vp = v_pool(c, h);
 
   float top = -kInf, sum = 0.f;
-  f32x16 o[DB];
+  acc o[DB];
 #pragma unroll
   for (int d = 0; d < DB; d++)
 #pragma unroll
-    for (int k = 0; k < 16; k++) o[d][k] = 0.f;
+    for (int k = 0; k < A; k++) o[d][k] = 0.f;
 
   // The tiles that any row sees, in order: from c0 on, less those between the prefix and the first document.
   const int end_up = c0 + (max(0, end - c0) + BK - 1) / BK * BK;
@@ -124,44 +131,49 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
       dma(fixed(run_at(vp, block, at)) + v_off[o], to + kTile + p * kThreads * 8);
     }
   };
-  const int vi = lane & 15, vr = 4 * half + (vi >> 2), vc = (lane >> 4 & 1) * 2 + ((vi & 3) >> 1), ve = (vi & 1) * 4;
-  const int key_at = 2 * tile_at<D>(col, half), val_at = 2 * (kTile + tile_at<D>(vr, vc) + ve);
+  // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
+  // a row) and by whole rows.  Element e = 4 x + y of a score block is slot 4 * (64 / R) x + 4 grp + y of its R.
+  const int vi = lane & 15, vr = 4 * grp + (vi >> 2), vc = R == 32 ? (lane >> 4 & 1) * 2 + ((vi & 3) >> 1) : (vi & 3) >> 1, ve = (vi & 1) * 4;
+  const int key_at = 2 * tile_at<D>(col, grp), val_at = 2 * (kTile + tile_at<D>(vr, vc) + ve);
   // whether any of the wave's rows sees anything of a tile, and whether all see all of it
   auto sees = [&](int t0) { return rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre); };
-  // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
-  // a row) and by whole rows
-  auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k << 5) + 64 * D * u); };
-  auto vals = [&](int va, int u, int v, int d) {
-    return read_tr2<T>((const char*)lds + (va ^ d << 6) + 32 * D * (2 * u + v), (const char*)lds + (va ^ d << 6 ^ 32) + 32 * D * (2 * u + v) + 16 * D);
+  auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k * (1024 / R)) + 2 * R * D * u); };
+  // values of the 512 / R slots of weight operand i, columns R d .. R d + R - 1
+  auto vals = [&](int va, int i, int d) {
+    const char* at = (const char*)lds + i * (512 / R) * 2 * D;
+    const int x = va ^ d * 2 * R;
+    if constexpr (R == 32) return read_tr2<T>(at + x, at + (x ^ 32) + 16 * D);
+    else return read_tr2<T>(at + x, at + x + 32 * D);
   };
-  auto scores = [&](f32x16(&sc)[KT], int buf) {
+  auto scores = [&](acc(&sc)[KT], int buf) {
     const int ka = here(buf * 4 * kTile + key_at);
 #pragma unroll
     for (int u = 0; u < KT; u++)
 #pragma unroll
-      for (int k = 0; k < 16; k++) sc[u][k] = 0.f;
+      for (int k = 0; k < A; k++) sc[u][k] = 0.f;
 #pragma unroll
     for (int k = 0; k < KC; k++)
 #pragma unroll
-      for (int u = 0; u < KT; u++) sc[u] = mma32(keys(ka, u, k), qf[k], sc[u]);
+      for (int u = 0; u < KT; u++) sc[u] = mma(keys(ka, u, k), qf[k], sc[u]);
   };
+  auto slot_in = [](int u, int k) { return R * u + (k & 3) + 256 / R * (k >> 2); };  // less 4 grp
   // cap, distance, masks, and the maximum that the weights refer to
-  auto fold = [&](f32x16(&sc)[KT], uint32_t(&seen)[KT], int t0) {
+  auto fold = [&](acc(&sc)[KT], uint32_t(&seen)[BK / 32], int t0) {
     const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
     if (a.softcap > 0.f) {
 #pragma unroll
       for (int u = 0; u < KT; u++)
 #pragma unroll
-        for (int k = 0; k < 16; k++) sc[u][k] = capped(sc[u][k], f);
+        for (int k = 0; k < A; k++) sc[u][k] = capped(sc[u][k], f);
     }
     if (a.d_slope) {
-      const int base_at = here(q.base - t0 - 4 * half);
-      const float far = (float)(here(row.pos - t0) - 4 * half);
+      const int base_at = here(q.base - t0 - 4 * grp);
+      const float far = (float)(here(row.pos - t0) - 4 * grp);
 #pragma unroll
       for (int u = 0; u < KT; u++)
 #pragma unroll
-        for (int k = 0; k < 16; k++) {
-          const int j = 32 * u + (k & 3) + 8 * (k >> 2);
+        for (int k = 0; k < A; k++) {
+          const int j = slot_in(u, k);
           float gap = far - (float)j;
           if (drafts && t0 + BK > q.base) {
             const int i = j - base_at, d = depths[max(0, min(i, RKC_MAX_TREE_ROWS - 1))];
@@ -171,22 +183,24 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
         }
     }
 #pragma unroll
-    for (int u = 0; u < KT; u++) seen[u] = 0xffffffff;
+    for (int x = 0; x < BK / 32; x++) seen[x] = 0xffffffff;
     if (!whole) {
 #pragma unroll
-      for (int u = 0; u < KT; u++) {
-        const int j0 = t0 + 32 * u;
-        seen[u] = seen_of(row, j0, drafts ? line_window(lines[qi], 4, j0 - q.base) : 0) >> 4 * half;
-#pragma unroll
-        for (int k = 0; k < 16; k++) sc[u][k] = masked(sc[u][k], seen[u], (k & 3) + 8 * (k >> 2));
+      for (int x = 0; x < BK / 32; x++) {
+        const int j0 = t0 + 32 * x;
+        seen[x] = seen_of(row, j0, drafts ? line_window(lines[qi], 4, j0 - q.base) : 0) >> 4 * grp;
       }
+#pragma unroll
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int k = 0; k < A; k++) sc[u][k] = masked(sc[u][k], seen[slot_in(u, k) / 32], slot_in(u, k) % 32);
     }
     float most = -kInf;
 #pragma unroll
     for (int u = 0; u < KT; u++)
 #pragma unroll
-      for (int k = 0; k < 16; k++) most = fmaxf(most, sc[u][k]);
-    most = max32(most) * f.post;
+      for (int k = 0; k < A; k++) most = fmaxf(most, sc[u][k]);
+    most = (R == 32 ? max32(most) : max32(max16(most))) * f.post;
     // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
     if (__any(most > top + 8.f)) {
       const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
@@ -195,12 +209,12 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
       for (int d = 0; d < DB; d++) o[d] *= by;
     }
   };
-  // The products' operands have the cache's type: the weights are rounded to it here, their sum is not.
-  auto weights = [&](const f32x16& sc, int v) {
+  // Weight operand i.  The products' operands have the cache's type: the weights are rounded to it here, their sum is not.
+  auto weights = [&](const acc(&sc)[KT], int i) {
     const float mx = top == -kInf ? 0.f : top;
     f32x8 p;
 #pragma unroll
-    for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[8 * v + k], f.post, -mx));
+    for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[(8 * i + k) / A][(8 * i + k) % A], f.post, -mx));
     sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     return __builtin_convertvector(p, V8);
   };
@@ -235,8 +249,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
         if constexpr (careful) hurt = __syncthreads_or(hurt);
         else __syncthreads();
       }
-      f32x16 sc[KT];
-      uint32_t seen[KT];
+      acc sc[KT];
+      uint32_t seen[BK / 32];
       if (sees(t0)) {
         scores(sc, buf);
         fold(sc, seen, t0);
@@ -245,19 +259,20 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
         if (sees(t0)) {
 #pragma unroll
           for (int d = 0; d < DB; d++) {
-            f32x16 n;
+            acc n;
 #pragma unroll
-            for (int k = 0; k < 16; k++) n[k] = 0.f;
+            for (int k = 0; k < A; k++) n[k] = 0.f;
 #pragma unroll 1
-            for (int x = 0; x < 2 * KT; x++) {
-              const uint32_t bits = (KT > 1 && x >> 1 ? seen[KT - 1] : seen[0]) >> 16 * (x & 1);
-              V8 by, vt = vals(va, x >> 1, x & 1, d);
+            for (int x = 0; x < NP; x++) {
+              const int j0 = 512 / R * x;
+              const uint32_t bits = (BK > 32 && j0 >= 32 ? seen[BK / 32 - 1] : seen[0]) >> (j0 & 31);
+              V8 by, vt = vals(va, x, d);
 #pragma unroll
-              for (int k = 0; k < 8; k++) by[k] = (T)(bits >> ((k & 3) + 8 * (k >> 2)) & 1 ? 1.f : 0.f);
-              n = mma32(strip<T>(vt), by, n);
+              for (int k = 0; k < 8; k++) by[k] = (T)(bits >> ((k & 3) + 256 / R * (k >> 2)) & 1 ? 1.f : 0.f);
+              n = mma(strip<T>(vt), by, n);
             }
 #pragma unroll
-            for (int k = 0; k < 16; k++) o[d][k] += hurt_by(n[k]);
+            for (int k = 0; k < A; k++) o[d][k] += hurt_by(n[k]);
           }
         }
         __syncthreads();
@@ -270,13 +285,11 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
       }
       if (sees(t0)) {
 #pragma unroll
-        for (int u = 0; u < KT; u++)
+        for (int x = 0; x < NP; x++) {
+          const V8 pb = weights(sc, x);
 #pragma unroll
-          for (int v = 0; v < 2; v++) {
-            const V8 pb = weights(sc[u], v);
-#pragma unroll
-            for (int d = 0; d < DB; d++) o[d] = mma32(vals(va, u, v, d), pb, o[d]);
-          }
+          for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb, o[d]);
+        }
       }
       buf = buf == kAhead ? 0 : buf + 1;
     }
@@ -307,17 +320,15 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
     };
-    f32x16 sc[KT];
-    V8 pb[2 * KT];
+    acc sc[KT];
+    V8 pb[NP];
     bool had = false;  // weights of the tile before are there
     auto outputs = [&](int i) {
       const int va = here((i & 3) * 4 * kTile + val_at);
 #pragma unroll
-      for (int u = 0; u < KT; u++)
+      for (int x = 0; x < NP; x++)
 #pragma unroll
-        for (int v = 0; v < 2; v++)
-#pragma unroll
-          for (int d = 0; d < DB; d++) o[d] = mma32(vals(va, u, v, d), pb[2 * u + v], o[d]);
+        for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb[x], o[d]);
     };
     auto multiply = [&](int i) {
       const bool has = i < n_tiles && sees(slot_of(i));
@@ -328,7 +339,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
         {
           __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
-          for (int k = 0; k < KT * (KC + 2 * DB); k++) {
+          for (int k = 0; k < KT * KC + NP * DB; k++) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
           }
@@ -344,12 +355,10 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
     auto weigh = [&](int i) {
       const int t0 = slot_of(i);
       if (had) {
-        uint32_t seen[KT];
+        uint32_t seen[BK / 32];
         fold(sc, seen, t0);
 #pragma unroll
-        for (int u = 0; u < KT; u++)
-#pragma unroll
-          for (int v = 0; v < 2; v++) pb[2 * u + v] = weights(sc[u], v);
+        for (int x = 0; x < NP; x++) pb[x] = weights(sc, x);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
@@ -394,54 +403,54 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : D == 64 && W == 4 ? 3 : 2) v
 #pragma unroll
   for (int d = 0; d < DB; d++)
 #pragma unroll
-    for (int k = 0; k < 16; k++) odd = __builtin_fmaf(o[d][k], 0.f, odd);
+    for (int k = 0; k < A; k++) odd = __builtin_fmaf(o[d][k], 0.f, odd);
   if (__syncthreads_or(odd != 0.f)) {
     top = -kInf, sum = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
-      for (int k = 0; k < 16; k++) o[d][k] = 0.f;
+      for (int k = 0; k < A; k++) o[d][k] = 0.f;
     go_over(std::true_type());
   }
   if (bad) flag(c, s, RKC_CS_BLOCK);
 
-  sum = sum32(sum);
+  sum = R == 32 ? sum32(sum) : sum32(sum16(sum));
   if (!mine) return;
   typedef T T4 __attribute__((ext_vector_type(4)));
   if (pl.splits == 1) {
     const float by = sum == 0.f ? 0.f : 1.f / sum;
-    T* to = (T*)a.d_out + (q.row0 + qi) * a.out_row_stride + qh * a.out_head_stride + 4 * half;
+    T* to = (T*)a.d_out + (q.row0 + qi) * a.out_row_stride + qh * a.out_head_stride + 4 * grp;
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
-      for (int k = 0; k < 4; k++) {
+      for (int k = 0; k < A / 4; k++) {
         f32x4 x = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * by;
-        *(T4*)(to + 32 * d + 8 * k) = __builtin_convertvector(x, T4);
+        *(T4*)(to + R * d + 256 / R * k) = __builtin_convertvector(x, T4);
       }
-    if (half == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
+    if (grp == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
   } else {
-    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + 32 * part + col;
-    float* to = (float*)((char*)a.d_scratch + pl.part_at) + at * D + 4 * half;
+    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + R * part + col;
+    float* to = (float*)((char*)a.d_scratch + pl.part_at) + at * D + 4 * grp;
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
-      for (int k = 0; k < 4; k++) *(f32x4*)(to + 32 * d + 8 * k) = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
+      for (int k = 0; k < A / 4; k++) *(f32x4*)(to + R * d + 256 / R * k) = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
     float* st = (float*)((char*)a.d_scratch + pl.stat_at) + at * 2;
-    if (half == 0) st[0] = top, st[1] = sum;
+    if (grp == 0) st[0] = top, st[1] = sum;
   }
 }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, int R>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  attend_tile<T, D, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  attend_tile<T, D, W, R><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 template <typename T>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  if (c->head_dim == 256) return go<T, 256, 4>(c, a, p, s);
-  if (c->head_dim == 128) return p->rows == 256 ? go<T, 128, 8>(c, a, p, s) : go<T, 128, 4>(c, a, p, s);
-  return go<T, 64, 4>(c, a, p, s);
+  if (c->head_dim == 256) return go<T, 256, 8, 16>(c, a, p, s);
+  if (c->head_dim == 128) return p->rows == 256 ? go<T, 128, 8, 32>(c, a, p, s) : go<T, 128, 4, 32>(c, a, p, s);
+  return go<T, 64, 4, 32>(c, a, p, s);
 }
 
 }  // namespace
