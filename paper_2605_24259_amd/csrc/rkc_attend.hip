@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void attend_join(const rkc_cache c, const rkc_
   for (int k = group; k < n; k += N) {
     const float m_k = st[(int64_t)k * pl.rows * 2], l_k = st[(int64_t)k * pl.rows * 2 + 1];
     const f32x4 x = *(const f32x4*)(part + (int64_t)k * pl.rows * D);
-    if (m_k != -kInf) {
+    if (l_k != 0.f) {  // a chunk of which the row sees anything
       const float by = ex2(m_k - top);
       sum += l_k * by, o += x * by;
     }

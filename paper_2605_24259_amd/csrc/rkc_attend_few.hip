@@ -12,15 +12,15 @@
 
 namespace {
 
-template <typename T, int D, int NT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+template <typename T, int D, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int KC = D / 32, DB = D / 16, VP = D / 16;  // key operands, output blocks, 16-byte pieces of V per lane
   constexpr int kTile = 32 * D;                         // elements of a wave's V tile
-  constexpr int kJoin = 16 * NT * D * 4;                // bytes of a wave's output tile at the join
+  constexpr int kJoin = 16 * D * 4;                // bytes of a wave's output tile at the join
   constexpr int kLds = kTile * 2 > kJoin ? kTile * 2 : kJoin;
   __shared__ __attribute__((aligned(16))) char lds[kWaves * kLds];
-  __shared__ float stat[kWaves][16 * NT][2], total[16 * NT];
+  __shared__ float stat[kWaves][16][2], total[16];
 
   const int H = c.kv_heads, G = a.q_heads / H;
   // The parts of a sequence are neighbours, turned by one from head to head: XCDs take workgroups in turn, and where the
@@ -41,25 +41,20 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
   const Scale f = load_scale(a);
-  Row row[NT];
-  int qh[NT], qi[NT];
-  V8 qf[NT][KC];
-  float slope[NT];
-#pragma unroll
-  for (int t = 0; t < NT; t++) {
-    const int m = min(16 * t + col, M - 1);
-    qi[t] = m / G, qh[t] = h * G + m % G;
-    row[t] = load_row(a, q, s, qi[t]);
-    slope[t] = a.d_slope ? a.d_slope[qh[t]] * kLog2e / f.post : 0.f;
-    const T* p = (const T*)a.d_q + (q.row0 + qi[t]) * a.q_row_stride + qh[t] * a.q_head_stride + quad * 8;
+  const int mine_m = min(col, M - 1), qi = mine_m / G, qh = h * G + mine_m % G;
+  Row row = load_row(a, q, s, qi);
+  const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
+  V8 qf[KC];
+  {
+    const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + quad * 8;
 #pragma unroll
     for (int k = 0; k < KC; k++) {
-      qf[t][k] = *(const V8*)(p + 32 * k);
-      if (f.negate) qf[t][k] = negated(qf[t][k]);
+      qf[k] = *(const V8*)(p + 32 * k);
+      if (f.negate) qf[k] = negated(qf[k]);
     }
   }
-  // a tree's rows are at most 32 here: lines as bits of a register, walked through the lanes' parents
-  uint32_t line[NT] = {};
+  // a tree's rows are at most 16 here: lines as bits of a register, walked through the lanes' parents
+  uint32_t line = 0;
   int depth_of = 0;  // depth of row `lane`
   if (a.d_parent && c1 > q.base) {
     int par = -1;
@@ -76,11 +71,8 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
       if (at >= 0) mine |= 1u << at, at = up;
     }
     depth_of = __popc(mine) - 1;
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-      line[t] = (uint32_t)__shfl((int)mine, qi[t]);
-      row[t].pos = q.base + __shfl(depth_of, qi[t]);
-    }
+    line = (uint32_t)__shfl((int)mine, qi);
+    row.pos = q.base + __shfl(depth_of, qi);
   } else if (a.d_parent && a.d_slope) {
     // distances need the rows' depths in every chunk
     int par = lane < q.n ? a.d_parent[q.row0 + lane] : -1;
@@ -90,33 +82,21 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
       const int up = __shfl(par, at & 63);
       if (at >= 0) d++, at = up;
     }
-#pragma unroll
-    for (int t = 0; t < NT; t++) row[t].pos = q.base + __shfl(d, qi[t]);
+    row.pos = q.base + __shfl(d, qi);
   }
   // slots that all rows see, and slots that any sees
-  int all_from = row[0].start, all_to = row[0].end, all_pre = row[0].prefix, any_from = row[0].start;
-  int any_to = max(row[0].end, row[0].prefix);
-#pragma unroll
-  for (int t = 1; t < NT; t++) {
-    all_from = max(all_from, row[t].start), all_to = min(all_to, row[t].end), any_from = min(any_from, row[t].start);
-    any_to = max(any_to, max(row[t].end, row[t].prefix));
-  }
-  all_from = wave_max(all_from), all_to = wave_min(all_to), any_from = wave_min(any_from), any_to = wave_max(any_to);
-  all_pre = uni(all_pre);
+  const int all_from = wave_max(row.start), all_to = wave_min(row.end), any_from = wave_min(row.start), all_pre = uni(row.prefix);
+  int any_to = wave_max(max(row.end, row.prefix));
   if (a.d_parent) any_to = q.len;
   const int end = min(c1, any_to);  // of what is looked at here: a chunk is a multiple of 32 slots
 
   const Pool kp = k_pool(c, h), vp = v_pool(c, h);
   T* tile = (T*)(lds + wave * kLds);
 
-  float top[NT], sum[NT];
-  f32x4 o[NT][DB];
+  float top = -kInf, sum = 0.f;
+  f32x4 o[DB];
 #pragma unroll
-  for (int t = 0; t < NT; t++) {
-    top[t] = -kInf, sum[t] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; d++) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int d = 0; d < DB; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // The tiles of 32 slots that any row sees, in order: from c0 on, less those between the prefix and the first document.
   const int end_up = c0 + (max(0, end - c0) + 31) / 32 * 32;
@@ -164,15 +144,13 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
   }
   for (; i < n_tiles; i += kWaves) {
     const int t0 = slot_of(i);
-    f32x4 sc[NT][2];
+    f32x4 sc[2];
 #pragma unroll
-    for (int t = 0; t < NT; t++)
+    for (int u = 0; u < 2; u++) {
+      sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < 2; u++) {
-        sc[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KC; k++) sc[t][u] = mma16(kf[u][k], qf[t][k], sc[t][u]);
-      }
+      for (int k = 0; k < KC; k++) sc[u] = mma16(kf[u][k], qf[k], sc[u]);
+    }
     const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
     bool hurt = false;
     const int pa = here(put_at), va = here(val_at);
@@ -191,77 +169,66 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
       }
       hurt = __any(hurt);
     }
-    uint32_t seen[NT];
+    uint32_t seen = 0xffffffff;
+    if (a.softcap > 0.f) {
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-      if (a.softcap > 0.f) {
+      for (int e = 0; e < 8; e++) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3], f);
+    }
+    if (a.d_slope) {
+      const float far = (float)(here(row.pos - t0) - quad * 4);
 #pragma unroll
-        for (int e = 0; e < 8; e++) sc[t][e >> 2][e & 3] = capped(sc[t][e >> 2][e & 3], f);
-      }
-      if (a.d_slope) {
-        const float far = (float)(here(row[t].pos - t0) - quad * 4);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          float gap = far - (float)(16 * (e >> 2) + (e & 3));
-          if (a.d_parent && t0 + 32 > q.base) {
-            const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
-            gap = at >= 0 ? (float)(row[t].pos - q.base - d) : gap;
-          }
-          sc[t][e >> 2][e & 3] = __builtin_fmaf(-slope[t], fabsf(gap), sc[t][e >> 2][e & 3]);
+      for (int e = 0; e < 8; e++) {
+        float gap = far - (float)(16 * (e >> 2) + (e & 3));
+        if (a.d_parent && t0 + 32 > q.base) {
+          const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
+          gap = at >= 0 ? (float)(row.pos - q.base - d) : gap;
         }
-      }
-      seen[t] = 0xffffffff;
-      if (!whole) {
-        const int from = t0 - q.base;
-        const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line[t] >> from : line[t] << -from;
-        seen[t] = seen_of(row[t], t0, drafted) >> 4 * quad;
-#pragma unroll
-        for (int e = 0; e < 8; e++) sc[t][e >> 2][e & 3] = masked(sc[t][e >> 2][e & 3], seen[t], 16 * (e >> 2) + (e & 3));
+        sc[e >> 2][e & 3] = __builtin_fmaf(-slope, fabsf(gap), sc[e >> 2][e & 3]);
       }
     }
+    if (!whole) {
+      const int from = t0 - q.base;
+      const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line >> from : line << -from;
+      seen = seen_of(row, t0, drafted) >> 4 * quad;
+#pragma unroll
+      for (int e = 0; e < 8; e++) sc[e >> 2][e & 3] = masked(sc[e >> 2][e & 3], seen, 16 * (e >> 2) + (e & 3));
+    }
     auto vals = [&](int d) { return read_tr2<T>((const char*)tile + (va ^ d << 5), (const char*)tile + (va ^ d << 5) + 32 * D); };
-    if (pl.keep) {  // one column tile
+    if (pl.keep) {
       float* to = (float*)((char*)a.d_scratch + pl.score_at) + (int64_t)(s * H + h) * (a.max_rows * G) * pl.wide + (int64_t)t0 * (a.max_rows * G) + 32 * col + quad * 4;
-      if (col < M) *(f32x4*)to = sc[0][0] * f.post, *(f32x4*)(to + 16) = sc[0][1] * f.post;
+      if (col < M) *(f32x4*)to = sc[0] * f.post, *(f32x4*)(to + 16) = sc[1] * f.post;
     }
     if (i + kWaves < n_tiles) {
       load(i + kWaves);
       if (i + 2 * kWaves < n_tiles) look_up(i + 2 * kWaves);
     }
-    V8 pb[NT];
+    float most = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+    most = max32(max16(most)) * f.post;
+    // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+    if (__any(most > top + 8.f)) {
+      const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
+      top = now, sum *= by;
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-      float most = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
-                         fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
-      most = max32(max16(most)) * f.post;
-      // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
-      if (__any(most > top[t] + 8.f)) {
-        const float now = fmaxf(top[t], most), by = now == -kInf ? 1.f : ex2(top[t] - now);
-        top[t] = now, sum[t] *= by;
-#pragma unroll
-        for (int d = 0; d < DB; d++) o[t][d] *= by;
-      }
-      const float m = top[t] == -kInf ? 0.f : top[t];
-      f32x8 p;
-#pragma unroll
-      for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[t][e >> 2][e & 3], f.post, -m));
-      sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
-      pb[t] = __builtin_convertvector(p, V8);
+      for (int d = 0; d < DB; d++) o[d] *= by;
     }
+    const float m = top == -kInf ? 0.f : top;
+    f32x8 p;
+#pragma unroll
+    for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[e >> 2][e & 3], f.post, -m));
+    sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    // the products' operands have the cache's type: the weights are rounded to it here, their sum is not
+    const V8 pb = __builtin_convertvector(p, V8);
     if (hurt) {
+      V8 by;
 #pragma unroll
-      for (int t = 0; t < NT; t++) {
-        V8 by;
+      for (int e = 0; e < 8; e++) by[e] = (T)(seen >> (16 * (e >> 2) + (e & 3)) & 1 ? 1.f : 0.f);
 #pragma unroll
-        for (int e = 0; e < 8; e++) by[e] = (T)(seen[t] >> (16 * (e >> 2) + (e & 3)) & 1 ? 1.f : 0.f);
+      for (int d = 0; d < DB; d++) {
+        V8 vt = vals(d);
+        const f32x4 n = mma16(strip<T>(vt), by, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int d = 0; d < DB; d++) {
-          V8 vt = vals(d);
-          const f32x4 n = mma16(strip<T>(vt), by, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int k = 0; k < 4; k++) o[t][d][k] += hurt_by(n[k]);
-        }
+        for (int k = 0; k < 4; k++) o[d][k] += hurt_by(n[k]);
       }
       for (int k = lane; k < kTile / 8; k += 64) {
         V8 v = *(const V8*)(tile + 8 * k);
@@ -270,61 +237,41 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
       }
     }
 #pragma unroll
-    for (int d = 0; d < DB; d++) {
-      const V8 vt = vals(d);
-#pragma unroll
-      for (int t = 0; t < NT; t++) o[t][d] = mma16(vt, pb[t], o[t][d]);
-    }
+    for (int d = 0; d < DB; d++) o[d] = mma16(vals(d), pb, o[d]);
   }
 
   if (bad) flag(c, s, RKC_CS_BLOCK);
 
-  // join the waves
-#pragma unroll
-  for (int t = 0; t < NT; t++) {
-    sum[t] = sum32(sum16(sum[t]));
-    if (quad == 0) stat[wave][16 * t + col][0] = top[t], stat[wave][16 * t + col][1] = sum[t];
-  }
+  // join the waves; one that saw nothing of a row has a sum of 0
+  sum = sum32(sum16(sum));
+  if (quad == 0) stat[wave][col][0] = top, stat[wave][col][1] = sum;
   __syncthreads();
-  float m_all[NT], l_all[NT];
+  float m_all = -kInf, l_all = 0.f;
 #pragma unroll
-  for (int t = 0; t < NT; t++) {
-    float m = -kInf, l = 0.f;
+  for (int w = 0; w < kWaves; w++) m_all = fmaxf(m_all, stat[w][col][0]);
 #pragma unroll
-    for (int w = 0; w < kWaves; w++) m = fmaxf(m, stat[w][16 * t + col][0]);
+  for (int w = 0; w < kWaves; w++) l_all += stat[w][col][1] == 0.f ? 0.f : stat[w][col][1] * ex2(stat[w][col][0] - m_all);
+  {
+    const float by = ex2(top - m_all);
+    float* to = (float*)(lds + wave * kLds) + col * D + quad * 4;
+    // 16 rows of D floats: rotated so that the rows' 16-byte pieces do not share banks
 #pragma unroll
-    for (int w = 0; w < kWaves; w++) {
-      const float x = stat[w][16 * t + col][0];
-      l += x == -kInf ? 0.f : stat[w][16 * t + col][1] * ex2(x - m);
-    }
-    m_all[t] = m, l_all[t] = l;
-    const float by = top[t] == -kInf ? 0.f : ex2(top[t] - m);
-    float* to = (float*)(lds + wave * kLds) + (16 * t + col) * D + quad * 4;
-#pragma unroll
-    for (int d = 0; d < DB; d++) {
-      f32x4 x = o[t][d] * by;
-      // 16 rows of D floats: rotated so that the rows' 16-byte pieces do not share banks
-      *(f32x4*)(to + 16 * ((d + col) % DB)) = top[t] == -kInf ? f32x4{0.f, 0.f, 0.f, 0.f} : x;
-    }
+    for (int d = 0; d < DB; d++) *(f32x4*)(to + 16 * ((d + col) % DB)) = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * by;
   }
   const int unit = s * H + h;
   if (wave == 0 && quad == 0) {
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-      const int m = 16 * t + col;
-      if (pl.splits == 1) {
-        if (m < M) a.d_lse[(int64_t)(q.row0 + qi[t]) * a.q_heads + qh[t]] = l_all[t] > 0.f || l_all[t] != l_all[t] ? kLn2 * (m_all[t] + lg2(l_all[t])) : -kInf;
-      } else {
-        float* st = (float*)((char*)a.d_scratch + pl.stat_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + m) * 2;
-        st[0] = m_all[t], st[1] = l_all[t];
-      }
-      total[m] = l_all[t];
+    total[col] = l_all;
+    if (pl.splits > 1) {
+      float* st = (float*)((char*)a.d_scratch + pl.stat_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + col) * 2;
+      st[0] = m_all, st[1] = l_all;
+    } else if (col < M) {
+      a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = l_all == 0.f ? -kInf : kLn2 * (m_all + lg2(l_all));
     }
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < min(16 * NT, M) * (D / 4); x += 64 * kWaves) {
+  for (int x = threadIdx.x; x < M * (D / 4); x += 64 * kWaves) {
     const int m = x / (D / 4), b = x % (D / 4), d = b >> 2;
-    const float* from = (const float*)lds + m * D + 16 * ((d + (m & 15)) % DB) + (b & 3) * 4;
+    const float* from = (const float*)lds + m * D + 16 * ((d + m) % DB) + (b & 3) * 4;
     f32x4 y = *(const f32x4*)from;
 #pragma unroll
     for (int w = 1; w < kWaves; w++) y += *(const f32x4*)((const char*)from + w * kLds);
@@ -340,19 +287,18 @@ __global__ __launch_bounds__(64 * kWaves, D * NT <= 128 ? 2 : 1) void attend_few
   }
 }
 
-template <typename T, int D, int NT, int W>
+template <typename T, int D, int W>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  attend_few<T, D, NT, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  attend_few<T, D, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 template <typename T, int D>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
   if constexpr (D <= 128) {
-    if (p->rows == 32) return go<T, D, 2, 4>(c, a, p, s);
-    if (p->waves == 8) return go<T, D, 1, 8>(c, a, p, s);
+    if (p->waves == 8) return go<T, D, 8>(c, a, p, s);
   }
-  return go<T, D, 1, 4>(c, a, p, s);
+  return go<T, D, 4>(c, a, p, s);
 }
 
 template <typename T>

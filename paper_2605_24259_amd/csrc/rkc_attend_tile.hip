@@ -418,13 +418,14 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   if (!mine) return;
   typedef T T4 __attribute__((ext_vector_type(4)));
   if (pl.splits == 1) {
-    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    const float by = 1.f / sum;
     T* to = (T*)a.d_out + (q.row0 + qi) * a.out_row_stride + qh * a.out_head_stride + 4 * grp;
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
       for (int k = 0; k < A / 4; k++) {
         f32x4 x = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * by;
+        if (sum == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
         *(T4*)(to + R * d + 256 / R * k) = __builtin_convertvector(x, T4);
       }
     if (grp == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));

@@ -1,7 +1,7 @@
 """The operators on a paged KV cache against a plain 64-bit implementation, at the sizes and masks where they can go
 wrong.
 
-Tolerances.  Scores are sums of 32-bit products: relative to A = scale * sum |q| |k| (+ cap + slope * distance) their error
+Tolerances.  Scores are sums of 32-bit products: relative to A = |scale| sum |q| |k| (+ cap + slope * distance) their error
 is a few units of 2^-24, more with the exponent's base changed and the softmax sum behind it; 2^-20 (8 + A) is allowed
 for a logarithm and, relative, for a weight.  Outputs add two roundings to the cache's type (unit roundoff u: 2^-8 or
 2^-11), of the weights and of the result: u (sum p |v| + |out|), and what a float16 weight below its normal range loses.
@@ -47,7 +47,7 @@ def reach(c):
     q = np.nan_to_num(c.q.double().numpy(), nan=0, posinf=0, neginf=0)
     if not q.size:
         return 1.0
-    return c.scale * np.linalg.norm(q, axis=-1).max() * np.linalg.norm(k, axis=-1).max() + c.softcap + \
+    return abs(c.scale) * np.linalg.norm(q, axis=-1).max() * np.linalg.norm(k, axis=-1).max() + c.softcap + \
         (0 if c.slope is None else float(c.slope.max()) * far)
 
 
@@ -118,7 +118,8 @@ def test_the_largest_tree():
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("dim,group,lens,rows", [
     (64, 1, [5, 130, 0, 257], [5, 129, 0, 257]), (128, 4, [70, 200, 33], [33, 64, 0]), (256, 2, [140, 64], [90, 64]),
-    (64, 7, [100], [37]), (128, 1, [400, 1], [3, 1])])
+    (64, 7, [100], [37]), (128, 1, [400, 1], [3, 1]), (128, 3, [900, 513, 64], [60, 130, 64]), (256, 2, [700, 333], [100, 9]),
+    (64, 2, [777], [100])])
 def test_chunks(dtype, dim, group, lens, rows):
     say("case chunk", dtype, dim, group, lens, rows)
     c = ref.Case(dim, lens, rows, dim=dim, group=group, dtype=dtype, bias=dim == 128, softcap=20.0 if group == 2 else 0.0)
@@ -177,6 +178,35 @@ def test_what_is_not_seen_may_be_anything(dtype, form):
     o, z = c.attend()
     assert np.isnan(o).any() and np.isfinite(o).any()
     check_attend(c, out, lse, (o, z))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-3, 5.0])
+@pytest.mark.parametrize("group,rows", [(2, 3), (4, 40)])
+def test_scales(scale, group, rows):
+    """Scores that are all alike, turned round, flat, and a softmax that picks single slots."""
+    say("case scale", scale, group, rows)
+    for softcap in (0.0, 4.0):
+        c = ref.Case(rows, [300, rows], [rows, rows], dim=128, group=group, scale=scale, softcap=softcap)
+        g = gpu_cache(c)
+        out, lse = run_attend(c)
+        check_attend(c, out, lse)
+        check_weigh(c, g.weigh(c.q.cuda(), lse, ints(c.offset), ints(c.lens), **mask(c)), lse, 1.0, None)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,rows,n", [(2, 3, 40), (2, 3, 2500), (2, 80, 100), (2, 20, 2500)])
+def test_queries_that_are_not_numbers(dim, group, rows, n):
+    """A row whose query has a NaN gets NaN, its neighbours what they always get; one chunk and several."""
+    c = ref.Case(n, [n], [rows], kv_heads=1, group=group, dim=dim)
+    want = run_attend(c)
+    c.q[1, 0, 3] = float("nan")
+    out, lse = run_attend(c)
+    assert out[1, 0].isnan().all() and lse[1, 0].isnan()
+    keep = np.ones((rows, group), bool)
+    keep[1, 0] = False
+    import torch
+    assert torch.equal(out[torch.from_numpy(keep)], want[0][torch.from_numpy(keep)])
+    assert torch.equal(lse[torch.from_numpy(keep)], want[1][torch.from_numpy(keep)])
 
 
 def test_scores_of_minus_infinity():
@@ -278,9 +308,22 @@ def test_weigh(dtype, dim, group, lens, rows, kw):
                        to[torch.from_numpy(np.pad(inside, ((0, 0), (0, 0), (0, length - max(lens)))))])
     # with the attention itself
     out2, lse2, w2 = g.attend(q, o, n, weight=c.weight.cuda(), decay=0.5, **mask(c, max_len=max(lens)))
-    assert torch.equal(out2, out) or np.abs(out2.double().cpu() - out.double().cpu()).max() < 0.1
+    check_attend(c, out2, lse2)
     check_weigh(c, w2, lse2, 0.5, c.weight)
     assert not g.status.any().item()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4, 30])
+def test_account_of_documents(rows):
+    """Attention with its account where slots lie before every row's document, with and without a prefix."""
+    for prefix in (None, [50, 7]):
+        lens = [700, 300]
+        c = ref.Case(rows, lens, [rows] * 2, dim=128, group=2, row_start=[min(x, 650) for x in [400] * rows + [130] * rows], prefix=prefix)
+        g = gpu_cache(c)
+        w = c.weight.cuda()
+        out, lse, got = g.attend(c.q.cuda(), ints(c.offset), ints(c.lens), weight=w, decay=0.5, **mask(c, max_len=700))
+        check_attend(c, out, lse)
+        check_weigh(c, got, lse, 0.5, c.weight)
 
 
 def test_no_rows():
