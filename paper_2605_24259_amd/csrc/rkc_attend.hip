@@ -147,7 +147,7 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
-  const int64_t want = p.few ? 12 * 256 : c->head_dim == 256 || p.rows == 256 ? 256 : 2 * 256, grain = p.few || c->head_dim == 256 ? 128 : 256;
+  const int64_t want = p.few ? 10 * 256 : c->head_dim == 256 || p.rows == 256 ? 256 : 2 * 256, grain = p.few || c->head_dim == 256 ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;  // workgroups along a sequence
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;

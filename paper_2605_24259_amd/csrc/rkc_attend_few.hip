@@ -23,10 +23,10 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
   __shared__ float stat[kWaves][16][2], total[16];
 
   const int H = c.kv_heads, G = a.q_heads / H;
-  // The parts of a sequence are neighbours, turned by one from head to head: XCDs take workgroups in turn, and where the
-  // parts are a multiple of 8 an XCD would else have the same part of every sequence, the last ones of short
-  // sequences being empty (64 sequences of 1 to 4,096 slots: 159 us instead of 120).
-  const int u = blockIdx.x / pl.splits, h = u % H, s = u / H, split = (blockIdx.x % pl.splits + u) % pl.splits;
+  // The parts of a sequence are neighbours, turned by a number of their own in each: XCDs take workgroups in turn, and
+  // an XCD would else have the same parts of every sequence, the last ones of short sequences being empty (64 sequences
+  // of 1 to 4,096 slots in 8 parts: 159 us instead of 120).
+  const int u = blockIdx.x / pl.splits, h = u % H, s = u / H, split = (blockIdx.x % pl.splits + (u * 0x9e3779b1u >> 16)) % pl.splits;
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), quad = lane >> 4, col = lane & 15;
   const Seq q = load_seq(c, a, s);
   if (!q.ok) {
@@ -133,8 +133,8 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
     }
   };
   // byte offsets in the tile: of this lane's piece of V, and of its first values for a product
-  const int put_at = 2 * tile_at<D>(lane / (D / 8), lane % (D / 8));
-  const int val_at = 2 * (tile_at<D>(quad * 4 + (col >> 2), (col & 3) >> 1) + (col & 1) * 4);
+  const int put_at = 2 * vals16_at<D>(lane / (D / 8), lane % (D / 8));
+  const int val_at = 2 * (vals16_at<D>(quad * 4 + (col >> 2), (col & 3) >> 1) + (col & 1) * 4);
 
   int i = wave;
   if (i < n_tiles) {
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
     const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
     bool hurt = false;
     const int pa = here(put_at), va = here(val_at);
-    auto put = [&](int p, u32x4 x) { *(u32x4*)((char*)tile + ((pa ^ tile_x<D>(p * RP) << 4) + p * RP * 2 * D)) = x; };
+    auto put = [&](int p, u32x4 x) { *(u32x4*)((char*)tile + ((pa ^ vals16_x<D>(p * RP) << 4) + p * RP * 2 * D)) = x; };
     if (whole) {
 #pragma unroll
       for (int p = 0; p < VP; p++) put(p, vf[p]);

@@ -104,11 +104,13 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   bool bad = false;
   // this thread's pieces of a tile: a wave's pieces of one load lie in 16 slots of one page
   const int lane_run = uni(tid / CH & ~15);
+  auto key_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : keys16_at<D>(r, c); };
+  auto val_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : vals16_at<D>(r, c); };
   uint32_t k_off[2], v_off[2];  // of a piece in its run; the chunk is the one that the tile's layout has at its place
 #pragma unroll
   for (int p = 0; p < 2; p++) {
-    const uint32_t r = (p * kThreads + tid) / CH, e = (tile_at<D>(r, tid % CH) - r * D) * 2;
-    k_off[p] = (r & 15) * kp.slot + e, v_off[p] = (r & 15) * vp.slot + e;
+    const uint32_t r = (p * kThreads + tid) / CH;
+    k_off[p] = (r & 15) * kp.slot + (key_in(r, tid % CH) - r * D) * 2, v_off[p] = (r & 15) * vp.slot + (val_in(r, tid % CH) - r * D) * 2;
   }
   int page[P];  // of the next tile to be loaded
   auto run_of = [&](int t0, int p) {  // a run behind the end stands for the first one
@@ -134,7 +136,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
   // a row) and by whole rows.  Element e = 4 x + y of a score block is slot 4 * (64 / R) x + 4 grp + y of its R.
   const int vi = lane & 15, vr = 4 * grp + (vi >> 2), vc = R == 32 ? (lane >> 4 & 1) * 2 + ((vi & 3) >> 1) : (vi & 3) >> 1, ve = (vi & 1) * 4;
-  const int key_at = 2 * tile_at<D>(col, grp), val_at = 2 * (kTile + tile_at<D>(vr, vc) + ve);
+  const int key_at = 2 * key_in(col, grp), val_at = 2 * (kTile + val_in(vr, vc) + ve);
   // whether any of the wave's rows sees anything of a tile, and whether all see all of it
   auto sees = [&](int t0) { return rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre); };
   auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k * (1024 / R)) + 2 * R * D * u); };

@@ -83,6 +83,12 @@ __device__ __forceinline__ int wave_max(int x) { return wave_all(x, [](int a, in
 template <int D> __device__ __forceinline__ constexpr int tile_x(int r) { return D == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3); }
 template <int D> __device__ __forceinline__ constexpr int tile_at(int r, int c) { return r * D + ((c ^ tile_x<D>(r)) << 3); }
 
+// The same for products of 16 rows.  Keys, four chunks of 16 rows at a time: the number is the row's own.  Values, 32 bytes
+// of 16 rows at a time: pairs of chunks stay together.
+template <int D> __device__ __forceinline__ constexpr int keys16_at(int r, int c) { return r * D + ((c ^ (D == 64 ? r >> 1 & 7 : r & 15)) << 3); }
+template <int D> __device__ __forceinline__ constexpr int vals16_x(int r) { return D == 64 ? (r >> 1 & 3) << 1 : (r & 7) << 1; }
+template <int D> __device__ __forceinline__ constexpr int vals16_at(int r, int c) { return r * D + ((c ^ vals16_x<D>(r)) << 3); }
+
 // Keeps the compiler from moving what follows from x out of a loop, where every element of a tile would cost a register.
 __device__ __forceinline__ int here(int x) {
   asm volatile("" : "+v"(x));

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rk
     for (int x = tid; x < rows_up * (D / 8); x += kThreads) {
       const int r = x / (D / 8), m = min(mb + r, M - 1), qi = m / G;
       V8 v = *(const V8*)((const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + (h * G + m - qi * G) * a.q_head_stride + x % (D / 8) * 8);
-      *(V8*)(rows_q + tile_at<D>(r, x % (D / 8))) = sc.negate ? negated(v) : v;
+      *(V8*)(rows_q + keys16_at<D>(r, x % (D / 8))) = sc.negate ? negated(v) : v;
     }
     if (tid < rows_up) {
       const int m = mb + tid;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rk
         const int rm = m0 + quad * 4;  // rows of this lane's four elements of a product
         V8 qf[KC];
 #pragma unroll
-        for (int k = 0; k < KC; k++) qf[k] = *(const V8*)(rows_q + tile_at<D>(m0 + col, 4 * k + quad));
+        for (int k = 0; k < KC; k++) qf[k] = *(const V8*)(rows_q + keys16_at<D>(m0 + col, 4 * k + quad));
         const f32x4 z = *(const f32x4*)(lse2 + rm);  // rows behind the last one have a sum of infinity
         f32x4 x[kRuns];
 #pragma unroll
