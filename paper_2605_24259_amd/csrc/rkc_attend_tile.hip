@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
 
   const Pool kp = k_pool(c, h), vp = v_pool(c, h);
 
-  float top = -kInf, sum = 0.f;
+  float top = -kInf, sum = 0.f, lift = 0.f;  // lift: what all scores of a tile and lane are to lose yet
   acc o[DB];
 #pragma unroll
   for (int d = 0; d < DB; d++)
@@ -168,7 +168,14 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
 #pragma unroll
         for (int k = 0; k < A; k++) sc[u][k] = capped(sc[u][k], f);
     }
-    if (a.d_slope) {
+    if (a.d_slope && t0 + BK <= all_to) {  // all slots lie before all rows: the part that is the same for a row's slots waits
+      lift = slope * (float)(row.pos - t0 - 4 * grp) * f.post;
+#pragma unroll
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int k = 0; k < A; k++) sc[u][k] = __builtin_fmaf(slope, (float)slot_in(u, k), sc[u][k]);
+    } else if (a.d_slope) {
+      lift = 0.f;
       const int base_at = here(q.base - t0 - 4 * grp);
       const float far = (float)(here(row.pos - t0) - 4 * grp);
 #pragma unroll
@@ -202,7 +209,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
     for (int u = 0; u < KT; u++)
 #pragma unroll
       for (int k = 0; k < A; k++) most = fmaxf(most, sc[u][k]);
-    most = (R == 32 ? max32(most) : max32(max16(most))) * f.post;
+    most = most * f.post - lift;
+    most = R == 32 ? max32(most) : max32(max16(most));
     // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
     if (__any(most > top + 8.f)) {
       const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
@@ -213,7 +221,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   };
   // Weight operand i.  The products' operands have the cache's type: the weights are rounded to it here, their sum is not.
   auto weights = [&](const acc(&sc)[KT], int i) {
-    const float mx = top == -kInf ? 0.f : top;
+    const float mx = (top == -kInf ? 0.f : top) + lift;
     f32x8 p;
 #pragma unroll
     for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[(8 * i + k) / A][(8 * i + k) % A], f.post, -mx));
