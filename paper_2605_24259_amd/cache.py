@@ -70,12 +70,9 @@ def declare(lib):
 _HERE = contextlib.nullcontext()
 
 
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
-
-
 class PagedCache:
-    """Blocks of keys and values, and the sequences that lie in them.
+    """Blocks of keys and values, and the sequences that lie in them.  Calls run on the current device, which has to be
+    the cache's.
 
     k, v         [blocks, slots, kv_heads, head_dim], bfloat16 or float16, on the GPU: any strides (multiples of 8
                  elements) with the last dimension contiguous; 16, 32, ... 1,024 slots a block; head_dim 64, 128 or
@@ -99,11 +96,15 @@ class PagedCache:
             raise TypeError(f"k and v are bfloat16 or float16, alike: {k.dtype}, {v.dtype}")
         if k.stride(3) != 1 or v.stride(3) != 1:
             raise ValueError("the last dimension of k and v must be contiguous")
-        self._int32 = torch.int32
+        self._int32, self._torch, self._raw_stream = torch.int32, torch, torch._C._cuda_getCurrentRawStream
+        self._index, self._scale = k.get_device(), 1 / math.sqrt(k.shape[3])
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         if not k.is_cuda or v.device != k.device:
             raise ValueError("k and v must be on one GPU")
-        self.block_table = self._ints(block_table, "block_table", 2)
+        if block_table.dtype is not torch.int32 or block_table.device != self.device or block_table.dim() != 2 or \
+                not block_table.is_contiguous():
+            raise ValueError(f"block_table: a contiguous int32 tensor [seqs, pages] on {self.device} is wanted")
+        self.block_table = block_table
         self.status = torch.zeros(block_table.shape[0], dtype=torch.int32, device=self.device)
         c = _Cache()
         c.n_seqs, c.max_pages = block_table.shape
@@ -111,81 +112,69 @@ class PagedCache:
         c.dtype = types[k.dtype]
         c.k_block_stride, c.k_slot_stride, c.k_head_stride = k.stride()[:3]
         c.v_block_stride, c.v_slot_stride, c.v_head_stride = v.stride()[:3]
-        c.d_k, c.d_v, c.d_block_table, c.d_status = k.data_ptr(), v.data_ptr(), _ptr(self.block_table), _ptr(self.status)
+        c.d_k, c.d_v, c.d_block_table, c.d_status = k.data_ptr(), v.data_ptr(), block_table.data_ptr(), self.status.data_ptr()
         self._c, self._c_ref = c, ctypes.byref(c)
-        self._torch, self._raw_stream = torch, torch._C._cuda_getCurrentRawStream
-        self._index = k.device.index
         self.n_seqs, self.kv_heads, self.head_dim = int(c.n_seqs), int(c.kv_heads), int(c.head_dim)
         self.max_len = int(c.max_pages) * int(c.page_tokens)
 
-    def _ints(self, t, name, dim=1, n=None, optional=False):
-        if t is None and optional:
-            return None
-        if t.dtype != self._int32 or t.device != self.device or t.dim() != dim or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous int32 tensor of {dim} dimension(s) on {self.device} is wanted")
-        if n is not None and t.shape[0] != n:
-            raise ValueError(f"{name}: {n} values are wanted, got {t.shape[0]}")
-        return t
+    def _ints(self, t, name, n):
+        """Address of a contiguous int32 tensor of n values on the cache's device."""
+        if t.dtype is not self._int32 or t.get_device() != self._index or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous int32 tensor of {n} values on {self.device} is wanted, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
 
     def _account(self, t, name, dtype, max_len):
-        if t.dtype != dtype or t.device != self.device or t.dim() != 3 or t.stride(2) != 1 or \
-                t.shape[0] != self.n_seqs or t.shape[1] != self.kv_heads or t.shape[2] < max_len:
+        """Strides of an account (or of its positions)."""
+        if t.dtype is not dtype or t.get_device() != self._index or t.dim() != 3 or \
+                t.shape[0] != self.n_seqs or t.shape[1] != self.kv_heads or t.shape[2] < max_len or t.stride(2) != 1:
             raise ValueError(f"{name}: [{self.n_seqs}, {self.kv_heads}, >= {max_len}] of {dtype} on {self.device}, the last "
-                             "dimension contiguous, is wanted")
-        return t
+                             f"dimension contiguous, is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        # of a dimension of one, the stride says nothing
+        return t.stride(0) if self.n_seqs > 1 else 0, t.stride(1) if self.kv_heads > 1 else 0
 
     def _attention(self, q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent):
-        torch = self._torch
-        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype != self.dtype or q.device != self.device or q.stride(2) != 1:
+        """Checks what attend and weigh share; the fields of rkc_attention in two runs, around those of the outputs."""
+        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not self.dtype or q.get_device() != self._index or q.stride(2) != 1:
             raise ValueError(f"q: [rows, heads, {self.head_dim}] of {self.dtype} on {self.device}, the last dimension "
-                             "contiguous, is wanted")
-        if q.shape[1] % self.kv_heads or not q.shape[1]:
-            raise ValueError(f"q: {q.shape[1]} heads are no multiple of the cache's {self.kv_heads}")
-        n = q.shape[0]
-        if slope is not None and (slope.dtype != torch.float32 or slope.device != self.device or not slope.is_contiguous()
-                                  or tuple(slope.shape) != (q.shape[1],)):
-            raise ValueError(f"slope: [{q.shape[1]}] float32 on {self.device} is wanted")
-        a = _Attention()
-        a.n_rows, a.q_heads, a.max_rows = n, q.shape[1], max_rows
-        a.max_len = self.max_len if max_len is None else max_len
-        a.scale = 1 / math.sqrt(self.head_dim) if scale is None else scale
-        a.softcap, a.decay = softcap, 1.0
-        a.q_row_stride, a.q_head_stride = q.stride(0), q.stride(1)
-        a.d_q = q.data_ptr()
-        a.d_row_offset = _ptr(self._ints(row_offset, "row_offset", n=self.n_seqs + 1))
-        a.d_length = _ptr(self._ints(length, "length", n=self.n_seqs))
-        a.d_row_start = _ptr(self._ints(row_start, "row_start", n=n, optional=True))
-        a.d_prefix = _ptr(self._ints(prefix, "prefix", n=self.n_seqs, optional=True))
-        a.d_parent = _ptr(self._ints(parent, "parent", n=n, optional=True))
-        a.d_slope = _ptr(slope)
-        return a
+                             f"contiguous, is wanted, got {q.dtype} {tuple(q.shape)} on {q.device}")
+        n, heads, _ = q.shape
+        if heads % self.kv_heads or not heads:
+            raise ValueError(f"q: {heads} heads are no multiple of the cache's {self.kv_heads}")
+        if slope is not None and (slope.dtype is not self._torch.float32 or slope.get_device() != self._index
+                                  or not slope.is_contiguous() or tuple(slope.shape) != (heads,)):
+            raise ValueError(f"slope: [{heads}] float32 on {self.device} is wanted")
+        offsets, lengths = self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)
+        head = (n, heads, max_rows, self.max_len if max_len is None else max_len, self._scale if scale is None else scale, softcap)
+        tail = (q.data_ptr(), offsets, lengths, None if row_start is None else self._ints(row_start, "row_start", n),
+                None if prefix is None else self._ints(prefix, "prefix", self.n_seqs),
+                None if parent is None else self._ints(parent, "parent", n), None if slope is None else slope.data_ptr())
+        return head, (q.stride(0), q.stride(1)), tail
 
-    def _weights(self, a, weight, weight_out, decay):
+    def _weights(self, weight, weight_out, n):
+        """(weight_out, its strides) for the account `weight`, or none."""
         torch = self._torch
-        n = int(a.max_len)
-        if weight is not None:
-            self._account(weight, "weight", torch.float32, n)
+        at = None if weight is None else self._account(weight, "weight", torch.float32, n)
         if weight_out is None:
             weight_out = torch.zeros(self.n_seqs, self.kv_heads, n, device=self.device) if weight is None else \
                 torch.empty_strided(weight.shape, weight.stride(), dtype=weight.dtype, device=self.device).zero_()
-        else:
-            self._account(weight_out, "weight_out", torch.float32, n)
-        if weight is not None and weight.stride() != weight_out.stride():
+        to = self._account(weight_out, "weight_out", torch.float32, n)
+        if at is not None and at != to:
             raise ValueError(f"weight and weight_out differ in strides: {weight.stride()}, {weight_out.stride()}")
-        a.weight_seq_stride, a.weight_head_stride = weight_out.stride()[:2]
-        a.d_weight_in, a.d_weight, a.decay = _ptr(weight), weight_out.data_ptr(), decay
-        return weight_out
+        return weight_out, to
 
-    def _call(self, name, args, stream):
+    def _call(self, f, name, args, stream):
         # the current stream of the cache's device; looked up by number, a twentieth of the cost of a Stream object
-        at = self._raw_stream(self._index) if stream is None else _stream_ptr(stream)
-        st = getattr(self._lib, name)(self._c_ref, ctypes.byref(args), at)
+        st = f(self._c_ref, args, self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
         if st != 0:
             raise RkcError(st, name)
 
     def _on(self, stream):
         """Tensors made in a call belong to the stream that the call runs on."""
-        return self._torch.cuda.stream(stream) if stream is not None else _HERE
+        return _HERE if stream is None else self._torch.cuda.stream(stream)
+
+    def _scratch(self, need):
+        return self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
 
     def attend(self, q, row_offset, length, *, max_rows, max_len=None, scale=None, softcap=0.0, slope=None, prefix=None,
                row_start=None, parent=None, out=None, weight=None, decay=1.0, weight_out=None, stream=None):
@@ -206,24 +195,24 @@ class PagedCache:
         Returns (out, lse), or (out, lse, weight_out): out as q, lse [rows, heads] float32, the natural logarithm
         of the softmax sums.  A row that sees nothing gets zeros and -inf.
         """
-        torch = self._torch
-        a = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
+        head, q_strides, tail = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
+        weigh, strides = weight is not None or weight_out is not None, (0, 0)
         with self._on(stream):
             if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or out.stride(2) != 1:
+                out = q.new_empty(q.shape)
+            elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or out.stride(2) != 1:
                 raise ValueError("out: a tensor like q, the last dimension contiguous, is wanted")
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-            a.out_row_stride, a.out_head_stride = out.stride(0), out.stride(1)
-            a.d_out, a.d_lse = out.data_ptr(), lse.data_ptr()
-            weigh = weight is not None or weight_out is not None
+            lse = q.new_empty(q.shape[:2], dtype=self._torch.float32)
             if weigh:
-                weight_out = self._weights(a, weight, weight_out, decay)
-            need = self._lib.rkc_attend_scratch_bytes(self._c_ref, ctypes.byref(a))
+                weight_out, strides = self._weights(weight, weight_out, head[3])
+            a = _Attention(*head, decay, 0, *q_strides, out.stride(0), out.stride(1), *strides, *tail, out.data_ptr(), lse.data_ptr(),
+                           None if weight is None else weight.data_ptr(), weight_out.data_ptr() if weigh else None)
+            ref = ctypes.byref(a)
+            need = self._lib.rkc_attend_scratch_bytes(self._c_ref, ref)
             if need:
-                scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+                scratch = self._scratch(need)
                 a.d_scratch, a.scratch_bytes = scratch.data_ptr(), need
-            self._call("rkc_attend", a, stream)
+            self._call(self._lib.rkc_attend, "rkc_attend", ref, stream)
         return (out, lse, weight_out) if weigh else (out, lse)
 
     def weigh(self, q, lse, row_offset, length, *, max_rows, max_len=None, scale=None, softcap=0.0, slope=None, prefix=None,
@@ -234,14 +223,14 @@ class PagedCache:
         gets  decay * weight[s, h, j] + sum of exp(score - lse)  over the rows and the head's queries; slots behind
         the length are left alone.  weight_out may be weight; by default it is new and zero behind the length.
         """
-        torch = self._torch
-        a = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
-        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.device != self.device or not lse.is_contiguous():
+        head, q_strides, tail = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
+        if lse.dtype is not self._torch.float32 or lse.shape != q.shape[:2] or lse.get_device() != self._index or not lse.is_contiguous():
             raise ValueError(f"lse: a contiguous float32 tensor {tuple(q.shape[:2])} on {self.device} is wanted")
-        a.d_lse = lse.data_ptr()
         with self._on(stream):
-            weight_out = self._weights(a, weight, weight_out, decay)
-            self._call("rkc_weigh", a, stream)
+            weight_out, strides = self._weights(weight, weight_out, head[3])
+            a = _Attention(*head, decay, 0, *q_strides, 0, 0, *strides, *tail, None, lse.data_ptr(),
+                           None if weight is None else weight.data_ptr(), weight_out.data_ptr())
+            self._call(self._lib.rkc_weigh, "rkc_weigh", ctypes.byref(a), stream)
         return weight_out
 
     def evict(self, weight, length, budget, *, protect=None, recent_from=None, pos=None, max_len=None, weight_out=None,
@@ -259,32 +248,25 @@ class PagedCache:
         ones given), valid up to the new lengths.
         """
         torch = self._torch
-        n = (min(self.max_len, weight.shape[-1]) if max_len is None else max_len)
-        self._account(weight, "weight", torch.float32, n)
-        e = _Eviction()
+        n = min(self.max_len, weight.shape[-1]) if max_len is None else max_len
+        strides = self._account(weight, "weight", torch.float32, n)
         with self._on(stream):
             if weight_out is None:
                 weight_out = torch.empty_strided(weight.shape, weight.stride(), dtype=weight.dtype, device=self.device)
             if pos_out is None:
                 pos_out = torch.empty_strided(weight.shape, weight.stride(), dtype=torch.int32, device=self.device)
-            self._account(weight_out, "weight_out", torch.float32, n)
-            for name, t in (("pos", pos), ("pos_out", pos_out)):
-                if t is not None:
-                    self._account(t, name, torch.int32, n)
-            for name, t in (("weight_out", weight_out), ("pos", pos), ("pos_out", pos_out)):
-                if t is not None and t.stride() != weight.stride():
+            for name, t, dtype in (("weight_out", weight_out, torch.float32), ("pos", pos, torch.int32), ("pos_out", pos_out, torch.int32)):
+                if t is not None and self._account(t, name, dtype, n) != strides:
                     raise ValueError(f"{name} and weight differ in strides: {t.stride()}, {weight.stride()}")
-            e.max_len = n
-            e.weight_seq_stride, e.weight_head_stride = weight.stride()[:2]
-            e.d_length = _ptr(self._ints(length, "length", n=self.n_seqs))
-            e.d_budget = _ptr(self._ints(budget, "budget", n=self.n_seqs))
-            e.d_protect = _ptr(self._ints(protect, "protect", n=self.n_seqs, optional=True))
-            e.d_recent_from = _ptr(self._ints(recent_from, "recent_from", n=self.n_seqs, optional=True))
-            e.d_weight, e.d_pos = weight.data_ptr(), _ptr(pos)
             length_out = torch.empty_like(length)
-            e.d_weight_out, e.d_pos_out, e.d_length_out = weight_out.data_ptr(), pos_out.data_ptr(), length_out.data_ptr()
-            need = self._lib.rkc_evict_scratch_bytes(self._c_ref, ctypes.byref(e))
-            scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-            e.d_scratch, e.scratch_bytes = scratch.data_ptr(), scratch.numel()
-            self._call("rkc_evict", e, stream)
+            e = _Eviction(n, 0, *strides, self._ints(length, "length", self.n_seqs), self._ints(budget, "budget", self.n_seqs),
+                          None if protect is None else self._ints(protect, "protect", self.n_seqs),
+                          None if recent_from is None else self._ints(recent_from, "recent_from", self.n_seqs),
+                          weight.data_ptr(), None if pos is None else pos.data_ptr(), weight_out.data_ptr(), pos_out.data_ptr(),
+                          length_out.data_ptr())
+            ref = ctypes.byref(e)
+            need = self._lib.rkc_evict_scratch_bytes(self._c_ref, ref)
+            scratch = self._scratch(need)
+            e.d_scratch, e.scratch_bytes = scratch.data_ptr(), need
+            self._call(self._lib.rkc_evict, "rkc_evict", ref, stream)
         return length_out, weight_out, pos_out

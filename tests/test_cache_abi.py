@@ -124,6 +124,7 @@ def test_eviction_checks(lib, fault, status):
 def test_scratch(lib):
     null = None
     c, a, e = structs()
+    c.max_pages, a.max_len = 256, 4096  # long enough that the attention splits a sequence
     for name, x in (("rkc_attend", a), ("rkc_evict", e)):
         need = getattr(lib, name + "_scratch_bytes")(ctypes.byref(c), ctypes.byref(x))
         assert need > 0
