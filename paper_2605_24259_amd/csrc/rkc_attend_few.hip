@@ -170,10 +170,7 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
       hurt = __any(hurt);
     }
     uint32_t seen = 0xffffffff;
-    if (a.softcap > 0.f) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) sc[e >> 2][e & 3] = capped(sc[e >> 2][e & 3], f);
-    }
+    if (a.softcap > 0.f) cap_all(sc, f);
     if (a.d_slope) {
       const float far = (float)(here(row.pos - t0) - quad * 4);
 #pragma unroll
@@ -206,8 +203,8 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
                        fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
     most = max32(max16(most)) * f.post;
     // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
-    if (__any(most > top + 8.f)) {
-      const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
+    if (__any(most > top + (8.f + kRoom<T>))) {
+      const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
       top = now, sum *= by;
 #pragma unroll
       for (int d = 0; d < DB; d++) o[d] *= by;

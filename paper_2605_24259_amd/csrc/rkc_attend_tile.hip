@@ -162,12 +162,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   // cap, distance, masks, and the maximum that the weights refer to
   auto fold = [&](acc(&sc)[KT], uint32_t(&seen)[BK / 32], int t0) {
     const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
-    if (a.softcap > 0.f) {
-#pragma unroll
-      for (int u = 0; u < KT; u++)
-#pragma unroll
-        for (int k = 0; k < A; k++) sc[u][k] = capped(sc[u][k], f);
-    }
+    if (a.softcap > 0.f) cap_all(sc, f);
     if (a.d_slope && t0 + BK <= all_to) {  // all slots lie before all rows: the part that is the same for a row's slots waits
       lift = slope * (float)(row.pos - t0 - 4 * grp) * f.post;
 #pragma unroll
@@ -212,8 +207,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
     most = most * f.post - lift;
     most = R == 32 ? max32(most) : max32(max16(most));
     // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
-    if (__any(most > top + 8.f)) {
-      const float now = fmaxf(top, most), by = now == -kInf ? 1.f : ex2(top - now);
+    if (__any(most > top + (8.f + kRoom<T>))) {
+      const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
       top = now, sum *= by;
 #pragma unroll
       for (int d = 0; d < DB; d++) o[d] *= by;

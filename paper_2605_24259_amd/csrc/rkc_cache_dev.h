@@ -132,8 +132,14 @@ template <typename T> __device__ __forceinline__ typename Vec8<T>::t read_tr2(co
 // replaced by zeros, and once more with a code in their place against "seen" in place of the weights; the counts
 // in that sum say what the rows get.
 template <typename T> struct Bits;
-template <> struct Bits<__bf16> { static constexpr uint16_t e = 0x7f80; };
+template <> struct Bits<__bf16> { static constexpr uint16_t e = 0x7f80; };  // the exponent's bits
 template <> struct Bits<_Float16> { static constexpr uint16_t e = 0x7c00; };
+
+// Weights are exp2(score - top), and top lies this far below the row's maximum when it is set: with 16-bit floats of 5
+// bits of exponent, the many small weights of a long row would else fall among the numbers without a leading one and
+// lose bits there.  Up to 2^8 more is let stand until the maximum moves, 2^14 in all.
+template <typename T> constexpr float kRoom = 0.f;
+template <> inline constexpr float kRoom<_Float16> = 6.f;
 
 template <typename T> __device__ __forceinline__ bool any_hurt(u32x4 x) {
   bool bad = false;
@@ -307,27 +313,59 @@ __device__ __forceinline__ int block_of(const rkc_cache& c, int id, bool& bad) {
   return out ? 0 : id;
 }
 
-// The factors of a score: x = raw * pre, or capped; then x - slope * distance; weights are exp2(x * post - maximum).
-// Without a cap the scale stays out of the scores until the exponent takes it up; a negative scale goes into
-// the queries' signs, so that the maximum of the scores is that of the products.
+// The factors of a score: x = raw, or capped; then x - slope * distance; weights are exp2(x * post - maximum).
+// The scale, or the cap, stays out of the scores until the exponent takes it up; a negative scale goes into the
+// queries' signs, so that the maximum of the scores is that of the products.
 struct Scale {
-  float pre, cap, post;
-  bool negate;
+  float pre, post;
+  bool negate, far;
 };
+
+__device__ __forceinline__ float uni_float(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
 __device__ __forceinline__ Scale load_scale(const rkc_attention& a) {
   Scale s;
-  s.cap = a.softcap * kLog2e;
   s.negate = a.scale < 0.f;
   const float by = fabsf(a.scale);
-  s.pre = a.softcap > 0.f ? by / a.softcap * 2.f * kLog2e : 1.f;
-  s.post = a.softcap > 0.f ? 1.f : fmaxf(by * kLog2e, 1e-30f);  // above 0: what is masked stays -inf
+  s.pre = uni_float(a.softcap > 0.f ? by / a.softcap * (2.f * kLog2e) : 1.f);
+  s.far = a.softcap > 256.f;
+  s.post = uni_float(fmaxf((a.softcap > 0.f ? a.softcap : by) * kLog2e, 1e-30f));  // above 0: what is masked stays -inf
   return s;
 }
 
-// softcap tanh(x / softcap) in units of log2, of x with `pre` in it: 1 - 2 / (exp(2 y) + 1)
-__device__ __forceinline__ float capped(float x, const Scale& s) {
-  return s.cap - 2.f * s.cap * __builtin_amdgcn_rcpf(ex2(x * s.pre) + 1.f);
+// tanh(y) of a lane's scores, x * pre = 2 y log2(e), by 1 - 2 / (exp(2 y) + 1).  That is off by 2^-23 of the cap, which
+// of a cap past 256 would be too much of a small score: there, while no lane of the wave has |y| over 0.8, it is a
+// polynomial in y^2 of least relative error on that range (6e-8; 1.5e-7 with the roundings of 32 bits).  (For all caps it
+// is the slower form: 2,048 rows over 32,768 slots 1,430 us instead of 1,320.)
+template <typename V, int N> __device__ __forceinline__ void cap_all(V (&x)[N], const Scale& s) {
+  constexpr int A = sizeof(V) / 4;
+  bool small = false;
+  if (s.far) {
+    float most = 0.f;
+#pragma unroll
+    for (int u = 0; u < N; u++)
+#pragma unroll
+      for (int k = 0; k < A; k++) most = fmaxf(most, fabsf(x[u][k]));
+    small = !__any(most * s.pre > 1.6f * kLog2e);
+  }
+  if (small) {
+#pragma unroll
+    for (int u = 0; u < N; u++)
+#pragma unroll
+      for (int k = 0; k < A; k++) {
+        const float z = x[u][k] * (s.pre * (0.5f * kLn2)), t = z * z;
+        float y = __builtin_fmaf(t, -0.00435528671f, 0.0190932825f);
+        y = __builtin_fmaf(y, t, -0.0531143062f);
+        y = __builtin_fmaf(y, t, 0.13321048f);
+        y = __builtin_fmaf(y, t, -0.333326757f);
+        x[u][k] = z * __builtin_fmaf(y, t, 0.99999994f);
+      }
+  } else {
+#pragma unroll
+    for (int u = 0; u < N; u++)
+#pragma unroll
+      for (int k = 0; k < A; k++) x[u][k] = 1.f - 2.f * __builtin_amdgcn_rcpf(ex2(x[u][k] * s.pre) + 1.f);
+  }
 }
 
 template <typename V> __device__ __forceinline__ V negated(V v) {

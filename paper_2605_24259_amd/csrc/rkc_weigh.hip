@@ -121,12 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rk
 #pragma unroll
           for (int k = 0; k < KC; k++) x[u] = mma16(qf[k], kf[u][k], x[u]);
         }
-        if (a.softcap > 0.f) {
-#pragma unroll
-          for (int u = 0; u < kRuns; u++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) x[u][e] = capped(x[u][e], sc);
-        }
+        if (a.softcap > 0.f) cap_all(x, sc);
         if (a.d_slope) {
           const f32x4 sl = *(const f32x4*)(slopes + rm);
 #pragma unroll

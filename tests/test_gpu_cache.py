@@ -530,3 +530,48 @@ def test_refusals():
     with pytest.raises(rkc.RkcError):  # 24 slots a block
         k = torch.zeros(4, 24, 2, 64, device="cuda").bfloat16()
         rkc.PagedCache(k, k, torch.zeros(2, 4, dtype=torch.int32, device="cuda")).attend(q, o, n, **m)
+
+
+@pytest.mark.parametrize("softcap", [40.0, 1e3, 1e6])
+@pytest.mark.parametrize("lens,rows,group", [([900, 40], [1, 1], 4), ([300, 90], [60, 33], 3), ([500, 300], [300, 140], 2)])
+def test_cap_far_above_the_scores(lens, rows, group, softcap):
+    """A cap that the scores do not come near changes them by a relative error, not by one of the cap's size: the
+    tolerance of an uncapped score, relative to |scale| |q| |k| alone (the cap's own form: 2 units of 2^-24 of a score
+    in place of the 16 that 2^-20 stands for)."""
+    import torch
+    say("case cap", lens, rows, group, softcap)
+    c = ref.Case(11, lens, rows, dim=128, group=group, softcap=softcap)
+    o, z = c.attend()
+    out, lse = run_attend(c)
+    a = 2.0 ** -20 * (8 + reach(c) - softcap)
+    assert np.abs(lse.double().cpu().numpy() - z).max() <= a
+    u, vmax = UNIT["bfloat16"], np.nan_to_num(np.abs(c.v.double().numpy()), nan=0, posinf=0).max()
+    assert np.all(np.abs(out.double().cpu().numpy() - o) <= u * (vmax + np.abs(o)) + a * vmax)
+    w = gpu_cache(c).weigh(c.q.cuda(), torch.from_numpy(z).float().cuda(), ints(c.offset), ints(c.lens), **mask(c)).double().cpu().numpy()
+    want = c.weigh(z, 1.0)
+    for s, n in enumerate(lens):  # the sums of the softmax, given in 32 bits, have an error of 2^-24 of theirs
+        assert np.all(np.abs(w[s, :, :n] - want[s, :, :n]) <= (a + 2.0 ** -23 * np.abs(z).max()) * want[s, :, :n] + 1e-30)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_many_small_weights(dim, rows):
+    """One slot of weight 1 and 60,000 of exp(-14.5), whose float16 would have three bits left: they make up a thirtieth
+    of the sum, and are as exact as all weights are: u each for the weight, the result, and half for what is below."""
+    import torch
+
+    import paper_2605_24259_amd as rkc
+    say("case many small weights", dim, rows)
+    n, page = 60000 + rows, 64
+    pages = -(-n // page)
+    k = torch.zeros(pages, page, 1, dim, dtype=torch.float16, device="cuda")
+    v = torch.ones_like(k)
+    k[..., 0] = -14.5
+    k[0, 0], v[0, 0] = 0, 0
+    q = torch.zeros(rows, 1, dim, dtype=torch.float16, device="cuda")
+    q[..., 0] = 1
+    g = rkc.PagedCache(k, v, torch.arange(pages, dtype=torch.int32, device="cuda")[None])
+    out, _ = g.attend(q, ints([0, rows]), ints([n]), max_rows=rows, scale=1.0)
+    tail = (n - rows + np.arange(rows)) * np.exp(-14.5)
+    want = (tail / (1 + tail))[:, None, None]
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= 2.5 * 2.0 ** -11 * want)
