@@ -379,8 +379,8 @@ template <typename V> __device__ __forceinline__ V negated(V v) {
 rkc_status rkc_cache_check(const rkc_cache* c);
 rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool weigh);
 
-// Entry of the two attention kernels: one for up to 32 packed rows (rows x query heads of a key/value head) of a
-// sequence, one for tiles of 128; chunk: slots per workgroup, splits: workgroups along a sequence.
+// Entry of the two attention kernels: one for up to 16 packed rows (rows x query heads of a key/value head) of a
+// sequence, one for tiles of 128 or 256; chunk: slots per workgroup, splits: workgroups along a sequence.
 struct rkc_plan {
   bool few;
   int units;   // sequences x key/value heads x row tiles

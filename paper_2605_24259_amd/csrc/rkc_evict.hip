@@ -1,6 +1,7 @@
 // rkc_evict.hip -- eviction from a paged cache by the account of its slots.
 //
-// One workgroup decides for a head of a sequence: the account of the last slot to be kept is found 8 bits of its
+// Kept are the protected first slots, recent ones, and of the others those of the largest account.  One workgroup decides
+// for a head of a sequence of up to 16,384 slots, one for each tile of that many in longer ones (evict_round): the account of the last slot to be kept is found 8 bits of its
 // 32-bit order at a time, by counts of the digits in LDS (whole numbers: their order does not matter); ties go to the
 // lowest slots, and prefix sums pair the gaps in front of the new end with the kept slots behind it.  A second kernel moves their
 // keys and values.  Sources lie behind the new end and targets before it, so that the moves need no order among
@@ -194,7 +195,9 @@ __device__ __forceinline__ void list_moves(const evict_args& g, int row, const H
   }
 }
 
-// Sequences of at most one tile: one workgroup decides for a head.
+// Sequences of at most one tile: one workgroup decides for a head, whose accounts stay in its registers: one read of
+// them, four counts of a digit.  Bound by latency and by the LDS additions of the counts: 13 us for 8 heads of up to 1,280
+// slots, 26 us for 256 of 5,000 to 16,384.  (A copy of the counts for each lane left no room for as many waves: 39 us.)
 __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
   // counts of 256 digits, a copy for each of 16 lanes: at most 4 lanes of an addition meet in a word, whatever the digits
   __shared__ __attribute__((aligned(16))) uint32_t hist[256 * kCopies];
@@ -276,7 +279,8 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
 }
 
 // Longer sequences: a workgroup for each tile of a head, and a launch for each step, which reads what the tiles of the
-// step before wrote.  Rounds 0, 1 and 2 count 11, 11 and 10 bits of the order; round 3 tallies each tile (ties, those of
+// step before wrote, as one workgroup would take a tile after the other (8 heads of 65,536 slots 145 us a call instead of
+// 78).  Rounds 0, 1 and 2 count 11, 11 and 10 bits of the order; round 3 tallies each tile (ties, those of
 // them before the new end, kept slots without ties before and behind it); round 4 lists and writes.
 template <int ROUND>
 __global__ __launch_bounds__(kThreads) void evict_round(const evict_args g) {
@@ -426,7 +430,8 @@ __global__ __launch_bounds__(kThreads) void evict_round(const evict_args g) {
   list_moves(g, row, x, t, keep, table, gap0, from0, nullptr);
 }
 
-// Moves the keys and values of up to kMoves slots of a head of a sequence, 16 bytes a lane.
+// Moves the keys and values of up to kMoves slots of a head of a sequence, 16 bytes a lane.  Bound by the copy: 256 heads
+// of 5,000 to 16,384 slots of 128 elements down to half move 0.69 GB in 158 us, 4.4 TB/s read and written.
 __global__ __launch_bounds__(256) void evict_move(const evict_args g, int chunks) {
   const rkc_cache& c = g.c;
   const int row = blockIdx.x / chunks, first = blockIdx.x % chunks * kMoves, n = min(g.count[row] - first, kMoves);
