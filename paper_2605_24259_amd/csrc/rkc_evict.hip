@@ -76,20 +76,21 @@ __device__ __forceinline__ Head load_head(const evict_args& g, int row) {
   return x;
 }
 
-// A tile of a head's slots: a thread has slots tid, tid + 1024, ... of it.
-struct Tile {
+// A tile of a head's slots, of a workgroup of N threads: a thread has slots tid, tid + N, ... of it.
+template <int N> struct Tile {
+  static constexpr int kSlots = N * kItems;
   float wt[kItems];
   int ps[kItems];
   uint32_t open, recent;  // bit i: slot i of the thread is behind the protected ones; is recent
   int base;
-  __device__ __forceinline__ int slot(int i) const { return base + i * kThreads + (int)threadIdx.x; }
+  __device__ __forceinline__ int slot(int i) const { return base + i * N + (int)threadIdx.x; }
   __device__ __forceinline__ void load(const Head& x, int tile) {
-    base = tile * kTile, open = recent = 0;
+    base = tile * kSlots, open = recent = 0;
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
       const int j = slot(i);
       wt[i] = 0.f, ps[i] = j;
-      if (base + i * kThreads >= x.len) continue;
+      if (base + i * N >= x.len) continue;
       if (j < x.len) {
         wt[i] = x.w[j];
         if (x.pos) ps[i] = x.pos[j];
@@ -97,7 +98,7 @@ struct Tile {
     }
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
-      if (base + i * kThreads >= x.len) continue;
+      if (base + i * N >= x.len) continue;
       const int j = slot(i);
       const bool in = j >= x.held && j < x.len;
       open |= (in ? 1u : 0u) << i;
@@ -110,7 +111,7 @@ struct Tile {
     keep = among_recent ? 0 : recent, tie = 0;
 #pragma unroll
     for (int i = 0; i < kItems; i++) {
-      if (base + i * kThreads >= x.len) continue;
+      if (base + i * N >= x.len) continue;
       const uint32_t key = order_of(wt[i]);
       if (slot(i) < x.held) keep |= 1u << i;
       if (any && (in >> i & 1)) {
@@ -122,50 +123,50 @@ struct Tile {
 };
 
 // Counts of runs of 64 slots (of two kinds), then what lies before each in the tile; the last entry: the tile's.
-typedef uint32_t Runs[2][kItems * kWaves + 1];
-__device__ __forceinline__ void runs_before(Runs& table) {
-  constexpr int N = kItems * kWaves / 64;
+template <int N> struct Runs { uint32_t n[2][kItems * N / 64 + 1]; };
+template <int N> __device__ __forceinline__ void runs_before(Runs<N>& table) {
+  constexpr int kRuns = kItems * N / 64, K = kRuns / 64;
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   __syncthreads();
   if (wave < 2) {
-    uint32_t x[N], sum = 0;
+    uint32_t x[K], sum = 0;
 #pragma unroll
-    for (int k = 0; k < N; k++) x[k] = sum, sum += table[wave][lane * N + k];
+    for (int k = 0; k < K; k++) x[k] = sum, sum += table.n[wave][lane * K + k];
     const uint32_t to = wave_scan(sum);
 #pragma unroll
-    for (int k = 0; k < N; k++) table[wave][lane * N + k] = to - sum + x[k];
-    if (lane == 63) table[wave][kItems * kWaves] = to;
+    for (int k = 0; k < K; k++) table.n[wave][lane * K + k] = to - sum + x[k];
+    if (lane == 63) table.n[wave][kRuns] = to;
   }
   __syncthreads();
 }
 
 // The lowest `left` of a tile's ties stay.
-__device__ __forceinline__ void keep_ties(Runs& table, uint32_t tie, uint32_t left, uint32_t& keep) {
+template <int N> __device__ __forceinline__ void keep_ties(Runs<N>& table, uint32_t tie, uint32_t left, uint32_t& keep) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
 #pragma unroll
   for (int i = 0; i < kItems; i++) {
     const uint64_t m = __ballot(tie >> i & 1);
-    if (lane == 0) table[0][i * kWaves + wave] = __popcll(m), table[1][i * kWaves + wave] = 0;
+    if (lane == 0) table.n[0][i * (N / 64) + wave] = __popcll(m), table.n[1][i * (N / 64) + wave] = 0;
   }
   runs_before(table);
 #pragma unroll
   for (int i = 0; i < kItems; i++) {
     const uint64_t m = __ballot(tie >> i & 1);
-    if ((tie >> i & 1) && table[0][i * kWaves + wave] + lower(m) < left) keep |= 1u << i;
+    if ((tie >> i & 1) && table.n[0][i * (N / 64) + wave] + lower(m) < left) keep |= 1u << i;
   }
   __syncthreads();
 }
 
 // Lists a tile's gaps before the new end and its kept slots behind it, from places gap0 and from0 on, and writes what
 // stays; gap_at, if given: the gaps of the only tile.
-__device__ __forceinline__ void list_moves(const evict_args& g, int row, const Head& x, const Tile& t, uint32_t keep, Runs& table, int gap0, int from0, uint16_t* gap_at) {
+template <int N> __device__ __forceinline__ void list_moves(const evict_args& g, int row, const Head& x, const Tile<N>& t, uint32_t keep, Runs<N>& table, int gap0, int from0, uint16_t* gap_at) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
 #pragma unroll
   for (int i = 0; i < kItems; i++) {
     const int j = t.slot(i);
     const bool kept = keep >> i & 1;
     const uint64_t gap = __ballot(j < x.now && !kept), src = __ballot(j >= x.now && j < x.len && kept);
-    if (lane == 0) table[0][i * kWaves + wave] = __popcll(gap), table[1][i * kWaves + wave] = __popcll(src);
+    if (lane == 0) table.n[0][i * (N / 64) + wave] = __popcll(gap), table.n[1][i * (N / 64) + wave] = __popcll(src);
   }
   runs_before(table);
   int32_t* gaps = g.gaps + (int64_t)row * g.most;
@@ -173,9 +174,9 @@ __device__ __forceinline__ void list_moves(const evict_args& g, int row, const H
 #pragma unroll
   for (int i = 0; i < kItems; i++) {
     const int j = t.slot(i);
-    if (t.base + i * kThreads >= x.now) continue;
+    if (t.base + i * N >= x.now) continue;
     const bool kept = keep >> i & 1, is_gap = j < x.now && !kept;
-    const int at = gap0 + table[0][i * kWaves + wave] + lower(__ballot(is_gap));
+    const int at = gap0 + table.n[0][i * (N / 64) + wave] + lower(__ballot(is_gap));
     if (is_gap) gaps[at] = j;
     if (is_gap && gap_at) gap_at[at] = (uint16_t)j;
     if (j < x.now && kept) x.w_out[j] = t.wt[i], x.pos_out[j] = t.ps[i];
@@ -184,9 +185,9 @@ __device__ __forceinline__ void list_moves(const evict_args& g, int row, const H
 #pragma unroll
   for (int i = 0; i < kItems; i++) {
     const int j = t.slot(i);
-    if (t.base + i * kThreads >= x.len) continue;
+    if (t.base + i * N >= x.len) continue;
     const bool is_src = j >= x.now && j < x.len && (keep >> i & 1);
-    const int at = from0 + table[1][i * kWaves + wave] + lower(__ballot(is_src));
+    const int at = from0 + table.n[1][i * (N / 64) + wave] + lower(__ballot(is_src));
     if (is_src) from[at] = j;
     if (is_src && gap_at) {
       const int to = gap_at[at];
@@ -196,14 +197,16 @@ __device__ __forceinline__ void list_moves(const evict_args& g, int row, const H
 }
 
 // Sequences of at most one tile: one workgroup decides for a head, whose accounts stay in its registers: one read of
-// them, four counts of a digit.  Bound by latency and by the LDS additions of the counts: 13 us for 8 heads of up to 1,280
-// slots, 26 us for 256 of 5,000 to 16,384.  (A copy of the counts for each lane left no room for as many waves: 39 us.)
-__global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
+// them, up to four counts of a digit.  Four waves where the sequences are of up to 4,096 slots, as barriers of sixteen
+// cost more than they save (8 heads of up to 1,280 slots: 9.1 us instead of 13.6).  Bound by latency and by the LDS
+// additions of the counts: 26 us for 256 heads of 5,000 to 16,384.  (A copy of the counts for each lane left no room for
+// as many waves: 39 us.)
+template <int N> __global__ __launch_bounds__(N) void evict_choose(const evict_args g) {
   // counts of 256 digits, a copy for each of 16 lanes: at most 4 lanes of an addition meet in a word, whatever the digits
   __shared__ __attribute__((aligned(16))) uint32_t hist[256 * kCopies];
   uint16_t* const gap_at = (uint16_t*)hist;  // later: the gaps, at most half of the slots
-  static_assert(sizeof(hist) >= kTile / 2 * sizeof(uint16_t), "gaps");
-  __shared__ Runs table;
+  static_assert(sizeof(hist) >= N * kItems / 2 * sizeof(uint16_t), "gaps");
+  __shared__ Runs<N> table;
   __shared__ uint32_t found[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const Head x = load_head(g, blockIdx.x);
@@ -216,11 +219,11 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
   }
   if (tid == 0 && x.h == 0) g.e.d_length_out[x.s] = x.now;
   if (x.now == x.len) {
-    for (int j = tid; j < x.len; j += kThreads) x.w_out[j] = x.w[j], x.pos_out[j] = x.pos_at(j);
+    for (int j = tid; j < x.len; j += N) x.w_out[j] = x.w[j], x.pos_out[j] = x.pos_at(j);
     if (tid == 0) g.count[blockIdx.x] = 0;
     return;
   }
-  Tile t;
+  Tile<N> t;
   t.load(x, 0);
   int K = x.now - x.held;  // to be kept of the slots behind the protected ones
   bool among_recent = false;  // the choice is among the recent ones; else they stay, and it is among the others
@@ -239,22 +242,32 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
   uint32_t T = 0, left = K, same = 0;
   const uint32_t in = among_recent ? t.recent : t.open & ~t.recent;
   if (K > 0) {
+#pragma unroll
     for (int b = 24; b >= 0; b -= 8) {
-      ((u32x4*)hist)[tid] = u32x4{0, 0, 0, 0};
+      // all of them are: lower bits do not matter (few slots: 9.1 us instead of 11.8; many seldom end early, 27.8 for 26.4)
+      if (N == 256 && left == same) break;
+      for (int k = tid; k < 256 * kCopies / 4; k += N) ((u32x4*)hist)[k] = u32x4{0, 0, 0, 0};
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kItems; i++) {
-        if (i * kThreads >= x.len) continue;
+        if (i * N >= x.len) continue;
         const uint32_t key = order_of(t.wt[i]);
         if ((in >> i & 1) && (b == 24 || (key ^ T) >> b >> 8 == 0)) atomicAdd(&hist[(key >> b & 255) * kCopies + (lane & (kCopies - 1))], 1u);
       }
       __syncthreads();
-      const u32x4 x4 = ((const u32x4*)hist)[tid];  // a quarter of a digit's copies
-      uint32_t n = x4[0] + x4[1] + x4[2] + x4[3];
-      n += (uint32_t)dpp<0xb1>((int)n);  // quad_perm [1,0,3,2]
-      n += (uint32_t)dpp<0x4e>((int)n);  // quad_perm [2,3,0,1]
+      constexpr int Q = 1024 / N;
+      uint32_t n[Q];
+#pragma unroll
+      for (int k = 0; k < Q; k++) {
+        const u32x4 x4 = ((const u32x4*)hist)[k * N + tid];  // a quarter of a digit's copies
+        n[k] = x4[0] + x4[1] + x4[2] + x4[3];
+        n[k] += (uint32_t)dpp<0xb1>((int)n[k]);  // quad_perm [1,0,3,2]
+        n[k] += (uint32_t)dpp<0x4e>((int)n[k]);  // quad_perm [2,3,0,1]
+      }
       __syncthreads();
-      if ((tid & 3) == 0) hist[tid >> 2] = n;
+#pragma unroll
+      for (int k = 0; k < Q; k++)
+        if ((tid & 3) == 0) hist[k * (N / 4) + (tid >> 2)] = n[k];
       __syncthreads();
       if (wave == 0) {  // lane l: digits 255 - 4 l and the three below
         const u32x4 y = ((const u32x4*)hist)[63 - lane];
@@ -271,11 +284,11 @@ __global__ __launch_bounds__(kThreads) void evict_choose(const evict_args g) {
     }
   }
   uint32_t keep, tie;
-  t.judge(x, among_recent, K > 0, T, keep, tie);
-  if (left == same) keep |= tie;
-  else keep_ties(table, tie, left, keep);
+  const bool all = left == same;  // then T itself is to be kept: orders are above 0
+  t.judge(x, among_recent, K > 0, all && T ? T - 1 : T, keep, tie);
+  if (!all) keep_ties(table, tie, left, keep);
   list_moves(g, blockIdx.x, x, t, keep, table, 0, 0, gap_at);
-  if (tid == 0) g.count[blockIdx.x] = table[0][kItems * kWaves];
+  if (tid == 0) g.count[blockIdx.x] = table.n[0][kItems * N / 64];
 }
 
 // Longer sequences: a workgroup for each tile of a head, and a launch for each step, which reads what the tiles of the
@@ -286,7 +299,7 @@ template <int ROUND>
 __global__ __launch_bounds__(kThreads) void evict_round(const evict_args g) {
   constexpr int kShift[5] = {21, 10, 0, 0, 0};
   __shared__ __attribute__((aligned(16))) uint32_t hist[2 * kBins];
-  __shared__ Runs table;
+  __shared__ Runs<kThreads> table;
   __shared__ uint32_t sums[kWaves], found[3], told[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int row = blockIdx.x / g.parts, part = blockIdx.x % g.parts;
@@ -302,7 +315,7 @@ __global__ __launch_bounds__(kThreads) void evict_round(const evict_args g) {
   }
   if (part >= tiles) return;
   if (ROUND == 0 && part == 0 && tid == 0 && x.h == 0) g.e.d_length_out[x.s] = x.now;
-  Tile t;
+  Tile<kThreads> t;
   if (x.now == x.len) {  // nothing goes
     if (ROUND == 4) {
       t.load(x, part);
@@ -520,8 +533,10 @@ rkc_status rkc_evict(const rkc_cache* c, const rkc_eviction* e, void* stream) {
   if ((int64_t)rows * (chunks + 1) > 0x7fffffff) return RKC_E_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   const dim3 block(kThreads), one((unsigned)rows), tiles((unsigned)(rows * g.parts));
-  if (g.parts == 1) {
-    evict_choose<<<one, block, 0, s>>>(g);
+  if (e->max_len <= 256 * kItems) {
+    evict_choose<256><<<one, dim3(256), 0, s>>>(g);
+  } else if (g.parts == 1) {
+    evict_choose<kThreads><<<one, block, 0, s>>>(g);
   } else {
     evict_round<0><<<tiles, block, 0, s>>>(g);
     evict_round<1><<<tiles, block, 0, s>>>(g);
