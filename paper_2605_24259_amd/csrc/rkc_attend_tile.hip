@@ -243,6 +243,15 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
     int buf = 0;
     for (int i = 0; i < n_tiles; i++) {
       const int t0 = slot_of(i);
+      if constexpr (W == 4) {
+        // of a CU's workgroups those that have most left go first (2 prompts of 4,096 tokens, 16 heads of 64 elements: 122 us
+        // instead of 132)
+        const int left = n_tiles - i;
+        if (left >= 24) __builtin_amdgcn_s_setprio(3);
+        else if (left >= 16) __builtin_amdgcn_s_setprio(2);
+        else if (left >= 8) __builtin_amdgcn_s_setprio(1);
+        else __builtin_amdgcn_s_setprio(0);
+      }
       if (i + kAhead <= n_tiles) dma_barrier<2 * P * (kAhead - 1)>();
       else dma_barrier<0>();
       if (i + kAhead < n_tiles) load(i + kAhead, buf ? buf - 1 : kAhead);
