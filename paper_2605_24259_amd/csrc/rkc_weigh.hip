@@ -4,8 +4,9 @@
 // 16x16x32 products, with those of its next 32 on their way, and goes over the packed rows, whose queries lie in
 // LDS, 16 at a time; a lane adds up the weights of its slot's column in 32 bits, in a fixed order.  One read of the
 // keys; no atomics.  What bounds it: the read of the keys, with the products, and an exponential for every row and
-// slot in between (32 rows of 32 heads on each of 8 sequences of 6,000 to 16,384 slots, 8 heads of 128 elements:
-// 60 us, 3.6 TB/s, 440 TFLOP/s).
+// slot in between (32 rows of 32 heads, 8 heads of 128 elements: 32 sequences of 8,192 slots 146 us, 3.9 TB/s,
+// 470 TFLOP/s; 8 of 6,000 to 16,384 60 us, 3.6 TB/s).  Four workgroups a CU hide the latency between those: with the lines
+// of trees always in LDS there was room for three, 178 us instead of 146.
 #include "rkc_cache_dev.h"
 
 namespace {
@@ -13,20 +14,22 @@ namespace {
 constexpr int kThreads = 256, kRuns = 2, kSlots = 16 * kRuns, kTurn = kThreads / 64 * kSlots;
 constexpr int kBlock = 128;  // packed rows whose queries, masks and sums lie in LDS at a time
 static_assert(kThreads == RKC_MAX_TREE_ROWS, "tree_lines");
+constexpr int kTreeBytes = RKC_MAX_TREE_ROWS * 36;  // lines and depths
 
 struct RowIn {
   int start, end, pos, line;
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rkc_attention a, int chunks, int turns) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 2 : 4) void weigh(const rkc_cache c, const rkc_attention a, int chunks, int turns) {
   typedef typename Vec8<T>::t V8;
   constexpr int KC = D / 32;
   __shared__ __attribute__((aligned(16))) T rows_q[kBlock * D];
   __shared__ __attribute__((aligned(16))) float lse2[kBlock], slopes[kBlock];
   __shared__ RowIn in[kBlock];
-  __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
-  __shared__ int depths[RKC_MAX_TREE_ROWS];
+  extern __shared__ __attribute__((aligned(16))) char of_trees[];  // kTreeBytes where there are trees
+  uint64_t(*const lines)[4] = (uint64_t(*)[4])of_trees;
+  int* const depths = (int*)(of_trees + RKC_MAX_TREE_ROWS * 32);
 
   const int H = c.kv_heads, G = a.q_heads / H;
   const int h = blockIdx.x % H, part = blockIdx.x / H % chunks, s = blockIdx.x / (H * chunks);
@@ -173,19 +176,20 @@ __global__ __launch_bounds__(kThreads, 2) void weigh(const rkc_cache c, const rk
 
 template <typename T>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, hipStream_t s) {
-  // A workgroup keeps its queries for as many turns as leave three workgroups a CU, at most for one turn per 8 packed
+  // A workgroup keeps its queries for as many turns as leave four workgroups a CU, at most for one turn per 8 packed
   // rows: few rows are staged quickly, and short turns even out sequences of unlike length.
   const int64_t all = (int64_t)c->n_seqs * c->kv_heads * ((a->max_len + kTurn - 1) / kTurn);
   const int64_t most = (int64_t)a->max_rows * (a->q_heads / c->kv_heads) / 8;
-  int64_t turns = all / (3 * 256);
+  int64_t turns = all / (4 * 256);
   turns = turns > most ? most : turns;
   turns = turns > 16 ? 16 : turns < 2 ? 2 : turns;
   const int chunks = (int)((a->max_len + turns * kTurn - 1) / (turns * kTurn));
   if ((int64_t)c->n_seqs * c->kv_heads * chunks > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  const int lds = a->d_parent ? kTreeBytes : 0;
   const dim3 grid(c->n_seqs * c->kv_heads * chunks), block(kThreads);
-  if (c->head_dim == 64) weigh<T, 64><<<grid, block, 0, s>>>(*c, *a, chunks, (int)turns);
-  else if (c->head_dim == 128) weigh<T, 128><<<grid, block, 0, s>>>(*c, *a, chunks, (int)turns);
-  else weigh<T, 256><<<grid, block, 0, s>>>(*c, *a, chunks, (int)turns);
+  if (c->head_dim == 64) weigh<T, 64><<<grid, block, lds, s>>>(*c, *a, chunks, (int)turns);
+  else if (c->head_dim == 128) weigh<T, 128><<<grid, block, lds, s>>>(*c, *a, chunks, (int)turns);
+  else weigh<T, 256><<<grid, block, lds, s>>>(*c, *a, chunks, (int)turns);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
