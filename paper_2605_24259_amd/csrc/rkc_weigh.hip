@@ -1,12 +1,12 @@
 // rkc_weigh.hip -- the account of a cache: how much attention each of its slots received.
 //
-// weight_j = decay * before_j + sum over rows of exp(x_j - lse).  Softmax sums are given, so slots are independent: a wave holds the keys of 32 slots in registers as columns of
-// 16x16x32 products, with those of its next 32 on their way, and goes over the packed rows, whose queries lie in
-// LDS, 16 at a time; a lane adds up the weights of its slot's column in 32 bits, in a fixed order.  One read of the
-// keys; no atomics.  What bounds it: the read of the keys, with the products, and an exponential for every row and
-// slot in between (32 rows of 32 heads, 8 heads of 128 elements: 32 sequences of 8,192 slots 146 us, 3.9 TB/s,
-// 470 TFLOP/s; 8 of 6,000 to 16,384 60 us, 3.6 TB/s).  Four workgroups a CU hide the latency between those: with the lines
-// of trees always in LDS there was room for three, 178 us instead of 146.
+// weight_j = decay * before_j + sum over rows of exp(x_j - lse).  Softmax sums are given, so slots are independent: a
+// wave holds the keys of 32 slots in registers as columns of 16x16x32 products, with those of its next 32 on their way,
+// and goes over the packed rows, whose queries lie in LDS, 16 at a time; a lane adds up the weights of its slot's column
+// in 32 bits, in a fixed order.  One read of the keys; no atomics.  What bounds it: the read of the keys, with the
+// products and an exponential for every row and slot in between (32 rows of 32 heads, 8 heads of 128 elements: 32
+// sequences of 8,192 slots 146 us, 3.9 TB/s, 470 TFLOP/s; 8 of 6,000 to 16,384 60 us, 3.6 TB/s).  Four workgroups a CU
+// hide the latency between those: with the lines of trees always in LDS there was room for three, 178 us instead of 146.
 #include "rkc_cache_dev.h"
 
 namespace {
