@@ -4,43 +4,49 @@
 namespace {
 
 // Joins the chunks of a packed row: with m the largest of their maxima m_k, out = sum_k 2^(m_k - m) o_k / sum_k
-// 2^(m_k - m) l_k.  A workgroup for each row, D / 4 lanes for a chunk, as many chunks at a time as that leaves room for, so
-// that few rows of many chunks are read by many lanes at once.  Latency bounds it: 7 us for 64 sequences of up to 4,096
-// slots, 13 us for 5 of 262,144.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_join(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
-  constexpr int L = D / 4, N = 256 / L;
+// 2^(m_k - m) l_k.  D / 4 lanes read a chunk's output, and `groups` of so many lanes share a row's chunks, which join_plan
+// chooses: with few rows of many chunks many, as latency bounds it (5 rows of 32 heads in 64 chunks: 8.7 us), with many rows
+// one, where the reads do (24,900 rows of 64 elements in 3 chunks: 7.3 us, 41 with a workgroup for each row).
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(NT) void attend_join(const rkc_cache c, const rkc_attention a, const rkc_plan pl, int groups) {
+  constexpr int L = D / 4, N = NT / L;
   __shared__ __attribute__((aligned(16))) float part_o[N][D];
   __shared__ float part_l[N];
   const int H = c.kv_heads, G = a.q_heads / H, per = a.max_rows * G;
-  const int m = blockIdx.x % per, unit = blockIdx.x / per, s = unit / H, h = unit % H;
-  const int lane = threadIdx.x & 63, group = threadIdx.x / L, d = threadIdx.x % L * 4;
+  const int group = threadIdx.x / L, lane = threadIdx.x % L, d = lane * 4, mine = group % groups;
+  const int64_t id = (int64_t)blockIdx.x * (N / groups) + group / groups;
+  const int m = (int)(id % per), s = (int)min(id / per / H, (int64_t)c.n_seqs - 1), h = (int)(id / per % H);
   const Seq q = load_seq(c, a, s);
-  if (!q.ok || m >= q.n * G) return;
-  const int qt = m / pl.rows, last = (min(q.n * G, (qt + 1) * pl.rows) - 1) / G;
-  const int n = max(1, (rows_end(a, q, s, last) + pl.chunk - 1) / pl.chunk);
-  const int64_t at = ((int64_t)unit * pl.tiles + qt) * pl.splits * pl.rows + m % pl.rows;
-  const float* st = (const float*)((const char*)a.d_scratch + pl.stat_at) + at * 2;
-  const float* part = (const float*)((const char*)a.d_scratch + pl.part_at) + at * D + d;
-  float top = -kInf;
-  for (int k = lane; k < n; k += 64) top = fmaxf(top, st[(int64_t)k * pl.rows * 2]);
-  for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  float sum = 0.f;
+  const bool row_here = id < (int64_t)c.n_seqs * H * per && q.ok && m < q.n * G;
+  float top = -kInf, sum = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (row_here) {
+    const int qt = m / pl.rows, last = (min(q.n * G, (qt + 1) * pl.rows) - 1) / G;
+    const int n = max(1, (rows_end(a, q, s, last) + pl.chunk - 1) / pl.chunk);
+    const int64_t at = ((int64_t)(s * H + h) * pl.tiles + qt) * pl.splits * pl.rows + m % pl.rows;
+    const float* st = (const float*)((const char*)a.d_scratch + pl.stat_at) + at * 2;
+    const float* part = (const float*)((const char*)a.d_scratch + pl.part_at) + at * D + d;
+    for (int k = lane; k < n; k += L) top = fmaxf(top, st[(int64_t)k * pl.rows * 2]);
+#pragma unroll
+    for (int x = L / 2; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
 #pragma unroll 4
-  for (int k = group; k < n; k += N) {
-    const float m_k = st[(int64_t)k * pl.rows * 2], l_k = st[(int64_t)k * pl.rows * 2 + 1];
-    const f32x4 x = *(const f32x4*)(part + (int64_t)k * pl.rows * D);
-    if (l_k != 0.f) {  // a chunk of which the row sees anything
-      const float by = ex2(m_k - top);
-      sum += l_k * by, o += x * by;
+    for (int k = mine; k < n; k += groups) {
+      const float m_k = st[(int64_t)k * pl.rows * 2], l_k = st[(int64_t)k * pl.rows * 2 + 1];
+      const f32x4 x = *(const f32x4*)(part + (int64_t)k * pl.rows * D);
+      if (l_k != 0.f) {  // a chunk of which the row sees anything
+        const float by = ex2(m_k - top);
+        sum += l_k * by, o += x * by;
+      }
     }
   }
-  *(f32x4*)&part_o[group][d] = o;
-  if (d == 0) part_l[group] = sum;
-  __syncthreads();
-  if (group) return;
-  for (int k = 1; k < N && k < n; k++) o += *(const f32x4*)&part_o[k][d], sum += part_l[k];
+  if (groups > 1) {
+    *(f32x4*)&part_o[group][d] = o;
+    if (d == 0) part_l[group] = sum;
+    __syncthreads();
+    if (mine) return;
+    for (int k = 1; k < groups; k++) o += *(const f32x4*)&part_o[group + k][d], sum += part_l[group + k];
+  }
+  if (!row_here) return;
   const float by = sum == 0.f ? 0.f : 1.f / sum;
   const int64_t row = q.row0 + m / G, qh = h * G + m % G;
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -82,13 +88,26 @@ __global__ __launch_bounds__(256) void attend_account(const rkc_cache c, const r
   }
 }
 
+// Groups of lanes for a row: as many as leave each two chunks, until the card's 256 CUs have 1,024 lanes each.
+template <typename T, int D>
+rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  constexpr int L = D / 4;
+  const int64_t rows = (int64_t)c->n_seqs * c->kv_heads * a->max_rows * (a->q_heads / c->kv_heads);
+  int groups = 1;
+  while (groups < 1024 / L && groups * 4 <= p->splits && rows * L * groups < 256 * 1024) groups *= 2;
+  if (groups <= 256 / L) {
+    const int64_t each = 256 / L / groups;
+    attend_join<T, D, 256><<<dim3((unsigned)((rows + each - 1) / each)), dim3(256), 0, s>>>(*c, *a, *p, groups);
+  } else {
+    const int64_t each = 1024 / L / groups;
+    attend_join<T, D, 1024><<<dim3((unsigned)((rows + each - 1) / each)), dim3(1024), 0, s>>>(*c, *a, *p, groups);
+  }
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
 template <typename T>
 rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)c->n_seqs * c->kv_heads * a->max_rows * (a->q_heads / c->kv_heads))), block(256);
-  if (c->head_dim == 64) attend_join<T, 64><<<grid, block, 0, s>>>(*c, *a, *p);
-  else if (c->head_dim == 128) attend_join<T, 128><<<grid, block, 0, s>>>(*c, *a, *p);
-  else attend_join<T, 256><<<grid, block, 0, s>>>(*c, *a, *p);
-  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+  return c->head_dim == 64 ? join<T, 64>(c, a, p, s) : c->head_dim == 128 ? join<T, 128>(c, a, p, s) : join<T, 256>(c, a, p, s);
 }
 
 bool off16(const void* p) { return (uintptr_t)p & 15; }
