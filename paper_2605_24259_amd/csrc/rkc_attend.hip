@@ -4,7 +4,7 @@
 namespace {
 
 // Joins the chunks of a packed row: with m the largest of their maxima m_k, out = sum_k 2^(m_k - m) o_k / sum_k
-// 2^(m_k - m) l_k.  D / 4 lanes read a chunk's output, and `groups` of so many lanes share a row's chunks, which join_plan
+// 2^(m_k - m) l_k.  D / 4 lanes read a chunk's output, and `groups` of so many lanes share a row's chunks, which `join`
 // chooses: with few rows of many chunks many, as latency bounds it (5 rows of 32 heads in 64 chunks: 8.7 us), with many rows
 // one, where the reads do (24,900 rows of 64 elements in 3 chunks: 7.3 us, 41 with a workgroup for each row).
 template <typename T, int D, int NT>
@@ -169,7 +169,11 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   rkc_plan p = {};
   const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
   p.few = M <= 16;
-  p.rows = p.few ? 16 : M <= 128 || c->head_dim != 128 ? 128 : 256;
+  // 256 rows only where such tiles, counted with 256 slots each, are twice the card's CUs: fewer leave CUs idle and are slower
+  // from start to end (8 heads of 128 elements, 512 rows of 32 heads over 1,024 slots: 39.9 us, with 128 rows 35.0; over
+  // 8,192 90.2 and 98.6).
+  const int64_t wide = (int64_t)c->n_seqs * c->kv_heads * ((M + 255) / 256) * ((a->max_len + 255) / 256);
+  p.rows = p.few ? 16 : M <= 128 || c->head_dim != 128 || wide < 512 ? 128 : 256;
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
@@ -178,6 +182,10 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;
   if (chunk < grain) chunk = grain;
+  // Up to 512 slots the join, a second launch, costs more than shorter chunks save (512 rows of 32 heads of 128 elements:
+  // 20.8 us whole, 28.4 in two chunks; 40 of 64 over 300 slots 12.2 and 16.6), but for a few workgroups that go through 256
+  // elements a head (8 rows over 512 slots: 25.7 and 16.6; 512 rows 32.3 and 41.9).
+  if (!p.few && a->max_len <= 512 && (c->head_dim < 256 || units >= 32)) chunk = 512;
   // Short sequences whole, by eight waves: no second kernel for the join (four sequences of up to 80 slots: 10.6 us in one
   // kernel where the split took 6.0 and the join 4.4, and 12.9 us a call instead of 16.8).
   p.waves = p.few && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
