@@ -177,11 +177,17 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
-  const int64_t want = p.few ? 10 * 256 : c->head_dim == 256 || p.rows == 256 ? 256 : 2 * 256, grain = p.few || c->head_dim == 256 ? 128 : 256;
+  // Workgroups wanted: where one is all that a CU holds (256 elements a head, 256 rows), one a CU; of few rows ten, two at a
+  // time, as they even out unlike lengths (64 sequences of 1 to 4,096 slots: 122 us, with five 126, with three 141).
+  const bool wide_head = c->head_dim == 256;
+  const int64_t want = wide_head || p.rows == 256 ? 256 : p.few ? 10 * 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;  // workgroups along a sequence
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;
-  if (chunk < grain) chunk = grain;
+  // Of few rows no less than four tiles a wave, else starts and joins cost more than they save (one sequence of 32,768
+  // slots, 8 heads: 31 us, with one tile 42).
+  const int64_t least = p.few && !wide_head ? 512 : grain;
+  if (chunk < least) chunk = least;
   // Up to 512 slots the join, a second launch, costs more than shorter chunks save (512 rows of 32 heads of 128 elements:
   // 20.8 us whole, 28.4 in two chunks; 40 of 64 over 300 slots 12.2 and 16.6), but for a few workgroups that go through 256
   // elements a head (8 rows over 512 slots: 25.7 and 16.6; 512 rows 32.3 and 41.9).
