@@ -32,7 +32,8 @@ enum rkc_dtype { RKC_BF16 = 0, RKC_F16 = 1 };
 enum rkc_cache_status {
   RKC_CS_LENGTH = 1, /* length or row count outside its limits, or more rows than slots: the sequence is
                         left out and its outputs are not written                                        */
-  RKC_CS_BLOCK = 2,  /* a block id outside [0, n_blocks): block 0 was taken instead                 */
+  RKC_CS_BLOCK = 2,  /* a block id outside [0, n_blocks): block 0 was read instead; rkc_evict leaves out
+                        the moves into or out of such a block                                           */
   RKC_CS_PARENT = 4  /* a parent that is not -1 or an earlier row of its sequence: -1 was taken     */
 };
 

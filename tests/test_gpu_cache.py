@@ -421,6 +421,35 @@ def test_evict_leaves_shared_blocks_alone():
     assert not torch.equal(k[1], k0[1])
 
 
+@pytest.mark.parametrize("size,wrong", [(64, 3), (64, 1), (17000, 1), (17000, 700)])
+def test_evict_leaves_out_moves_of_blocks_that_are_not_there(size, wrong):
+    """A block id outside the pool: block 0, another sequence's, stays as it is, as do all but the sequence's other gaps."""
+    import torch
+
+    import paper_2605_24259_amd as rkc
+    say("case evict wrong block", size, wrong)
+    pages = -(-size // 16)
+    k = torch.randn(pages + 1, 16, 1, 64, device="cuda").bfloat16()
+    v = torch.randn_like(k)
+    table = torch.arange(1, pages + 1, dtype=torch.int32, device="cuda")[None].contiguous()
+    table[0, wrong] = 1 << 30
+    g = rkc.PagedCache(k, v, table)
+    k0, v0 = k.clone(), v.clone()
+    w = torch.arange(pages * 16, dtype=torch.float32, device="cuda").view(1, 1, -1).contiguous()  # the last half stays
+    length, wo, _ = g.evict(w, ints([size]), ints([size // 2]))
+    new = size // 2
+    assert length.tolist() == [new] and g.status.tolist() == [rkc.cache.CS_BLOCK]
+    assert torch.equal(wo[0, 0, :new], w[0, 0, size - new:size])
+    for x, x0 in ((k, k0), (v, v0)):
+        want = x0.clone()
+        flat, flat0 = want[1:].view(-1, 1, 64), x0[1:].view(-1, 1, 64)
+        to = torch.arange(new, device="cuda")
+        at = to + size - new
+        fine = (to // 16 != wrong) & (at // 16 != wrong)
+        flat[to[fine]] = flat0[at[fine]]
+        assert torch.equal(x, want)
+
+
 # ------------------------------------------------------------------------------------------------------------
 def test_other_streams_and_repeated_calls():
     """On a side stream behind work of its own; every call gives the same bits."""
