@@ -14,6 +14,9 @@
  * enqueues kernels on the stream, and a negative status means that nothing was enqueued.  What the host cannot
  * see (lengths, offsets, block ids and parents in device memory) is checked on the device: nothing outside the
  * buffers is read or written, and RKC_CS_* bits are OR'ed into the sequence's word of d_status.
+ *
+ * Strides of what a call writes (outputs, accounts, and K and V where slots are evicted) may put the dimensions in any
+ * order but must keep elements apart: strides of zero, as of a broadcast tensor, are for what is only read.
  */
 #ifndef RKC_CACHE_H
 #define RKC_CACHE_H
@@ -114,7 +117,7 @@ typedef struct rkc_eviction {
   const int32_t* d_pos;         /* the same, or NULL: a slot's position is its number                */
   float* d_weight_out;          /* the same, not d_weight                                            */
   int32_t* d_pos_out;           /* the same, not d_pos                                               */
-  int32_t* d_length_out;        /* [n_seqs], not d_length                                            */
+  int32_t* d_length_out;        /* [n_seqs], none of the four above                                  */
   void* d_scratch;              /* >= rkc_evict_scratch_bytes, 256-byte aligned                      */
   size_t scratch_bytes;
 } rkc_eviction;

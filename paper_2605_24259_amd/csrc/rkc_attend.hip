@@ -1,6 +1,8 @@
 // rkc_attend.hip -- C ABI of the attention over a paged cache: checks, choice of kernel, join of the chunks.
 #include "rkc_cache_dev.h"
 
+#include <utility>
+
 namespace {
 
 // Joins the chunks of a packed row: with m the largest of their maxima m_k, out = sum_k 2^(m_k - m) o_k / sum_k
@@ -118,6 +120,19 @@ constexpr int64_t kFar = (int64_t)1 << 40;  // strides between blocks and rows: 
 
 }  // namespace
 
+bool rkc_shared(int64_t width, int64_t n0, int64_t stride0, int64_t n1, int64_t stride1, int64_t n2, int64_t stride2) {
+  struct { int64_t n, stride; } d[3] = {{n0, stride0}, {n1, stride1}, {n2, stride2}};
+  if (d[0].stride > d[1].stride) std::swap(d[0], d[1]);
+  if (d[1].stride > d[2].stride) std::swap(d[1], d[2]);
+  if (d[0].stride > d[1].stride) std::swap(d[0], d[1]);
+  for (auto& x : d) {  // from the nearest on: each step goes past all that the nearer ones reach
+    if (x.n <= 1) continue;  // its stride says nothing
+    if (x.stride < width) return true;
+    width += (x.n - 1) * x.stride;
+  }
+  return false;
+}
+
 rkc_status rkc_cache_check(const rkc_cache* c) {
   if (!c) return RKC_E_NULL;
   if (c->n_seqs < 0 || c->n_blocks < 0 || c->max_pages < 0 || c->reserved) return RKC_E_RANGE;
@@ -157,6 +172,8 @@ rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool 
   for (const void* p : {(const void*)a->d_row_offset, (const void*)a->d_length, (const void*)a->d_row_start, (const void*)a->d_prefix,
                         (const void*)a->d_parent, (const void*)a->d_slope, (const void*)a->d_lse, (const void*)a->d_weight_in, (const void*)a->d_weight})
     if (off4(p)) return RKC_E_ALIGN;
+  if (!weigh && rkc_shared(c->head_dim, a->n_rows, a->out_row_stride, a->q_heads, a->out_head_stride)) return RKC_E_RANGE;
+  if (a->d_weight && rkc_shared(a->max_len, c->n_seqs, a->weight_seq_stride, c->kv_heads, a->weight_head_stride)) return RKC_E_RANGE;
   return RKC_OK;
 }
 

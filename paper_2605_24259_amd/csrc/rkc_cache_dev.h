@@ -377,6 +377,9 @@ template <typename V> __device__ __forceinline__ V negated(V v) {
 
 // Host side: what every call checks.
 rkc_status rkc_cache_check(const rkc_cache* c);
+// Whether rows of `width` elements that lie apart by three strides, of so many each, share elements: what is written
+// must not.
+bool rkc_shared(int64_t width, int64_t n0, int64_t stride0, int64_t n1, int64_t stride1, int64_t n2 = 1, int64_t stride2 = 0);
 rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool weigh);
 
 // Entry of the two attention kernels: one for up to 16 packed rows (rows x query heads of a key/value head) of a

@@ -524,7 +524,13 @@ rkc_status rkc_evict(const rkc_cache* c, const rkc_eviction* e, void* stream) {
                         (const void*)e->d_weight, (const void*)e->d_pos, (const void*)e->d_weight_out, (const void*)e->d_pos_out,
                         (const void*)e->d_length_out})
     if ((uintptr_t)p & 3) return RKC_E_ALIGN;
-  if (e->d_weight_out == e->d_weight || e->d_pos_out == e->d_pos || e->d_length_out == e->d_length) return RKC_E_RANGE;
+  if (e->d_weight_out == e->d_weight || e->d_pos_out == e->d_pos) return RKC_E_RANGE;
+  for (const int32_t* p : {e->d_length, e->d_budget, e->d_protect, e->d_recent_from})
+    if (e->d_length_out == p) return RKC_E_RANGE;
+  if (rkc_shared(e->max_len, c->n_seqs, e->weight_seq_stride, c->kv_heads, e->weight_head_stride)) return RKC_E_RANGE;
+  if (rkc_shared(c->head_dim, c->n_blocks, c->k_block_stride, c->page_tokens, c->k_slot_stride, c->kv_heads, c->k_head_stride) ||
+      rkc_shared(c->head_dim, c->n_blocks, c->v_block_stride, c->page_tokens, c->v_slot_stride, c->kv_heads, c->v_head_stride))
+    return RKC_E_RANGE;
   const size_t need = rkc_evict_scratch_bytes(c, e);
   if (!e->d_scratch || e->scratch_bytes < need) return RKC_E_SCRATCH;
   if ((uintptr_t)e->d_scratch & 255) return RKC_E_ALIGN;

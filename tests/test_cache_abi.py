@@ -153,3 +153,38 @@ def test_scratch_is_bounded(lib):
         a.max_rows, a.max_len = rows, length
         n = lib.rkc_attend_scratch_bytes(ctypes.byref(c), ctypes.byref(a))
         assert n <= 256 * 4 * (1 << 20), (rows, length, n)
+
+
+@pytest.mark.parametrize("name,what,fault", [
+    ("rkc_attend", "a", dict(out_row_stride=0)), ("rkc_attend", "a", dict(out_head_stride=0)), ("rkc_attend", "a", dict(out_head_stride=120)),
+    ("rkc_attend", "a", dict(out_row_stride=512)), ("rkc_attend", "a", dict(weight_seq_stride=0)),
+    ("rkc_weigh", "a", dict(weight_head_stride=0)), ("rkc_weigh", "a", dict(weight_seq_stride=1024)), ("rkc_weigh", "a", dict(weight_head_stride=1000)),
+    ("rkc_evict", "e", dict(weight_seq_stride=0)), ("rkc_evict", "e", dict(weight_head_stride=8)), ("rkc_evict", "c", dict(k_head_stride=0)),
+    ("rkc_evict", "c", dict(v_block_stride=0)), ("rkc_evict", "c", dict(v_slot_stride=128)), ("rkc_evict", "e", dict(d_length_out=0xb0000)),
+    ("rkc_evict", "e", dict(d_protect=0xf0000)), ("rkc_evict", "e", dict(d_recent_from=0xf0000))])
+def test_outputs_keep_apart(lib, name, what, fault):
+    """Elements that share memory are refused where a call writes them (-3); else the next thing wrong is the scratch."""
+    c, a, e = structs()
+    a.d_weight = 0x300000
+    c.max_pages, a.max_len = 64, 1024
+    x = e if name == "rkc_evict" else a
+    for k, v in fault.items():
+        setattr(dict(c=c, a=a, e=e)[what], k, v)
+    assert call(lib, name, c, x) == -3
+
+
+def test_orders_of_dimensions_keep_apart(lib):
+    """Any order of the dimensions is fine, and so is the stride of a dimension of one; keys that are only read may be
+    shared by the heads (the scratch is what is refused)."""
+    c, a, e = structs()
+    e.weight_seq_stride, e.weight_head_stride = 1024, 4096
+    c.k_head_stride, c.k_block_stride, c.k_slot_stride = 300 * 16 * 128, 16 * 128, 128
+    assert call(lib, "rkc_evict", c, e) == -5
+    c.max_pages, a.max_len = 256, 4096
+    a.out_row_stride, a.out_head_stride, c.k_head_stride = 128, 512, 0
+    assert call(lib, "rkc_attend", c, a) == -5
+    c.n_seqs = c.kv_heads = 1
+    e.weight_seq_stride = e.weight_head_stride = 0
+    c.v_head_stride = c.k_head_stride = 0
+    c.max_pages = 64
+    assert call(lib, "rkc_evict", c, e) == -5
