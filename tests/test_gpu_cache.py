@@ -503,6 +503,24 @@ def test_in_a_graph():
             assert torch.equal(a.nan_to_num(7), b.nan_to_num(7))
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim,rows", [(64, 1), (128, 5), (256, 3)])
+@pytest.mark.parametrize("n", [700, 5000])
+def test_weights_of_few_rows_keep_their_bits(dtype, dim, rows, n):
+    """Up to 16 packed rows: weights are the sum of two numbers of the type, whose error is u^2 in place of u, and for
+    float16 at least half a step of 2^-24 of weights whose sum is at least 2^-2; what is left of u is the result's rounding."""
+    say("case weights of few rows", dtype, dim, rows, n)
+    c = ref.Case(dim + rows + n, [n, n // 3], [rows] * 2, group=3, dim=dim, dtype=dtype)
+    g = gpu_cache(c)
+    out, lse = g.attend(c.q.cuda(), ints(c.offset), ints(c.lens), **mask(c))
+    want, z = c.attend()
+    got, u = out.double().cpu().numpy(), UNIT[dtype]
+    most = float(np.nan_to_num(c.v.double().numpy(), nan=0, posinf=0, neginf=0).__abs__().max())
+    few = n * 2.0 ** -23 if dtype == "float16" else 0
+    near = u * np.abs(want) + (2 * u * u + 2.0 ** -20 * (8 + reach(c)) + few) * most
+    assert (np.abs(got - want) <= near).all()
+
+
 def test_what_only_the_device_sees_is_flagged():
     """Bad lengths, row counts, block ids and parents: nothing outside the buffers is touched, the status says so and
     the other sequences are as always."""
