@@ -199,7 +199,7 @@ template <int N> __device__ __forceinline__ void list_moves(const evict_args& g,
 // Sequences of at most one tile: one workgroup decides for a head, whose accounts stay in its registers: one read of
 // them, up to four counts of a digit.  Four waves where the sequences are of up to 4,096 slots, as barriers of sixteen
 // cost more than they save (8 heads of up to 1,280 slots: 9.1 us instead of 13.6).  Bound by latency and by the LDS
-// additions of the counts: 26 us for 256 heads of 5,000 to 16,384.  (A copy of the counts for each lane left no room for
+// additions of the counts: 27 to 30 us for 256 heads of 5,000 to 16,384.  (A copy of the counts for each lane left no room for
 // as many waves: 39 us.)
 template <int N> __global__ __launch_bounds__(N) void evict_choose(const evict_args g) {
   // counts of 256 digits, a copy for each of 16 lanes: at most 4 lanes of an addition meet in a word, whatever the digits
