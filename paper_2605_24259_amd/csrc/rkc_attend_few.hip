@@ -15,6 +15,7 @@
 // anyway: outputs are as near to the formula's as with weights in 32 bits (4 sequences of up to 1,280 slots in float16:
 // 4.8e-5, with rounded weights alone up to 1.5 times as far), at the same time (898 us of 5 long ones, 899 without).
 #include "rkc_cache_dev.h"
+#include "rkc_tiles.h"
 
 namespace {
 
@@ -104,14 +105,9 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
 #pragma unroll
   for (int d = 0; d < DB; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // The tiles of 32 slots that any row sees, in order: from c0 on, less those between the prefix and the first document.
-  const int end_up = c0 + (max(0, end - c0) + 31) / 32 * 32;
-  const int gap_from = min(max((all_pre + 31) / 32 * 32, c0), end_up), gap_to = min(max(any_from / 32 * 32, gap_from), end_up);
-  const int n_tiles = (end_up - c0 - (gap_to - gap_from)) / 32;
-  auto slot_of = [&](int i) {
-    const int t = c0 + i * 32;
-    return t >= gap_from ? t + (gap_to - gap_from) : t;
-  };
+  const rkc_tiles<32> tiles(c0, end, all_pre, any_from);
+  const int n_tiles = tiles.n;
+  auto slot_of = [&](int i) { return tiles.slot(i); };
   V8 kf[2][KC];
   u32x4 vf[VP];
   bool bad = false;

@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "rkc_cache_dev.h"
+#include "rkc_tiles.h"
 
 namespace {
 
@@ -99,14 +100,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
 #pragma unroll
     for (int k = 0; k < A; k++) o[d][k] = 0.f;
 
-  // The tiles that any row sees, in order: from c0 on, less those between the prefix and the first document.
-  const int end_up = c0 + (max(0, end - c0) + BK - 1) / BK * BK;
-  const int gap_from = min(max((pre + BK - 1) / BK * BK, c0), end_up), gap_to = min(max(g_any_from / BK * BK, gap_from), end_up);
-  const int n_tiles = (end_up - c0 - (gap_to - gap_from)) / BK;
-  auto slot_of = [&](int i) {
-    const int t = c0 + i * BK;
-    return t >= gap_from ? t + (gap_to - gap_from) : t;
-  };
+  const rkc_tiles<BK> tiles(c0, end, pre, g_any_from);
+  const int n_tiles = tiles.n;
+  auto slot_of = [&](int i) { return tiles.slot(i); };
   bool bad = false;
   // this thread's pieces of a tile: a wave's pieces of one load lie in 16 slots of one page
   const int lane_run = uni(tid / CH & ~15);
@@ -234,12 +230,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   auto go_over = [&](auto with_care) {
     constexpr bool careful = decltype(with_care)::value;
     // kAhead tiles are on their way while one is worked on
-    look_up(0);
-#pragma unroll
-    for (int i = 0; i < kAhead; i++) {
-      if (i < n_tiles) load(i, i);
-      if (i + 1 < n_tiles) look_up(i + 1);
-    }
+    rkc_first_tiles<kAhead>(n_tiles, look_up, load);
     int buf = 0;
     for (int i = 0; i < n_tiles; i++) {
       const int t0 = slot_of(i);
@@ -321,12 +312,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   auto in_turns = [&] {
     static_assert(W != 8 || kAhead == 3, "four places");
     const bool behind = wave >= 4;
-    look_up(0);
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-      if (i < n_tiles) load(i, i);
-      if (i + 1 < n_tiles) look_up(i + 1);
-    }
+    rkc_first_tiles<2>(n_tiles, look_up, load);
     auto even = [&](int i) {
       if (i + 1 < n_tiles) dma_barrier<2 * P>();
       else dma_barrier<0>();
