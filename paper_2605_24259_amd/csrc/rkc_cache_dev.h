@@ -207,6 +207,7 @@ __device__ __forceinline__ void flag(const rkc_cache& c, int s, int bit) {
 __device__ __forceinline__ Row load_row(const rkc_attention& a, const Seq& q, int s, int i) {
   Row r;
   r.start = a.d_row_start ? max(0, a.d_row_start[q.row0 + i]) : 0;
+  if (a.d_parent) r.start = min(r.start, q.base);  // drafted slots are seen by `line` alone, also behind a later start
   r.end = a.d_parent ? q.base : q.base + i + 1;
   r.prefix = a.d_prefix ? max(0, min(word(a.d_prefix, s), a.d_parent ? q.base : q.len)) : 0;
   r.pos = q.base + i;

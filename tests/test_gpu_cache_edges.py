@@ -5,7 +5,7 @@ import pytest
 
 from tests import cache_reference as ref
 from tests.gpu_util import say
-from tests.test_gpu_cache import check_attend, run_attend
+from tests.test_gpu_cache import bush, check_attend, check_weigh, gpu_cache, ints, mask, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +26,32 @@ def test_row_tiles_of_padding_alone(dtype, dim, kv_heads, group, lens, rows, see
     check_attend(c, out, lse)
     seen = np.tile(np.arange(rows) < seeing, len(lens))
     assert np.isneginf(lse.cpu().numpy()[~seen]).all() and (out.cpu()[~seen] == 0).all() and lse.cpu()[seen].isfinite().all()
+
+
+@pytest.mark.parametrize("prefix", [False, True])
+@pytest.mark.parametrize("late", [1, "rows", NEVER])
+@pytest.mark.parametrize("dim,group,rows", [(64, 2, 3), (128, 4, 4), (256, 1, 9), (64, 1, 40), (64, 2, 70), (128, 3, 90), (256, 2, 70)])
+def test_trees_that_start_past_their_base(prefix, late, dim, group, rows):
+    """A tree's rows see their own slot and their ancestors' wherever row_start lies: past the base it takes the history away
+    and nothing else.  For all rows of one sequence, for the first 32 packed rows of another, which fill a wave, and
+    in long sequences that are cut."""
+    say("case late trees", prefix, late, dim, group, rows)
+    long = 1600 if rows * group <= 16 else 700
+    lens, ns, start, first = [rows + 20, rows + 75, rows + long, rows], [rows] * 4, [], max(1, 32 // group)
+    for s, n in enumerate(lens):
+        base = n - rows
+        past = base + 1 if late == 1 else base + rows if late == "rows" else NEVER
+        start += [past if s != 1 or i < first else 10 for i in range(rows)]
+    c = ref.Case(rows + dim, lens, ns, kv_heads=2, group=group, dim=dim, dtype="float16" if prefix else "bfloat16", parent=sum((bush(rows, s) for s in range(4)), []),
+                 row_start=start, prefix=[7, 40, 100, 0] if prefix else None, bias=dim == 128)
+    want = c.attend()
+    assert np.isfinite(want[1]).all()
+    out, lse = run_attend(c)
+    check_attend(c, out, lse, want)
+    g, w = gpu_cache(c), c.weight.cuda()
+    q, o, n = c.q.cuda(), ints(c.offset), ints(c.lens)
+    check_weigh(c, g.weigh(q, lse, o, n, weight=w, decay=0.5, **mask(c, max_len=max(lens))), lse, 0.5, c.weight)
+    out, lse, got = g.attend(q, o, n, weight=w, decay=0.5, **mask(c, max_len=max(lens)))
+    check_attend(c, out, lse, want)
+    check_weigh(c, got, lse, 0.5, c.weight)
+    assert not g.status.any().item()
