@@ -138,108 +138,122 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attend_few(cons
   const int put_at = 2 * vals16_at<D>(lane / (D / 8), lane % (D / 8));
   const int val_at = 2 * (vals16_at<D>(quad * 4 + (col >> 2), (col & 3) >> 1) + (col & 1) * 4);
 
-  int i = wave;
-  if (i < n_tiles) {
-    look_up(i);
-    load(i);
-    if (i + kWaves < n_tiles) look_up(i + kWaves);
-  }
-  for (; i < n_tiles; i += kWaves) {
-    const int t0 = slot_of(i);
-    f32x4 sc[2];
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-      sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KC; k++) sc[u] = mma16(kf[u][k], qf[k], sc[u]);
+  // A tile that all rows see is multiplied as it is.  An infinity in it would meet the rest of a weight, which may be zero or
+  // negative, and come out as NaN: an output that is not finite has the wave go over its tiles once more, all looked through.
+  for (bool careful = false;; careful = true) {
+    int i = wave;
+    if (i < n_tiles) {
+      look_up(i);
+      load(i);
+      if (i + kWaves < n_tiles) look_up(i + kWaves);
     }
-    const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
-    bool hurt = false;
-    const int pa = here(put_at), va = here(val_at);
-    auto put = [&](int p, u32x4 x) { *(u32x4*)((char*)tile + ((pa ^ vals16_x<D>(p * RP) << 4) + p * RP * 2 * D)) = x; };
-    if (whole) {
+    for (; i < n_tiles; i += kWaves) {
+      const int t0 = slot_of(i);
+      f32x4 sc[2];
 #pragma unroll
-      for (int p = 0; p < VP; p++) put(p, vf[p]);
-    } else {
+      for (int u = 0; u < 2; u++) {
+        sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int p = 0; p < VP; p++) {
-        const int j = t0 + p * RP + lane / (D / 8);
-        u32x4 x = vf[p];
-        if (j >= end || (j < any_from && j >= all_pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
-        hurt |= any_hurt<T>(x);
-        put(p, x);
+        for (int k = 0; k < KC; k++) sc[u] = mma16(kf[u][k], qf[k], sc[u]);
       }
-      hurt = __any(hurt);
-    }
-    uint32_t seen = 0xffffffff;
-    if (a.softcap > 0.f) cap_all(sc, f);
-    if (a.d_slope) {
-      const float far = (float)(here(row.pos - t0) - quad * 4);
+      const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
+      bool hurt = false;
+      const int pa = here(put_at), va = here(val_at);
+      auto put = [&](int p, u32x4 x) { *(u32x4*)((char*)tile + ((pa ^ vals16_x<D>(p * RP) << 4) + p * RP * 2 * D)) = x; };
+      if (whole && !careful) {
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        float gap = far - (float)(16 * (e >> 2) + (e & 3));
-        if (a.d_parent && t0 + 32 > q.base) {
-          const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
-          gap = at >= 0 ? (float)(row.pos - q.base - d) : gap;
+        for (int p = 0; p < VP; p++) put(p, vf[p]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < VP; p++) {
+          const int j = t0 + p * RP + lane / (D / 8);
+          u32x4 x = vf[p];
+          if (j >= end || (j < any_from && j >= all_pre)) x = u32x4{0, 0, 0, 0};  // no row sees it
+          hurt |= any_hurt<T>(x);
+          put(p, x);
         }
-        sc[e >> 2][e & 3] = __builtin_fmaf(-slope, fabsf(gap), sc[e >> 2][e & 3]);
+        hurt = __any(hurt);
       }
-    }
-    if (!whole) {
-      const int from = t0 - q.base;
-      const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line >> from : line << -from;
-      seen = seen_of(row, t0, drafted) >> 4 * quad;
+      uint32_t seen = 0xffffffff;
+      if (a.softcap > 0.f) cap_all(sc, f);
+      if (a.d_slope) {
+        const float far = (float)(here(row.pos - t0) - quad * 4);
 #pragma unroll
-      for (int e = 0; e < 8; e++) sc[e >> 2][e & 3] = masked(sc[e >> 2][e & 3], seen, 16 * (e >> 2) + (e & 3));
-    }
-    auto vals = [&](int d) { return read_tr2<T>((const char*)tile + (va ^ d << 5), (const char*)tile + (va ^ d << 5) + 32 * D); };
-    if (pl.keep) {
-      float* to = (float*)((char*)a.d_scratch + pl.score_at) + (int64_t)(s * H + h) * (a.max_rows * G) * pl.wide + (int64_t)t0 * (a.max_rows * G) + 32 * col + quad * 4;
-      if (col < M) *(f32x4*)to = sc[0] * f.post, *(f32x4*)(to + 16) = sc[1] * f.post;
-    }
-    if (i + kWaves < n_tiles) {
-      load(i + kWaves);
-      if (i + 2 * kWaves < n_tiles) look_up(i + 2 * kWaves);
-    }
-    float most = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-    most = max32(max16(most)) * f.post;
-    // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
-    if (__any(most > top + (8.f + kRoom<T>))) {
-      const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
-      top = now, sum *= by;
+        for (int e = 0; e < 8; e++) {
+          float gap = far - (float)(16 * (e >> 2) + (e & 3));
+          if (a.d_parent && t0 + 32 > q.base) {
+            const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
+            gap = at >= 0 ? (float)(row.pos - q.base - d) : gap;
+          }
+          sc[e >> 2][e & 3] = __builtin_fmaf(-slope, fabsf(gap), sc[e >> 2][e & 3]);
+        }
+      }
+      if (!whole) {
+        const int from = t0 - q.base;
+        const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line >> from : line << -from;
+        seen = seen_of(row, t0, drafted) >> 4 * quad;
 #pragma unroll
-      for (int d = 0; d < DB; d++) o[d] *= by;
-    }
-    const float m = top == -kInf ? 0.f : top;
-    f32x8 p;
+        for (int e = 0; e < 8; e++) sc[e >> 2][e & 3] = masked(sc[e >> 2][e & 3], seen, 16 * (e >> 2) + (e & 3));
+      }
+      auto vals = [&](int d) { return read_tr2<T>((const char*)tile + (va ^ d << 5), (const char*)tile + (va ^ d << 5) + 32 * D); };
+      if (pl.keep) {
+        float* to = (float*)((char*)a.d_scratch + pl.score_at) + (int64_t)(s * H + h) * (a.max_rows * G) * pl.wide + (int64_t)t0 * (a.max_rows * G) + 32 * col + quad * 4;
+        if (col < M) *(f32x4*)to = sc[0] * f.post, *(f32x4*)(to + 16) = sc[1] * f.post;
+      }
+      if (i + kWaves < n_tiles) {
+        load(i + kWaves);
+        if (i + 2 * kWaves < n_tiles) look_up(i + 2 * kWaves);
+      }
+      float most = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                         fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      most = max32(max16(most)) * f.post;
+      // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+      if (__any(most > top + (8.f + kRoom<T>))) {
+        const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
+        top = now, sum *= by;
 #pragma unroll
-    for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[e >> 2][e & 3], f.post, -m));
-    sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    // the products' operands have the cache's type: a weight is the sum of two of them, with at least twice its bits
-    const V8 pb = __builtin_convertvector(p, V8), pr = __builtin_convertvector(p - __builtin_convertvector(pb, f32x8), V8);
-    if (hurt) {
-      V8 by;
+        for (int d = 0; d < DB; d++) o[d] *= by;
+      }
+      const float m = top == -kInf ? 0.f : top;
+      f32x8 p;
 #pragma unroll
-      for (int e = 0; e < 8; e++) by[e] = (T)(seen >> (16 * (e >> 2) + (e & 3)) & 1 ? 1.f : 0.f);
+      for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[e >> 2][e & 3], f.post, -m));
+      sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      // the products' operands have the cache's type: a weight is the sum of two of them, with at least twice its bits
+      const V8 pb = __builtin_convertvector(p, V8), pr = __builtin_convertvector(p - __builtin_convertvector(pb, f32x8), V8);
+      if (hurt) {
+        V8 by;
+#pragma unroll
+        for (int e = 0; e < 8; e++) by[e] = (T)(seen >> (16 * (e >> 2) + (e & 3)) & 1 ? 1.f : 0.f);
+#pragma unroll
+        for (int d = 0; d < DB; d++) {
+          V8 vt = vals(d);
+          const f32x4 n = mma16(strip<T>(vt), by, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int k = 0; k < 4; k++) o[d][k] += hurt_by(n[k]);
+        }
+        for (int k = lane; k < kTile / 8; k += 64) {
+          V8 v = *(const V8*)(tile + 8 * k);
+          strip<T>(v);
+          *(V8*)(tile + 8 * k) = v;
+        }
+      }
 #pragma unroll
       for (int d = 0; d < DB; d++) {
-        V8 vt = vals(d);
-        const f32x4 n = mma16(strip<T>(vt), by, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-        for (int k = 0; k < 4; k++) o[d][k] += hurt_by(n[k]);
-      }
-      for (int k = lane; k < kTile / 8; k += 64) {
-        V8 v = *(const V8*)(tile + 8 * k);
-        strip<T>(v);
-        *(V8*)(tile + 8 * k) = v;
+        const V8 vt = vals(d);
+        o[d] = mma16(vt, pr, mma16(vt, pb, o[d]));
       }
     }
+    if (careful) break;
+    float odd = 0.f;  // stays 0 unless an output is not finite
 #pragma unroll
-    for (int d = 0; d < DB; d++) {
-      const V8 vt = vals(d);
-      o[d] = mma16(vt, pr, mma16(vt, pb, o[d]));
-    }
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+      for (int k = 0; k < 4; k++) odd = __builtin_fmaf(o[d][k], 0.f, odd);
+    if (!__any(odd != 0.f)) break;
+    top = -kInf, sum = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
   if (bad) flag(c, s, RKC_CS_BLOCK);

@@ -55,3 +55,32 @@ def test_trees_that_start_past_their_base(prefix, late, dim, group, rows):
     check_attend(c, out, lse, want)
     check_weigh(c, got, lse, 0.5, c.weight)
     assert not g.status.any().item()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim,group,rows,lens", [(64, 3, 1, [200, 1700]), (128, 4, 1, [131, 2000]), (256, 2, 1, [200, 700]),
+                                                 (128, 2, 6, [200, 1800]), (64, 2, 40, [300, 900]), (128, 1, 150, [400, 700])])
+def test_infinities_that_all_rows_see(dtype, dim, group, rows, lens):
+    """Infinite values, and NaN, at slots of tiles that every row sees whole: infinite outputs, of the value's sign, NaN where
+    both signs meet or a NaN is, and all other elements as always.  Each column has a slot of its own, so that what a
+    weight loses to rounding takes both signs and zero."""
+    say("case infinities", dtype, dim, group, rows, lens)
+    plain = ref.Case(dim + rows, lens, [rows] * 2, kv_heads=1, group=group, dim=dim, dtype=dtype, parent=bush(rows) * 2)
+    base, free = run_attend(plain)
+    c = ref.Case(dim + rows, lens, [rows] * 2, kv_heads=1, group=group, dim=dim, dtype=dtype, parent=bush(rows) * 2)
+
+    def put(s, slot, col, value):
+        c.v[c.table[s, slot // c.page], slot % c.page, :, col] = value
+    for s, n in enumerate(lens):
+        history = (n - rows) // 64 * 64
+        for col in range(0, dim, 2):
+            put(s, (col * 7 + 3 * s) % history, col, float("inf" if col % 4 else "-inf"))
+        put(s, 5, 8, float("inf"))  # beside a negative one
+        put(s, 9, 12, float("nan"))
+    o, z = c.attend()
+    out, lse = run_attend(c)
+    got = out.double().cpu().numpy()
+    assert np.isinf(o).sum() >= o.size // 2 - 3 * o.size // dim and np.isnan(o[..., 12]).all() and np.isnan(o[..., 8]).all()
+    check_attend(c, out, lse, (o, z))
+    import torch
+    assert torch.equal(out[..., 1::2], base[..., 1::2]) and torch.equal(lse, free)
