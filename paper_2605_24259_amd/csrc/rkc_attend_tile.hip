@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   }
   const bool tree = a.d_parent != nullptr, drafts = tree && c1 > q.base;
   if (drafts || (tree && a.d_slope)) {
-    tree_lines(c, a, q, s, split == 0 && h == 0 && qt == 0, lines, depths);
+    tree_lines(c, a, q, s, h == 0 && qt == 0, lines, depths);  // of a cut sequence, only parts that reach the tree come here
     row.pos = q.base + depths[qi];
   }
   // slots that all of the wave's rows see, and slots that any of them, and of the workgroup's, sees

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 4) void weigh(const rkc_ca
   load(0);
   const bool tree = a.d_parent != nullptr;
   const bool drafts = tree && w0 + n_turns * kTurn > q.base;
-  if (drafts || (tree && a.d_slope)) tree_lines(c, a, q, s, part == 0 && h == 0, lines, depths);
+  if (drafts || (tree && a.d_slope)) tree_lines(c, a, q, s, h == 0, lines, depths);  // only parts that reach the tree come here
   const int pre = a.d_prefix ? max(0, min(word(a.d_prefix, s), tree ? q.base : q.len)) : 0;
   const Scale sc = load_scale(a);
 

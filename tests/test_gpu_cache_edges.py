@@ -84,3 +84,31 @@ def test_infinities_that_all_rows_see(dtype, dim, group, rows, lens):
     check_attend(c, out, lse, (o, z))
     import torch
     assert torch.equal(out[..., 1::2], base[..., 1::2]) and torch.equal(lse, free)
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dim,group,rows", [(64, 1, 3), (64, 1, 40), (128, 4, 60), (256, 2, 30), (128, 4, 100)])
+def test_parents_are_flagged_where_sequences_are_cut(dim, group, rows, bias):
+    """A parent that is none is taken for -1 and told of by each call, wherever in its sequence the tree lies."""
+    import torch
+
+    import paper_2605_24259_amd as rkc
+    say("case parents", dim, group, rows, bias)
+    lens = [2000, 1990, 40 + rows, 1700]
+    c = ref.Case(dim + rows, lens, [rows] * 4, kv_heads=1, group=group, dim=dim, parent=bush(rows) * 4, bias=bias)
+    g, told = gpu_cache(c), rkc.cache.CS_PARENT
+    q, o, n, m = c.q.cuda(), ints(c.offset), ints(c.lens), mask(c, max_len=2000)
+    wrong = m["parent"].clone()
+    wrong[rows - 1], wrong[rows + 1], wrong[2 * rows + 2] = rows - 1, -2, 1 << 30
+    right = wrong.clone()
+    for at in (rows - 1, rows + 1, 2 * rows + 2):
+        right[at] = -1
+    want = g.attend(q, o, n, **dict(m, parent=right))
+    account = g.weigh(q, want[1], o, n, **dict(m, parent=right))
+    assert not g.status.any().item()
+    got = g.attend(q, o, n, **dict(m, parent=wrong))
+    assert g.status.tolist() == [told, told, told, 0]
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    g.status.zero_()
+    assert torch.equal(g.weigh(q, want[1], o, n, **dict(m, parent=wrong)), account)
+    assert g.status.tolist() == [told, told, told, 0]
