@@ -11,9 +11,11 @@
  * matters to the masks only.
  *
  * Ownership and errors are those of rkc.h: the caller owns every buffer, nothing is allocated, a call only
- * enqueues kernels on the stream, and a negative status means that nothing was enqueued.  What the host cannot
- * see (lengths, offsets, block ids and parents in device memory) is checked on the device: nothing outside the
- * buffers is read or written, and RKC_CS_* bits are OR'ed into the sequence's word of d_status.
+ * enqueues kernels on the stream, and a negative status means that nothing was enqueued (RKC_E_HIP, an error of
+ * the runtime itself: that not all was).  A call whose launches would have 2^32 lanes or more (as the account of
+ * 1,024 sequences and 8 heads with a max_len of 2^20) is RKC_E_UNSUPPORTED.  What the host cannot see (lengths,
+ * offsets, block ids and parents in device memory) is checked on the device: nothing outside the buffers is read
+ * or written, and RKC_CS_* bits are OR'ed into the sequence's word of d_status.
  *
  * Strides of what a call writes (outputs, accounts, and K and V where slots are evicted) may put the dimensions in any
  * order but must keep elements apart: strides of zero, as of a broadcast tensor, are for what is only read.

@@ -90,26 +90,36 @@ __global__ __launch_bounds__(256) void attend_account(const rkc_cache c, const r
   }
 }
 
+struct Join {
+  int groups, lanes;  // of a row, in units of D / 4 lanes; of a workgroup
+  int64_t workgroups;
+};
+
 // Groups of lanes for a row: as many as leave each two chunks, until the card's 256 CUs have 1,024 lanes each.
-template <typename T, int D>
-rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  constexpr int L = D / 4;
+Join join_plan(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p) {
+  const int L = c->head_dim / 4;
   const int64_t rows = (int64_t)c->n_seqs * c->kv_heads * a->max_rows * (a->q_heads / c->kv_heads);
-  int groups = 1;
-  while (groups < 1024 / L && groups * 4 <= p->splits && rows * L * groups < 256 * 1024) groups *= 2;
-  if (groups <= 256 / L) {
-    const int64_t each = 256 / L / groups;
-    attend_join<T, D, 256><<<dim3((unsigned)((rows + each - 1) / each)), dim3(256), 0, s>>>(*c, *a, *p, groups);
-  } else {
-    const int64_t each = 1024 / L / groups;
-    attend_join<T, D, 1024><<<dim3((unsigned)((rows + each - 1) / each)), dim3(1024), 0, s>>>(*c, *a, *p, groups);
-  }
-  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+  Join j = {1, 256, 0};
+  while (j.groups < 1024 / L && j.groups * 4 <= p->splits && rows * L * j.groups < 256 * 1024) j.groups *= 2;
+  if (j.groups > 256 / L) j.lanes = 1024;
+  const int64_t each = j.lanes / L / j.groups;
+  j.workgroups = (rows + each - 1) / each;
+  return j;
+}
+
+template <typename T, int D>
+void join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, const Join& j, hipStream_t s) {
+  const dim3 grid((unsigned)j.workgroups);
+  if (j.lanes == 256) attend_join<T, D, 256><<<grid, dim3(256), 0, s>>>(*c, *a, *p, j.groups);
+  else attend_join<T, D, 1024><<<grid, dim3(1024), 0, s>>>(*c, *a, *p, j.groups);
 }
 
 template <typename T>
-rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  return c->head_dim == 64 ? join<T, 64>(c, a, p, s) : c->head_dim == 128 ? join<T, 128>(c, a, p, s) : join<T, 256>(c, a, p, s);
+rkc_status join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, const Join& j, hipStream_t s) {
+  if (c->head_dim == 64) join<T, 64>(c, a, p, j, s);
+  else if (c->head_dim == 128) join<T, 128>(c, a, p, j, s);
+  else join<T, 256>(c, a, p, j, s);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 bool off16(const void* p) { return (uintptr_t)p & 15; }
@@ -250,17 +260,22 @@ rkc_status rkc_attend(const rkc_cache* c, const rkc_attention* a, void* stream) 
   if (a->n_rows == 0 || a->max_rows == 0) return a->d_weight ? rkc_weigh(c, a, stream) : RKC_OK;
   hipStream_t s = (hipStream_t)stream;
   const rkc_plan p = rkc_attend_plan(c, a);
-  if ((int64_t)p.units * p.splits > 0x7fffffff || (int64_t)c->n_seqs * c->kv_heads * p.tiles * p.rows > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  // rows of tiles are counted in 32 bits
+  if ((int64_t)c->n_seqs * c->kv_heads * p.tiles * p.rows > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  const Join j = join_plan(c, a, &p);
+  const int parts = (a->max_len + 1023) / 1024;
+  if (!rkc_fits((int64_t)p.units * p.splits, rkc_attend_lanes(c, &p)) || (p.splits > 1 && !rkc_fits(j.workgroups, j.lanes)) ||
+      (a->d_weight && !(p.keep ? rkc_fits((int64_t)p.units * parts, 256) : rkc_weigh_fits(c, a))))
+    return RKC_E_UNSUPPORTED;
   if (p.bytes) {
     if (!a->d_scratch || a->scratch_bytes < p.bytes) return RKC_E_SCRATCH;
     if ((uintptr_t)a->d_scratch & 255) return RKC_E_ALIGN;
   }
   rkc_status st = p.few ? rkc_attend_few(c, a, &p, s) : rkc_attend_tile(c, a, &p, s);
-  if (st == RKC_OK && p.splits > 1) st = c->dtype == RKC_BF16 ? join<__bf16>(c, a, &p, s) : join<_Float16>(c, a, &p, s);
+  if (st == RKC_OK && p.splits > 1) st = c->dtype == RKC_BF16 ? join<__bf16>(c, a, &p, j, s) : join<_Float16>(c, a, &p, j, s);
   if (st != RKC_OK || !a->d_weight) return st;
   if (!p.keep) return rkc_weigh(c, a, stream);
-  const int parts = (a->max_len + 1023) / 1024;
-  if ((int64_t)p.units * parts > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  if (!parts) return RKC_OK;  // of lengths of 0
   attend_account<<<dim3(p.units * parts), dim3(256), 0, s>>>(*c, *a, p, parts);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }

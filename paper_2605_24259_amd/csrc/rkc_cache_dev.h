@@ -382,6 +382,10 @@ rkc_status rkc_cache_check(const rkc_cache* c);
 // must not.
 bool rkc_shared(int64_t width, int64_t n0, int64_t stride0, int64_t n1, int64_t stride1, int64_t n2 = 1, int64_t stride2 = 0);
 rkc_status rkc_attention_check(const rkc_cache* c, const rkc_attention* a, bool weigh);
+// Whether so many workgroups can be launched: the runtime counts a launch's lanes in 32 bits.  Asked of every launch of a
+// call before the first one.
+inline bool rkc_fits(int64_t workgroups, int lanes) { return workgroups <= 0x7fffffff && workgroups * lanes <= 0xffffffffll; }
+bool rkc_weigh_fits(const rkc_cache* c, const rkc_attention* a);
 
 // Entry of the two attention kernels: one for up to 16 packed rows (rows x query heads of a key/value head) of a
 // sequence, one for tiles of 128 or 256; chunk: slots per workgroup, splits: workgroups along a sequence.
@@ -399,6 +403,8 @@ struct rkc_plan {
   size_t score_at;
 };
 rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a);
+// Lanes of a workgroup of the kernel that the plan takes.
+inline int rkc_attend_lanes(const rkc_cache* c, const rkc_plan* p) { return 64 * (p->few ? p->waves : p->rows == 256 || c->head_dim == 256 ? 8 : 4); }
 rkc_status rkc_attend_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 rkc_status rkc_attend_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 

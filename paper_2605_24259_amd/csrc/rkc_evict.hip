@@ -539,7 +539,7 @@ rkc_status rkc_evict(const rkc_cache* c, const rkc_eviction* e, void* stream) {
   g.c = *c, g.e = *e;
   lay_out(c, e, (char*)e->d_scratch, &g);
   const int64_t chunks = (e->max_len / 2 + kMoves - 1) / kMoves;
-  if ((int64_t)rows * (chunks + 1) > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  if (!rkc_fits((int64_t)rows * g.parts, kThreads) || !rkc_fits((int64_t)rows * chunks, 256)) return RKC_E_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   const dim3 block(kThreads), one((unsigned)rows), tiles((unsigned)(rows * g.parts));
   if (e->max_len <= 256 * kItems) {

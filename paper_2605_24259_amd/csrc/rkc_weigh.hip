@@ -174,29 +174,41 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 4) void weigh(const rkc_ca
   if (bad) flag(c, s, RKC_CS_BLOCK);
 }
 
-template <typename T>
-rkc_status go(const rkc_cache* c, const rkc_attention* a, hipStream_t s) {
-  // A workgroup keeps its queries for as many turns as leave four workgroups a CU, at most for one turn per 8 packed
-  // rows: few rows are staged quickly, and short turns even out sequences of unlike length.
-  const int64_t all = (int64_t)c->n_seqs * c->kv_heads * ((a->max_len + kTurn - 1) / kTurn);
+struct Cut {
+  int turns, chunks;
+  int64_t workgroups;
+};
+
+// A workgroup keeps its queries for as many turns as leave four workgroups a CU, at most for one turn per 8 packed
+// rows: few rows are staged quickly, and short turns even out sequences of unlike length.
+Cut cut_of(const rkc_cache* c, const rkc_attention* a) {
+  const int64_t units = (int64_t)c->n_seqs * c->kv_heads, all = units * ((a->max_len + kTurn - 1) / kTurn);
   const int64_t most = (int64_t)a->max_rows * (a->q_heads / c->kv_heads) / 8;
   int64_t turns = all / (4 * 256);
   turns = turns > most ? most : turns;
   turns = turns > 16 ? 16 : turns < 2 ? 2 : turns;
   const int chunks = (int)((a->max_len + turns * kTurn - 1) / (turns * kTurn));
-  if ((int64_t)c->n_seqs * c->kv_heads * chunks > 0x7fffffff) return RKC_E_UNSUPPORTED;
+  return {(int)turns, chunks, units * chunks};
+}
+
+template <typename T>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, hipStream_t s) {
+  const Cut cut = cut_of(c, a);
   const int lds = a->d_parent ? kTreeBytes : 0;
-  const dim3 grid(c->n_seqs * c->kv_heads * chunks), block(kThreads);
-  if (c->head_dim == 64) weigh<T, 64><<<grid, block, lds, s>>>(*c, *a, chunks, (int)turns);
-  else if (c->head_dim == 128) weigh<T, 128><<<grid, block, lds, s>>>(*c, *a, chunks, (int)turns);
-  else weigh<T, 256><<<grid, block, lds, s>>>(*c, *a, chunks, (int)turns);
+  const dim3 grid((unsigned)cut.workgroups), block(kThreads);
+  if (c->head_dim == 64) weigh<T, 64><<<grid, block, lds, s>>>(*c, *a, cut.chunks, cut.turns);
+  else if (c->head_dim == 128) weigh<T, 128><<<grid, block, lds, s>>>(*c, *a, cut.chunks, cut.turns);
+  else weigh<T, 256><<<grid, block, lds, s>>>(*c, *a, cut.chunks, cut.turns);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 }  // namespace
 
+bool rkc_weigh_fits(const rkc_cache* c, const rkc_attention* a) { return rkc_fits(cut_of(c, a).workgroups, kThreads); }
+
 extern "C" rkc_status rkc_weigh(const rkc_cache* c, const rkc_attention* a, void* stream) {
   if (rkc_status st = rkc_attention_check(c, a, true)) return st;
   if (c->n_seqs == 0 || a->max_len == 0) return RKC_OK;
+  if (!rkc_weigh_fits(c, a)) return RKC_E_UNSUPPORTED;
   return c->dtype == RKC_BF16 ? go<__bf16>(c, a, (hipStream_t)stream) : go<_Float16>(c, a, (hipStream_t)stream);
 }
