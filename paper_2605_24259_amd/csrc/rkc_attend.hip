@@ -257,9 +257,10 @@ size_t rkc_attend_scratch_bytes(const rkc_cache* c, const rkc_attention* a) {
 rkc_status rkc_attend(const rkc_cache* c, const rkc_attention* a, void* stream) {
   if (rkc_status st = rkc_attention_check(c, a, false)) return st;
   if (c->n_seqs == 0) return RKC_OK;
-  if (a->n_rows == 0 || a->max_rows == 0) return a->d_weight ? rkc_weigh(c, a, stream) : RKC_OK;
+  if (a->n_rows == 0) return a->d_weight ? rkc_weigh(c, a, stream) : RKC_OK;
   hipStream_t s = (hipStream_t)stream;
-  const rkc_plan p = rkc_attend_plan(c, a);
+  rkc_plan p = rkc_attend_plan(c, a);
+  if (a->max_rows == 0) p.splits = 1, p.keep = false, p.bytes = 0;  // sequences that have rows all the same are told of
   // rows of tiles are counted in 32 bits
   if ((int64_t)c->n_seqs * c->kv_heads * p.tiles * p.rows > 0x7fffffff) return RKC_E_UNSUPPORTED;
   const Join j = join_plan(c, a, &p);

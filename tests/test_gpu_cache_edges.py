@@ -112,3 +112,19 @@ def test_parents_are_flagged_where_sequences_are_cut(dim, group, rows, bias):
     g.status.zero_()
     assert torch.equal(g.weigh(q, want[1], o, n, **dict(m, parent=wrong)), account)
     assert g.status.tolist() == [told, told, told, 0]
+
+
+@pytest.mark.parametrize("account", [False, True])
+def test_rows_where_none_may_be(account):
+    """max_rows of 0 and rows all the same: their sequences are left out and told of, like any that have too many."""
+    import torch
+
+    import paper_2605_24259_amd as rkc
+    say("case no rows allowed", account)
+    c = ref.Case(3, [50, 2000, 7], [2, 0, 1])
+    g, w = gpu_cache(c), c.weight.cuda()
+    out, to = torch.full_like(c.q, 5.0).cuda(), torch.full_like(w, 3.0)
+    more = dict(weight=w, weight_out=to, decay=0.5) if account else {}
+    g.attend(c.q.cuda(), ints(c.offset), ints(c.lens), out=out, **mask(c, max_rows=0, max_len=2000), **more)
+    assert g.status.tolist() == [rkc.cache.CS_LENGTH, 0, rkc.cache.CS_LENGTH] and (out == 5).all()
+    assert (to[0] == 3).all() and (to[2] == 3).all() and torch.equal(to[1, :, :2000], w[1, :, :2000] * 0.5 if account else torch.full_like(to[1, :, :2000], 3.0))
