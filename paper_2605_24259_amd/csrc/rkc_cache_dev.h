@@ -335,37 +335,41 @@ __device__ __forceinline__ Scale load_scale(const rkc_attention& a) {
 }
 
 // tanh(y) of a lane's scores, x * pre = 2 y log2(e), by 1 - 2 / (exp(2 y) + 1).  That is off by 2^-23 of the cap, which
-// of a cap past 256 would be too much of a small score: there, while no lane of the wave has |y| over 0.8, it is a
-// polynomial in y^2 of least relative error on that range (6e-8; 1.5e-7 with the roundings of 32 bits).  (For all caps it
-// is the slower form: 2,048 rows over 32,768 slots 1,430 us instead of 1,320.)
+// of a cap past 256 would be too much of a small score: there, a score with |y| up to 0.8 takes a polynomial in y^2 of least
+// relative error on that range (6e-8; 3e-7 with the roundings of 32 bits), whatever the scores beside it are: those are
+// other rows', or of slots that nothing sees.  (For all caps it is the slower form: 2,048 rows over 32,768 slots 1,430 us
+// instead of 1,320.)
+__device__ __forceinline__ float cap_by_exp(float y2) { return 1.f - 2.f * __builtin_amdgcn_rcpf(ex2(y2) + 1.f); }
+__device__ __forceinline__ float cap_small(float z) {
+  const float t = z * z;
+  float y = __builtin_fmaf(t, -0.00435528671f, 0.0190932825f);
+  y = __builtin_fmaf(y, t, -0.0531143062f);
+  y = __builtin_fmaf(y, t, 0.13321048f);
+  y = __builtin_fmaf(y, t, -0.333326757f);
+  return z * __builtin_fmaf(y, t, 0.99999994f);
+}
 template <typename V, int N> __device__ __forceinline__ void cap_all(V (&x)[N], const Scale& s) {
   constexpr int A = sizeof(V) / 4;
-  bool small = false;
-  if (s.far) {
-    float most = 0.f;
+  constexpr float kSmall = 1.6f * kLog2e, kHalf = 0.5f * kLn2;
+  auto each = [&](auto cap) {
 #pragma unroll
     for (int u = 0; u < N; u++)
 #pragma unroll
-      for (int k = 0; k < A; k++) most = fmaxf(most, fabsf(x[u][k]));
-    small = !__any(most * s.pre > 1.6f * kLog2e);
+      for (int k = 0; k < A; k++) x[u][k] = cap(x[u][k]);
+  };
+  if (!s.far) {
+    each([&](float y) { return cap_by_exp(y * s.pre); });
+    return;
   }
-  if (small) {
-#pragma unroll
-    for (int u = 0; u < N; u++)
-#pragma unroll
-      for (int k = 0; k < A; k++) {
-        const float z = x[u][k] * (s.pre * (0.5f * kLn2)), t = z * z;
-        float y = __builtin_fmaf(t, -0.00435528671f, 0.0190932825f);
-        y = __builtin_fmaf(y, t, -0.0531143062f);
-        y = __builtin_fmaf(y, t, 0.13321048f);
-        y = __builtin_fmaf(y, t, -0.333326757f);
-        x[u][k] = z * __builtin_fmaf(y, t, 0.99999994f);
-      }
+  float most = 0.f;
+  each([&](float y) { return most = fmaxf(most, fabsf(y)), y; });
+  if (__any(most * s.pre > kSmall)) {
+    // a small one's result is below kSmall, so that what is not small yet is told from it: few registers at a time
+    each([&](float y) { return y * s.pre; });
+    each([&](float y) { return fabsf(y) <= kSmall ? cap_small(y * kHalf) : y; });
+    each([&](float y) { return fabsf(y) <= kSmall ? y : cap_by_exp(y); });
   } else {
-#pragma unroll
-    for (int u = 0; u < N; u++)
-#pragma unroll
-      for (int k = 0; k < A; k++) x[u][k] = 1.f - 2.f * __builtin_amdgcn_rcpf(ex2(x[u][k] * s.pre) + 1.f);
+    each([&](float y) { return cap_small(y * (s.pre * kHalf)); });
   }
 }
 

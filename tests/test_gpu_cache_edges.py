@@ -5,7 +5,7 @@ import pytest
 
 from tests import cache_reference as ref
 from tests.gpu_util import say
-from tests.test_gpu_cache import bush, check_attend, check_weigh, gpu_cache, ints, mask, run_attend
+from tests.test_gpu_cache import UNIT, bush, check_attend, check_weigh, gpu_cache, ints, mask, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +128,38 @@ def test_rows_where_none_may_be(account):
     g.attend(c.q.cuda(), ints(c.offset), ints(c.lens), out=out, **mask(c, max_rows=0, max_len=2000), **more)
     assert g.status.tolist() == [rkc.cache.CS_LENGTH, 0, rkc.cache.CS_LENGTH] and (out == 5).all()
     assert (to[0] == 3).all() and (to[2] == 3).all() and torch.equal(to[1, :, :2000], w[1, :, :2000] * 0.5 if account else torch.full_like(to[1, :, :2000], 3.0))
+
+
+@pytest.mark.parametrize("softcap", [1e3, 1e6])
+@pytest.mark.parametrize("dim,group,rows,n", [(64, 2, 5, 90), (128, 4, 4, 2000), (256, 2, 6, 300), (64, 2, 40, 300), (128, 3, 60, 700), (256, 2, 70, 300)])
+@pytest.mark.parametrize("what", ["row", "slot"])
+def test_far_caps_beside_large_scores(softcap, dim, group, rows, n, what):
+    """A row's scores are capped as exactly beside a row, or a slot that it does not see, whose scores reach the cap as
+    they are without: to 2^-20 (8 + the largest |scale| |q| |k| of the slots that the row itself sees)."""
+    import torch
+    say("case caps", softcap, dim, group, rows, n, what)
+    c = ref.Case(dim + rows, [n], [rows], kv_heads=1, group=group, dim=dim, softcap=softcap, parent=bush(rows))
+    base, big = n - rows, softcap / 4
+    if what == "row":
+        c.q[1] *= big
+    else:
+        c.k[c.table[0, (base + 1) // 16], (base + 1) % 16] *= big
+    see = c.seen(0)[0]
+    k = np.linalg.norm(c.slots(c.k, 0, 0), axis=-1)
+    q = np.linalg.norm(c.q.double().numpy(), axis=-1)
+    top = np.where(see, k[None], 0).max(1)
+    a = 2.0 ** -20 * (8 + c.scale * q * top[:, None])
+    assert a.max() > 20 * a.min()  # scores that reach the cap are there, and such that do not
+    o, z = c.attend()
+    out, lse = run_attend(c)
+    assert np.all(np.abs(lse.double().cpu().numpy() - z) <= a), (np.abs(lse.double().cpu().numpy() - z) / a).max()
+    vmax = np.nan_to_num(c.v.double().numpy(), nan=0, posinf=0, neginf=0).__abs__().max()
+    u = UNIT["bfloat16"]
+    assert np.all(np.abs(out.double().cpu().numpy() - o) <= u * (vmax + np.abs(o)) + a[..., None] * vmax)
+    # each row's own part of the account, of a call with this row's sum alone
+    quiet = int(np.argmin(a.max(1)))
+    only = torch.full(z.shape, -np.inf, dtype=torch.float32)
+    only[quiet] = torch.from_numpy(z[quiet]).float()
+    w = gpu_cache(c).weigh(c.q.cuda(), only.cuda(), ints(c.offset), ints(c.lens), **mask(c)).double().cpu().numpy()[0, 0, :n]
+    want = c.weigh(only.double().numpy(), 1.0)[0, 0]
+    assert np.all(np.abs(w - want) <= (a[quiet].max() + 2.0 ** -23 * np.abs(z[quiet]).max() + 2.0 ** -22) * want + 1e-30)
