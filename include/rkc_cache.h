@@ -91,7 +91,8 @@ typedef struct rkc_attention {
   const int32_t* d_prefix;     /* [n_seqs] or NULL                                                   */
   const int32_t* d_parent;     /* [n_rows] row within its sequence, -1 for a root; or NULL           */
   const float* d_slope;        /* [q_heads] or NULL                                                  */
-  void* d_out;                 /* [n_rows][q_heads][head_dim], 16-byte aligned (rkc_attend)          */
+  void* d_out;                 /* [n_rows][q_heads][head_dim], 16-byte aligned (rkc_attend); may be d_q with
+                                  its strides where d_weight is NULL                                 */
   float* d_lse;                /* [n_rows][q_heads]: written by rkc_attend, read by rkc_weigh        */
   const float* d_weight_in;    /* [n_seqs][kv_heads][max_len] or NULL (zeros)                        */
   float* d_weight;             /* the same, may be d_weight_in; rkc_attend: or NULL.  Slots below the

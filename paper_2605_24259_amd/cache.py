@@ -191,6 +191,7 @@ class PagedCache:
         row_start   [rows] int32: the first slot a row sees beside the prefix (its document's start)
         parent      [rows] int32: rows are a tree; a row's parent within its sequence, -1 for a root
         weight      with it or ``weight_out``: the rows' attention weights are added to the account as in ``weigh``
+        out         takes the outputs; may be q where there is no account
 
         Returns (out, lse), or (out, lse, weight_out): out as q, lse [rows, heads] float32, the natural logarithm
         of the softmax sums.  A row that sees nothing gets zeros and -inf.

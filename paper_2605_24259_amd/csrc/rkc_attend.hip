@@ -258,6 +258,7 @@ rkc_status rkc_attend(const rkc_cache* c, const rkc_attention* a, void* stream) 
   if (rkc_status st = rkc_attention_check(c, a, false)) return st;
   if (c->n_seqs == 0) return RKC_OK;
   if (a->n_rows == 0) return a->d_weight ? rkc_weigh(c, a, stream) : RKC_OK;
+  if (a->d_weight && a->d_out == a->d_q) return RKC_E_RANGE;  // the account may read the queries again
   hipStream_t s = (hipStream_t)stream;
   rkc_plan p = rkc_attend_plan(c, a);
   if (a->max_rows == 0) p.splits = 1, p.keep = false, p.bytes = 0;  // sequences that have rows all the same are told of

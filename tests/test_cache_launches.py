@@ -61,3 +61,9 @@ def test_the_size_is_told_before_the_scratch(lib):  # noqa: F811
     a.d_scratch = 0
     assert call(lib, "rkc_attend", c, a) == UNSUPPORTED
     assert lib.rkc_attend_scratch_bytes(ctypes.byref(c), ctypes.byref(a)) >= 0
+
+
+def test_an_account_wants_the_queries_left_alone(lib):  # noqa: F811
+    c, a, e = structs()
+    a.d_weight, a.d_out = 0x300000, a.d_q
+    assert call(lib, "rkc_attend", c, a) == -3

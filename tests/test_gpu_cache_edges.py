@@ -163,3 +163,22 @@ def test_far_caps_beside_large_scores(softcap, dim, group, rows, n, what):
     w = gpu_cache(c).weigh(c.q.cuda(), only.cuda(), ints(c.offset), ints(c.lens), **mask(c)).double().cpu().numpy()[0, 0, :n]
     want = c.weigh(only.double().numpy(), 1.0)[0, 0]
     assert np.all(np.abs(w - want) <= (a[quiet].max() + 2.0 ** -23 * np.abs(z[quiet]).max() + 2.0 ** -22) * want + 1e-30)
+
+
+@pytest.mark.parametrize("dim,group,rows,lens", [(64, 2, 1, [300, 40]), (128, 4, 3, [2500, 90]), (256, 1, 4, [900, 30]), (64, 1, 200, [900, 200]), (128, 4, 40, [700, 90])])
+def test_outputs_in_place_of_queries(dim, group, rows, lens):
+    """Outputs may go where the queries were, but not with an account, for which the queries may be read again."""
+    import torch
+
+    import paper_2605_24259_amd as rkc
+    say("case in place", dim, group, rows, lens)
+    c = ref.Case(dim + rows, lens, [rows] * 2, group=group, dim=dim)
+    want = run_attend(c)
+    g, q, m = gpu_cache(c), c.q.cuda(), mask(c, max_len=max(lens))
+    o, n, w = ints(c.offset), ints(c.lens), c.weight.cuda()
+    for kw in (dict(weight=w), dict(weight_out=w)):
+        with pytest.raises(rkc.RkcError) as e:
+            g.attend(q, o, n, out=q, **kw, **m)
+        assert e.value.status == -3 and torch.equal(q, c.q.cuda()) and torch.equal(w, c.weight.cuda())
+    out, lse = g.attend(q, o, n, out=q, **mask(c))
+    assert out is q and torch.equal(out, want[0]) and torch.equal(lse, want[1])
