@@ -108,15 +108,14 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
   const int lane_run = uni(tid / CH & ~15);
   auto key_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : keys16_at<D>(r, c); };
   auto val_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : vals16_at<D>(r, c); };
-  uint32_t k_off[2], v_off[2];  // of a piece in its run; the chunk is the one that the tile's layout has at its place
-#pragma unroll
-  for (int p = 0; p < 2; p++) {
-    const uint32_t r = (p * kThreads + tid) / CH;
-    k_off[p] = (r & 15) * kp.slot + (key_in(r, tid % CH) - r * D) * 2, v_off[p] = (r & 15) * vp.slot + (val_in(r, tid % CH) - r * D) * 2;
-  }
+  // Of a piece in its run; the chunk is the one that the tile's layout has at its place.  A thread's pieces lie whole runs
+  // apart, and the layouts repeat after 16 rows.
+  static_assert(kThreads / CH % 16 == 0, "runs");
+  const uint32_t r = threadIdx.x / CH;
+  const uint32_t k_off = (r & 15) * kp.slot + (key_in(r, tid % CH) - r * D) * 2, v_off = (r & 15) * vp.slot + (val_in(r, tid % CH) - r * D) * 2;
   int page[P];  // of the next tile to be loaded
   auto run_of = [&](int t0, int p) {  // a run behind the end stands for the first one
-    const int at = t0 + lane_run + (p * kThreads / CH & ~15);
+    const int at = t0 + lane_run + p * kThreads / CH;
     return at < end ? at : t0;
   };
   auto look_up = [&](int i) {
@@ -129,10 +128,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void attend_tile(const rkc
     T* to = lds + buf * 2 * kTile + wave * 64 * 8;
 #pragma unroll
     for (int p = 0; p < P; p++) {
-      const int at = run_of(t0, p) & in_page, o = kThreads / CH >= 16 ? 0 : p & 1;
+      const int at = run_of(t0, p) & in_page;
       const int block = block_of(c, page[p], bad);
-      dma(fixed(run_at(kp, block, at)) + k_off[o], to + p * kThreads * 8);
-      dma(fixed(run_at(vp, block, at)) + v_off[o], to + kTile + p * kThreads * 8);
+      dma(fixed(run_at(kp, block, at)) + k_off, to + p * kThreads * 8);
+      dma(fixed(run_at(vp, block, at)) + v_off, to + kTile + p * kThreads * 8);
     }
   };
   // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
