@@ -9,7 +9,8 @@ The replay decides what happens to a pool's blocks; a ``PagedCache`` works on wh
     length, weight, pos = cache.evict(weight, length, budget, protect=claimed)
 
 Everything runs in the library's HIP kernels on the current stream (or ``stream``); torch provides buffers.
-Nothing is copied to the host and no call waits for the GPU.
+Nothing is copied to the host and no call waits for the GPU.  The operators are for serving: they have no gradients, and
+what they return has no history, also where queries or a cache require one.
 """
 from __future__ import annotations
 

@@ -208,7 +208,9 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   // time, as they even out unlike lengths (64 sequences of 1 to 4,096 slots: 122 us, with five 126, with three 141).
   const bool wide_head = c->head_dim == 256;
   const int64_t want = wide_head || p.rows == 256 ? 256 : p.few ? 10 * 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
-  const int64_t cut = units ? (want + units - 1) / units : 1;  // workgroups along a sequence
+  // Workgroups along a sequence; rounded up, so that there may be a few more than the card holds at once (six units of 256
+  // elements a head: 258).
+  const int64_t cut = units ? (want + units - 1) / units : 1;
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;
   // Of few rows no less than four tiles a wave, else starts and joins cost more than they save (one sequence of 32,768
@@ -219,7 +221,7 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   // 20.8 us whole, 28.4 in two chunks; 40 of 64 over 300 slots 12.2 and 16.6), but for a few workgroups that go through 256
   // elements a head (8 rows over 512 slots: 25.7 and 16.6; 512 rows 32.3 and 41.9).
   if (!p.few && a->max_len <= 512 && (c->head_dim < 256 || units >= 32)) chunk = 512;
-  // Short sequences whole, by eight waves: no second kernel for the join (four sequences of up to 80 slots: 10.6 us in one
+  // Short sequences whole, by eight waves: no second kernel for the join (four sequences of up to 1,280 slots: 10.6 us in one
   // kernel where the split took 6.0 and the join 4.4, and 12.9 us a call instead of 16.8).
   p.waves = p.few && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
   if (p.waves == 8) chunk = a->max_len < 32 ? 32 : (a->max_len + 31) / 32 * 32;

@@ -7,13 +7,15 @@
 // workgroups begin and end more often.
 // A workgroup takes a chunk of one sequence's slots for one head, its four waves (eight, see rkc_attend_plan) take 32 slots at a time:
 //   K goes from memory straight into the product's operand (a lane holds 8 elements of its slot's key),
-//   V goes through the wave's own 32-slot tile in LDS, from where it is read transposed (no barriers),
+//   V goes through the wave's own 32-slot tile in LDS, from where it is read transposed (no barriers; its bank
+//   conflicts are 0.04 of the LDS cycles of long sequences, 0.16 of those of many short ones),
 //   both for the next 32 slots are in flight while these are worked on.
 // Waves keep maxima, sums and outputs of their own (32 bits) and join them once at the end; chunks are joined by a
 // second kernel where a sequence has more than one.
 // Weights go into the second product as two operands each, rounded and the rest, as the matrix units wait for the read
 // anyway: outputs are as near to the formula's as with weights in 32 bits (4 sequences of up to 1,280 slots in float16:
 // 4.8e-5, with rounded weights alone up to 1.5 times as far), at the same time (898 us of 5 long ones, 899 without).
+// Heads of 256 elements leave a wave a SIMD: 4.6 TB/s of 5 sequences of 125,000 to 131,072 slots, 8 heads (1,141 us).
 #include "rkc_cache_dev.h"
 #include "rkc_tiles.h"
 

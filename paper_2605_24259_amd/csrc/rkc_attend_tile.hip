@@ -5,13 +5,16 @@
 // columns of its matrix products, and goes over the slots that any of them sees in tiles of 64 (32 at 256 elements a
 // head).  K and V of up to three tiles ahead are on their way from memory into LDS, past the registers.  Tiles that
 // every row sees skip the masks, waves whose rows see nothing of a tile skip it.
-//   D = 64, 128, up to 128 rows: 4 waves of 32 rows, 32x32x16 products, a barrier a tile
-//   D = 128, more:               8 waves of 32 rows in two groups that multiply and weigh in turns (in_turns)
-//   D = 256:                     8 waves of 16 rows, 16x16x32 products (of 32 rows the outputs alone would take 256 registers)
-// What bounds it: matrix products and the exponentials between them, at the clock that the card holds under both.
-// 2,048 rows of 32 heads over 32,768 slots (8 heads of 128 elements): 1,115 us, 955 TFLOP/s, 0.8 of a large matrix
-// product's rate; 1,310 us with a cap, whose exponential and reciprocal nothing hides.  At 256 elements a head 2,048
-// rows of 16 heads over 16,384 slots: 750 us, 690 TFLOP/s.  32 trees of 64 rows over 8,192 slots: 340 us, 800 TFLOP/s.
+//   D = 64, 128:   4 waves of 32 rows, 32x32x16 products, a barrier a tile
+//   D = 128, more than 128 packed rows where they fill the card (rkc_attend_plan): 8 waves of 32 rows in two groups that
+//                  multiply and weigh in turns (in_turns)
+//   D = 256:       8 waves of 16 rows, 16x16x32 products, in turns as well (a wave of 32 rows would hold 128 registers of
+//                  outputs, 64 of queries and 16 of scores, of the 256 that two waves a SIMD have; that form is not built)
+// What bounds it: matrix products and the exponentials between them.  2,048 rows of 32 heads over 32,768 slots (8 heads of
+// 128 elements): 1,040 us, 1,020 TFLOP/s, 0.86 of a large matrix product's rate; 1,311 us with a cap, of which the matrix
+// units are at work for 0.36 and the vector units' issue is taken for 0.65, so that the two hardly overlap.  At 256 elements
+// a head 2,048 rows of 16 heads over 16,384 slots: 680 us, 760 TFLOP/s.  32 trees of 64 rows over 8,192 slots: 345 us, 790
+// TFLOP/s.
 #include <type_traits>
 
 #include "rkc_cache_dev.h"

@@ -293,8 +293,10 @@ template <int N> __global__ __launch_bounds__(N) void evict_choose(const evict_a
 
 // Longer sequences: a workgroup for each tile of a head, and a launch for each step, which reads what the tiles of the
 // step before wrote, as one workgroup would take a tile after the other (8 heads of 65,536 slots 145 us a call instead of
-// 78).  Rounds 0, 1 and 2 count 11, 11 and 10 bits of the order; round 3 tallies each tile (ties, those of
-// them before the new end, kept slots without ties before and behind it); round 4 lists and writes.
+// 78).  Every workgroup adds up the counts of all its head's tiles, 8 KB each, so that what is read grows with the square
+// of the length: 4 x 32 KB a head and round at 65,536 slots, 4,096 x 32 MB at 2^26.
+// Rounds 0, 1 and 2 count 11, 11 and 10 bits of the order; round 3 tallies each tile (ties, those of them before the new end,
+// kept slots without ties before and behind it); round 4 lists and writes.
 template <int ROUND>
 __global__ __launch_bounds__(kThreads) void evict_round(const evict_args g) {
   constexpr int kShift[5] = {21, 10, 0, 0, 0};

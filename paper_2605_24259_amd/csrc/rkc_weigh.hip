@@ -7,6 +7,9 @@
 // products and an exponential for every row and slot in between (32 rows of 32 heads, 8 heads of 128 elements: 32
 // sequences of 8,192 slots 146 us, 3.9 TB/s, 470 TFLOP/s; 8 of 6,000 to 16,384 60 us, 3.6 TB/s).  Four workgroups a CU
 // hide the latency between those: with the lines of trees always in LDS there was room for three, 178 us instead of 146.
+// Of more than 128 packed rows the queries are staged anew for each turn of 128 slots, behind two barriers each, and bound
+// it: 1,024 rows of 32 heads over each of two prompts of 8,192 slots 318 us, 405 TFLOP/s; a whole prompt of 4,096 tokens,
+// which has 128 workgroups, 1,036 us, 66 TFLOP/s of what its rows see.
 #include "rkc_cache_dev.h"
 
 namespace {
