@@ -70,7 +70,8 @@ typedef struct rkc_cache {
  * The score of a row of query head h and a slot it sees is  x = scale q.k,  then softcap tanh(x / softcap) if
  * softcap > 0, then x - slope[h] |distance| if d_slope is given; the distance is that of the slots, drafted
  * slots counting as base + depth in the tree.  A row that sees nothing gets zeros and -inf.  Slots that no row
- * sees and slots behind the length may hold anything.  Query heads [g * h, g * (h + 1)) share key/value head h,
+ * sees and slots behind the length may hold anything; an infinite value that a row sees makes its output infinite,
+ * or NaN where its weight is below the range of 32 bits.  Query heads [g * h, g * (h + 1)) share key/value head h,
  * g = q_heads / kv_heads. */
 typedef struct rkc_attention {
   int32_t n_rows;   /* rows of all sequences = d_row_offset[n_seqs]                                  */
