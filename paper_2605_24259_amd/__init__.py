@@ -85,8 +85,9 @@ def load():
         lib.rkc_query_telemetry.restype = ctypes.c_int
         lib.rkc_status_string.argtypes = [ctypes.c_int]
         lib.rkc_status_string.restype = ctypes.c_char_p
-        from . import cache
+        from . import cache, packed
         cache.declare(lib)
+        packed.declare(lib)
         if lib.rkc_abi_version() != ABI_VERSION:
             raise RuntimeError(f"{LIB_PATH} implements ABI {lib.rkc_abi_version()}, this binding "
                                f"ABI {ABI_VERSION}; rebuild the library")
@@ -199,3 +200,4 @@ def replay(trace, stream=None):
 
 
 from .cache import PagedCache  # noqa: E402  (operators on the contents of a paged KV cache)
+from .packed import PackedCache  # noqa: E402  (the same in 4 bits)

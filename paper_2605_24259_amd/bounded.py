@@ -57,9 +57,7 @@ def run(prompt=70, chunk=10, budget=10, resident=60, usable=80, *, window=32, re
 
     def put(rows):
         """Keys and values of new tokens go behind the live slots."""
-        slots = torch.arange(live, live + rows, device=dev)
-        at = table[1, slots // BLOCK].long()
-        k[at, slots % BLOCK], v[at, slots % BLOCK] = rand(rows, kv_heads, head_dim), rand(rows, kv_heads, head_dim)
+        cache.store(rand(rows, kv_heads, head_dim), rand(rows, kv_heads, head_dim), ints(0, 0, rows), ints(held, live + rows))
         pos[1, :, live: live + rows] = torch.arange(seen, seen + rows, dtype=torch.int32, device=dev)
 
     for step in range(steps):

@@ -13,7 +13,7 @@ ROOT = os.path.dirname(PKG)
 SRCS = [os.path.join(PKG, "csrc", f) for f in ("rkc_replay.hip", "rkc_lean.hip", "rkc_lean_few.hip",
                                               "rkc_big.hip", "rkc_tiny.hip", "rkc_attend.hip",
                                               "rkc_attend_few.hip", "rkc_attend_tile.hip", "rkc_weigh.hip",
-                                              "rkc_evict.hip")]
+                                              "rkc_evict.hip", "rkc_rows.hip", "rkc_packed.hip", "rkc_packed_tile.hip")]
 LIB = os.path.join(PKG, "librkc.so")
 ARCH = "gfx950"
 

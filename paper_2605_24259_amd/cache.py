@@ -6,6 +6,8 @@ The replay decides what happens to a pool's blocks; a ``PagedCache`` works on wh
     out, lse = cache.attend(q, row_offset, length, max_rows=n)              # a prompt's chunk
     out, lse = cache.attend(q, row_offset, length, max_rows=n, parent=p)    # a tree of drafted tokens
     weight = cache.weigh(q, lse, row_offset, length, max_rows=n)            # the account of the slots
+    q = cache.store(k, v, row_offset, length, q=q, freq=f)                  # new rows, normed and turned
+    k, v = cache.read(row_offset, length, rows=n)                           # slots as rows again
     length, weight, pos = cache.evict(weight, length, budget, protect=claimed)
 
 Everything runs in the library's HIP kernels on the current stream (or ``stream``); torch provides buffers.
@@ -19,6 +21,7 @@ import ctypes
 import math
 
 from . import RkcError, _stream_ptr
+from .rows import RowOps
 
 MAX_TREE_ROWS = 256
 HEAD_DIMS = (64, 128, 256)
@@ -71,7 +74,73 @@ def declare(lib):
 _HERE = contextlib.nullcontext()
 
 
-class PagedCache:
+class _Cached(RowOps):
+    """What the caches of 16 and of 4 bits share: the sequences' table and status, checks of arguments, calls."""
+
+    def _bind(self, torch, held, block_table):
+        """The device, which is that of `held`, the table and the status words."""
+        self._int32, self._torch, self._raw_stream = torch.int32, torch, torch._C._cuda_getCurrentRawStream
+        self._index, self.device = held.get_device(), held.device
+        if block_table.dtype is not torch.int32 or block_table.device != self.device or block_table.dim() != 2 or \
+                not block_table.is_contiguous():
+            raise ValueError(f"block_table: a contiguous int32 tensor [seqs, pages] on {self.device} is wanted")
+        self.block_table = block_table
+        self.status = torch.zeros(block_table.shape[0], dtype=torch.int32, device=self.device)
+
+    def _finish(self, c):
+        """The library's struct and the sizes in it."""
+        self._c, self._c_ref = c, ctypes.byref(c)
+        self.n_seqs, self.kv_heads, self.head_dim = int(c.n_seqs), int(c.kv_heads), int(c.head_dim)
+        self.max_len = int(c.max_pages) * int(c.page_tokens)
+
+    def _ints(self, t, name, n):
+        """Address of a contiguous int32 tensor of n values on the cache's device."""
+        if t.dtype is not self._int32 or t.get_device() != self._index or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous int32 tensor of {n} values on {self.device} is wanted, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _attention(self, q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent):
+        """Checks what attend and weigh share; the fields of rkc_attention in two runs, around those of the outputs."""
+        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not self.dtype or q.get_device() != self._index or q.stride(2) != 1:
+            raise ValueError(f"q: [rows, heads, {self.head_dim}] of {self.dtype} on {self.device}, the last dimension "
+                             f"contiguous, is wanted, got {q.dtype} {tuple(q.shape)} on {q.device}")
+        n, heads, _ = q.shape
+        if heads % self.kv_heads or not heads:
+            raise ValueError(f"q: {heads} heads are no multiple of the cache's {self.kv_heads}")
+        if slope is not None and (slope.dtype is not self._torch.float32 or slope.get_device() != self._index
+                                  or not slope.is_contiguous() or tuple(slope.shape) != (heads,)):
+            raise ValueError(f"slope: [{heads}] float32 on {self.device} is wanted")
+        offsets, lengths = self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)
+        head = (n, heads, max_rows, self.max_len if max_len is None else max_len, self._scale if scale is None else scale, softcap)
+        tail = (q.data_ptr(), offsets, lengths, None if row_start is None else self._ints(row_start, "row_start", n),
+                None if prefix is None else self._ints(prefix, "prefix", self.n_seqs),
+                None if parent is None else self._ints(parent, "parent", n), None if slope is None else slope.data_ptr())
+        return head, (q.stride(0), q.stride(1)), tail
+
+    def _outputs(self, q, out):
+        """(out, lse) of an attention: new ones, or `out` as given."""
+        if out is None:
+            out = q.new_empty(q.shape)
+        elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or out.stride(2) != 1:
+            raise ValueError("out: a tensor like q, the last dimension contiguous, is wanted")
+        return out, q.new_empty(q.shape[:2], dtype=self._torch.float32)
+
+    def _call(self, f, name, args, stream):
+        # the current stream of the cache's device; looked up by number, a twentieth of the cost of a Stream object
+        st = f(self._c_ref, args, self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
+        if st != 0:
+            raise RkcError(st, name)
+
+    def _on(self, stream):
+        """Tensors made in a call belong to the stream that the call runs on."""
+        return _HERE if stream is None else self._torch.cuda.stream(stream)
+
+    def _scratch(self, need):
+        return self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
+
+
+class PagedCache(_Cached):
     """Blocks of keys and values, and the sequences that lie in them.  Calls run on the current device, which has to be
     the cache's.
 
@@ -97,16 +166,10 @@ class PagedCache:
             raise TypeError(f"k and v are bfloat16 or float16, alike: {k.dtype}, {v.dtype}")
         if k.stride(3) != 1 or v.stride(3) != 1:
             raise ValueError("the last dimension of k and v must be contiguous")
-        self._int32, self._torch, self._raw_stream = torch.int32, torch, torch._C._cuda_getCurrentRawStream
-        self._index, self._scale = k.get_device(), 1 / math.sqrt(k.shape[3])
-        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         if not k.is_cuda or v.device != k.device:
             raise ValueError("k and v must be on one GPU")
-        if block_table.dtype is not torch.int32 or block_table.device != self.device or block_table.dim() != 2 or \
-                not block_table.is_contiguous():
-            raise ValueError(f"block_table: a contiguous int32 tensor [seqs, pages] on {self.device} is wanted")
-        self.block_table = block_table
-        self.status = torch.zeros(block_table.shape[0], dtype=torch.int32, device=self.device)
+        self._bind(torch, k, block_table)
+        self.k, self.v, self.dtype, self._scale = k, v, k.dtype, 1 / math.sqrt(k.shape[3])
         c = _Cache()
         c.n_seqs, c.max_pages = block_table.shape
         c.n_blocks, c.page_tokens, c.kv_heads, c.head_dim = k.shape
@@ -114,16 +177,7 @@ class PagedCache:
         c.k_block_stride, c.k_slot_stride, c.k_head_stride = k.stride()[:3]
         c.v_block_stride, c.v_slot_stride, c.v_head_stride = v.stride()[:3]
         c.d_k, c.d_v, c.d_block_table, c.d_status = k.data_ptr(), v.data_ptr(), block_table.data_ptr(), self.status.data_ptr()
-        self._c, self._c_ref = c, ctypes.byref(c)
-        self.n_seqs, self.kv_heads, self.head_dim = int(c.n_seqs), int(c.kv_heads), int(c.head_dim)
-        self.max_len = int(c.max_pages) * int(c.page_tokens)
-
-    def _ints(self, t, name, n):
-        """Address of a contiguous int32 tensor of n values on the cache's device."""
-        if t.dtype is not self._int32 or t.get_device() != self._index or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous int32 tensor of {n} values on {self.device} is wanted, got {t.dtype} "
-                             f"{tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+        self._finish(c)
 
     def _account(self, t, name, dtype, max_len):
         """Strides of an account (or of its positions)."""
@@ -133,24 +187,6 @@ class PagedCache:
                              f"dimension contiguous, is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
         # of a dimension of one, the stride says nothing
         return t.stride(0) if self.n_seqs > 1 else 0, t.stride(1) if self.kv_heads > 1 else 0
-
-    def _attention(self, q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent):
-        """Checks what attend and weigh share; the fields of rkc_attention in two runs, around those of the outputs."""
-        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not self.dtype or q.get_device() != self._index or q.stride(2) != 1:
-            raise ValueError(f"q: [rows, heads, {self.head_dim}] of {self.dtype} on {self.device}, the last dimension "
-                             f"contiguous, is wanted, got {q.dtype} {tuple(q.shape)} on {q.device}")
-        n, heads, _ = q.shape
-        if heads % self.kv_heads or not heads:
-            raise ValueError(f"q: {heads} heads are no multiple of the cache's {self.kv_heads}")
-        if slope is not None and (slope.dtype is not self._torch.float32 or slope.get_device() != self._index
-                                  or not slope.is_contiguous() or tuple(slope.shape) != (heads,)):
-            raise ValueError(f"slope: [{heads}] float32 on {self.device} is wanted")
-        offsets, lengths = self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)
-        head = (n, heads, max_rows, self.max_len if max_len is None else max_len, self._scale if scale is None else scale, softcap)
-        tail = (q.data_ptr(), offsets, lengths, None if row_start is None else self._ints(row_start, "row_start", n),
-                None if prefix is None else self._ints(prefix, "prefix", self.n_seqs),
-                None if parent is None else self._ints(parent, "parent", n), None if slope is None else slope.data_ptr())
-        return head, (q.stride(0), q.stride(1)), tail
 
     def _weights(self, weight, weight_out, n):
         """(weight_out, its strides) for the account `weight`, or none."""
@@ -163,19 +199,6 @@ class PagedCache:
         if at is not None and at != to:
             raise ValueError(f"weight and weight_out differ in strides: {weight.stride()}, {weight_out.stride()}")
         return weight_out, to
-
-    def _call(self, f, name, args, stream):
-        # the current stream of the cache's device; looked up by number, a twentieth of the cost of a Stream object
-        st = f(self._c_ref, args, self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
-        if st != 0:
-            raise RkcError(st, name)
-
-    def _on(self, stream):
-        """Tensors made in a call belong to the stream that the call runs on."""
-        return _HERE if stream is None else self._torch.cuda.stream(stream)
-
-    def _scratch(self, need):
-        return self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
 
     def attend(self, q, row_offset, length, *, max_rows, max_len=None, scale=None, softcap=0.0, slope=None, prefix=None,
                row_start=None, parent=None, out=None, weight=None, decay=1.0, weight_out=None, stream=None):
@@ -200,11 +223,7 @@ class PagedCache:
         head, q_strides, tail = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
         weigh, strides = weight is not None or weight_out is not None, (0, 0)
         with self._on(stream):
-            if out is None:
-                out = q.new_empty(q.shape)
-            elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or out.stride(2) != 1:
-                raise ValueError("out: a tensor like q, the last dimension contiguous, is wanted")
-            lse = q.new_empty(q.shape[:2], dtype=self._torch.float32)
+            out, lse = self._outputs(q, out)
             if weigh:
                 weight_out, strides = self._weights(weight, weight_out, head[3])
             a = _Attention(*head, decay, 0, *q_strides, out.stride(0), out.stride(1), *strides, *tail, out.data_ptr(), lse.data_ptr(),

@@ -249,6 +249,16 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a) {
   return p;
 }
 
+bool rkc_join_fits(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p) {
+  const Join j = join_plan(c, a, p);
+  return rkc_fits(j.workgroups, j.lanes);
+}
+
+rkc_status rkc_attend_join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  const Join j = join_plan(c, a, p);
+  return c->dtype == RKC_BF16 ? join<__bf16>(c, a, p, j, s) : join<_Float16>(c, a, p, j, s);
+}
+
 extern "C" {
 
 size_t rkc_attend_scratch_bytes(const rkc_cache* c, const rkc_attention* a) {

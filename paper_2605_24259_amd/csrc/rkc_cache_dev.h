@@ -411,5 +411,8 @@ rkc_plan rkc_attend_plan(const rkc_cache* c, const rkc_attention* a);
 inline int rkc_attend_lanes(const rkc_cache* c, const rkc_plan* p) { return 64 * (p->few ? p->waves : p->rows == 256 || c->head_dim == 256 ? 8 : 4); }
 rkc_status rkc_attend_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 rkc_status rkc_attend_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
+// The join of a plan's parts, and whether it can be launched.
+bool rkc_join_fits(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p);
+rkc_status rkc_attend_join(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 
 #endif

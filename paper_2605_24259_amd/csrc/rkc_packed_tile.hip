@@ -1,0 +1,305 @@
+// rkc_packed_tile.hip -- attention of many rows over a paged cache in 4 bits (chunks of prompts, larger trees).
+//
+// out = sum_j exp(x_j - m) v_j / sum_j exp(x_j - m) in one pass over the slots, m the running maximum of a row's scores.
+// A workgroup of W waves holds R W packed rows (rows x query heads of one key/value head), R of them in each wave as the
+// columns of its matrix products, and goes over the slots that any of them sees in tiles of 64 (32 at 256 elements a
+// head).  A tile's codes and scales are loaded one tile ahead into registers, a thread's part of it each, and converted once
+// for all waves into 16 bits in LDS, while the tile before is worked on.  Tiles that every row sees skip the masks, waves whose
+// rows see nothing of a tile skip it.
+// A marked slot's scores are NaN by its key's first scale, and so only the rows that see it; values are always finite.
+#include <type_traits>
+
+#include "rkc_packed_dev.h"
+#include "rkc_tiles.h"
+
+namespace {
+
+template <int R> struct Acc;
+template <> struct Acc<32> { typedef f32x16 t; };
+template <> struct Acc<16> { typedef f32x4 t; };
+
+template <typename T, int D, int W, int R>
+__global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+  typedef typename Vec8<T>::t V8;
+  // R rows a wave: products of R x R, A elements a lane; tiles of BK slots, kAhead of them on their way
+  typedef typename Acc<R>::t acc;
+  constexpr int A = R * R / 64, kRows = R * W, kThreads = 64 * W;
+  constexpr int BK = D == 256 ? 32 : 64;
+  constexpr int KT = BK / R, KC = D * R / 512, DB = D / R, NP = KT * A / 8;  // score blocks, key operands, output blocks, weight operands
+  constexpr int E = BK * D / kThreads, PER = D / E, NC = E / 8;  // elements of a key, and of a value, per thread; threads of a slot; dwords
+  constexpr int kTile = BK * D;
+  __shared__ __attribute__((aligned(16))) T lds[2 * 2 * kTile];  // K and V of two tiles
+  __shared__ uint64_t lines[RKC_MAX_TREE_ROWS][4];
+  __shared__ int depths[RKC_MAX_TREE_ROWS], lim[W][2];
+
+  const int H = c.kv_heads, G = a.q_heads / H;
+  // Heads first: with 8 of them each XCD has one, and its cache that head's keys and values for the row tiles of a
+  // sequence, which are neighbours; the rows that see most go first.  (All heads on each XCD: trees 397 us instead of
+  // 334, documents 57 instead of 49; sequences before row tiles: 455 and 62.)
+  const int h = blockIdx.x % H, split = blockIdx.x / H % pl.splits, b = blockIdx.x / (H * pl.splits);
+  const int qt = pl.tiles - 1 - b % pl.tiles, s = pl.sorted ? seq_of_rank(c, a, b / pl.tiles) : b / pl.tiles;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), grp = lane / R, col = lane % R;
+  // which rows are the wave's: neighbours work in turns on one SIMD, also where a tile is not full
+  const int part = W == 8 ? (wave & 3) * 2 + (wave >> 2) : wave;
+  const Seq q = load_seq(c, a, s);
+  if (!q.ok) {
+    if (split == 0 && h == 0 && qt == 0 && tid == 0) flag(c, s, RKC_CS_LENGTH);
+    return;
+  }
+  const int M = q.n * G, m0 = qt * kRows;
+  if (m0 >= M) return;
+  const int last = (min(M, m0 + kRows) - 1) / G;
+  const int c0 = split * pl.chunk, c1 = min(rows_end(a, q, s, last), c0 + pl.chunk);
+  if (split && c0 >= c1) return;
+  const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
+  const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
+
+  const int m = min(m0 + R * part + col, M - 1), qi = m / G, qh = h * G + m % G;
+  const bool mine = m0 + R * part + col < M, rows = m0 + R * part < M;
+  const Scale f = load_scale(a);
+  Row row = load_row(a, q, s, qi);
+  const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
+  V8 qf[KC];
+  {
+    const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + grp * 8;
+#pragma unroll
+    for (int k = 0; k < KC; k++) {
+      qf[k] = *(const V8*)(p + 512 / R * k);
+      if (f.negate) qf[k] = negated(qf[k]);
+    }
+  }
+  const bool tree = a.d_parent != nullptr, drafts = tree && c1 > q.base;
+  if (drafts || (tree && a.d_slope)) {
+    tree_lines(c, a, q, s, h == 0 && qt == 0, lines, depths);  // of a cut sequence, only parts that reach the tree come here
+    row.pos = q.base + depths[qi];
+  }
+  // slots that all of the wave's rows see, and slots that any of them, and of the workgroup's, sees
+  int all_from = 0, any_from = 0;
+  if (a.d_row_start) all_from = wave_max(row.start), any_from = wave_min(row.start);
+  const int all_to = uni(row.end), pre = uni(row.prefix);  // a wave's first lane has its first row
+  const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, R - 1));
+  if (lane == 0) lim[wave][0] = any_from, lim[wave][1] = any_to;
+  __syncthreads();
+  int g_any_from = lim[0][0], g_any_to = lim[0][1];
+#pragma unroll
+  for (int k = 1; k < W; k++) g_any_from = min(g_any_from, lim[k][0]), g_any_to = max(g_any_to, lim[k][1]);
+  g_any_from = uni(g_any_from), g_any_to = uni(g_any_to);
+  const int end = min(c1, g_any_to);
+
+  const Codes held = codes_of<D>(c, h);
+
+  float top = -kInf, sum = 0.f, lift = 0.f;  // lift: what all scores of a tile and lane are to lose yet
+  acc o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; d++)
+#pragma unroll
+    for (int k = 0; k < A; k++) o[d][k] = 0.f;
+
+  const rkc_tiles<BK> tiles(c0, end, pre, g_any_from);
+  const int n_tiles = tiles.n;
+  auto slot_of = [&](int i) { return tiles.slot(i); };
+  bool bad = false;
+  // this thread's part of a tile: a wave's parts lie in 16 slots of one page
+  static_assert(64 / PER <= 16, "runs");
+  const int mine_slot = tid / PER, lane_run = uni(mine_slot & ~15), part_of = tid % PER;
+  auto key_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : keys16_at<D>(r, c); };
+  auto val_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : vals16_at<D>(r, c); };
+  typedef uint32_t codes_t __attribute__((ext_vector_type(NC)));
+  const uint32_t c_off = (mine_slot & 15) * (D / 2) + part_of * (E / 2), s_off = (mine_slot & 15) * (D / 32) + part_of * E / 32;
+  codes_t kf, vf;   // of the next tile
+  uint32_t ks, vs;
+  int page;         // of the one behind it
+  auto run_of = [&](int t0) {  // a run behind the end stands for the first one
+    const int at = t0 + lane_run;
+    return at < end ? at : t0;
+  };
+  auto look_up = [&](int i) { page = page_of(table, shift, run_of(slot_of(i))); };
+  auto load = [&](int i) {
+    const int at = run_of(slot_of(i)) & in_page;
+    const char* b = held.base + block_of(c, page, bad) * held.block;
+    const char* kb = fixed(b + at * (D / 2));
+    const char* sb = fixed(b + held.key_scales + at * (D / 32));
+    kf = *(const codes_t*)(kb + c_off);
+    vf = *(const codes_t*)(kb + held.values + c_off);
+    ks = *(const uint8_t*)(sb + s_off);
+    vs = *(const uint8_t*)(sb + (held.value_scales - held.key_scales) + s_off);
+  };
+  const int put_k = 2 * key_in(mine_slot, part_of * NC), put_v = 2 * (kTile + val_in(mine_slot, part_of * NC));
+  auto put = [&](int buf) {
+    const int pk = here(put_k + buf * 4 * kTile), pv = here(put_v + buf * 4 * kTile);
+    const float fk = scale_float(ks), fv = scale_float(min(vs, (uint32_t)kTopScale<T>));
+#pragma unroll
+    for (int k = 0; k < NC; k++) {
+      *(u32x4*)((char*)lds + (pk ^ k << 4)) = unpack8<T>(kf[k], fk);
+      *(u32x4*)((char*)lds + (pv ^ k << 4)) = unpack8<T>(vf[k], fv);
+    }
+  };
+  // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
+  // a row) and by whole rows.  Element e = 4 x + y of a score block is slot 4 * (64 / R) x + 4 grp + y of its R.
+  const int vi = lane & 15, vr = 4 * grp + (vi >> 2), vc = R == 32 ? (lane >> 4 & 1) * 2 + ((vi & 3) >> 1) : (vi & 3) >> 1, ve = (vi & 1) * 4;
+  const int key_at = 2 * key_in(col, grp), val_at = 2 * (kTile + val_in(vr, vc) + ve);
+  // whether any of the wave's rows sees anything of a tile, and whether all see all of it
+  auto sees = [&](int t0) { return rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre); };
+  auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k * (1024 / R)) + 2 * R * D * u); };
+  // values of the 512 / R slots of weight operand i, columns R d .. R d + R - 1
+  auto vals = [&](int va, int i, int d) {
+    const char* at = (const char*)lds + i * (512 / R) * 2 * D;
+    const int x = va ^ d * 2 * R;
+    if constexpr (R == 32) return read_tr2<T>(at + x, at + (x ^ 32) + 16 * D);
+    else return read_tr2<T>(at + x, at + x + 32 * D);
+  };
+  auto scores = [&](acc(&sc)[KT], int buf) {
+    const int ka = here(buf * 4 * kTile + key_at);
+#pragma unroll
+    for (int u = 0; u < KT; u++)
+#pragma unroll
+      for (int k = 0; k < A; k++) sc[u][k] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KC; k++)
+#pragma unroll
+      for (int u = 0; u < KT; u++) sc[u] = mma(keys(ka, u, k), qf[k], sc[u]);
+  };
+  auto slot_in = [](int u, int k) { return R * u + (k & 3) + 256 / R * (k >> 2); };  // less 4 grp
+  // cap, distance, masks, and the maximum that the weights refer to
+  auto fold = [&](acc(&sc)[KT], uint32_t(&seen)[BK / 32], int t0) {
+    const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
+    if (a.softcap > 0.f) cap_all(sc, f);
+    if (a.d_slope && t0 + BK <= all_to) {  // all slots lie before all rows: the part that is the same for a row's slots waits
+      lift = slope * (float)(row.pos - t0 - 4 * grp) * f.post;
+#pragma unroll
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int k = 0; k < A; k++) sc[u][k] = __builtin_fmaf(slope, (float)slot_in(u, k), sc[u][k]);
+    } else if (a.d_slope) {
+      lift = 0.f;
+      const int base_at = here(q.base - t0 - 4 * grp);
+      const float far = (float)(here(row.pos - t0) - 4 * grp);
+#pragma unroll
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int k = 0; k < A; k++) {
+          const int j = slot_in(u, k);
+          float gap = far - (float)j;
+          if (drafts && t0 + BK > q.base) {
+            const int i = j - base_at, d = depths[max(0, min(i, RKC_MAX_TREE_ROWS - 1))];
+            gap = i >= 0 ? (float)(row.pos - q.base - d) : gap;
+          }
+          sc[u][k] = __builtin_fmaf(-slope, fabsf(gap), sc[u][k]);
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < BK / 32; x++) seen[x] = 0xffffffff;
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < BK / 32; x++) {
+        const int j0 = t0 + 32 * x;
+        seen[x] = seen_of(row, j0, drafts ? line_window(lines[qi], 4, j0 - q.base) : 0) >> 4 * grp;
+      }
+#pragma unroll
+      for (int u = 0; u < KT; u++)
+#pragma unroll
+        for (int k = 0; k < A; k++) sc[u][k] = masked(sc[u][k], seen[slot_in(u, k) / 32], slot_in(u, k) % 32);
+    }
+    float most = -kInf;
+#pragma unroll
+    for (int u = 0; u < KT; u++)
+#pragma unroll
+      for (int k = 0; k < A; k++) most = fmaxf(most, sc[u][k]);
+    most = most * f.post - lift;
+    most = R == 32 ? max32(most) : max32(max16(most));
+    // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+    if (__any(most > top + (8.f + kRoom<T>))) {
+      const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
+      top = now, sum *= by;
+#pragma unroll
+      for (int d = 0; d < DB; d++) o[d] *= by;
+    }
+  };
+  // Weight operand i.  The products' operands have the cache's type: the weights are rounded to it here, their sum is not.
+  auto weights = [&](const acc(&sc)[KT], int i) {
+    const float mx = (top == -kInf ? 0.f : top) + lift;
+    f32x8 p;
+#pragma unroll
+    for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[(8 * i + k) / A][(8 * i + k) % A], f.post, -mx));
+    sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    return __builtin_convertvector(p, V8);
+  };
+
+  if (n_tiles > 0) {
+    look_up(0);
+    load(0);
+    if (n_tiles > 1) look_up(1);
+    put(0);
+    if (n_tiles > 1) load(1);
+    if (n_tiles > 2) look_up(2);
+  }
+  for (int i = 0; i < n_tiles; i++) {
+    const int t0 = slot_of(i), buf = i & 1;
+    __syncthreads();  // tile i is in LDS, and no wave reads tile i - 1 any more
+    const int va = here(buf * 4 * kTile + val_at);
+    acc sc[KT];
+    uint32_t seen[BK / 32];
+    const bool has = sees(t0);
+    if (has) scores(sc, buf);
+    if (i + 1 < n_tiles) {
+      put(buf ^ 1);
+      if (i + 2 < n_tiles) load(i + 2);
+      if (i + 3 < n_tiles) look_up(i + 3);
+    }
+    if (has) {
+      fold(sc, seen, t0);
+#pragma unroll
+      for (int x = 0; x < NP; x++) {
+        const V8 pb = weights(sc, x);
+#pragma unroll
+        for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb, o[d]);
+      }
+    }
+  }
+  if (bad) flag(c, s, RKC_CS_BLOCK);
+
+  sum = R == 32 ? sum32(sum) : sum32(sum16(sum));
+  if (!mine) return;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  if (pl.splits == 1) {
+    const float by = 1.f / sum;
+    T* to = (T*)a.d_out + (q.row0 + qi) * a.out_row_stride + qh * a.out_head_stride + 4 * grp;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+      for (int k = 0; k < A / 4; k++) {
+        f32x4 x = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * by;
+        if (sum == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
+        *(T4*)(to + R * d + 256 / R * k) = __builtin_convertvector(x, T4);
+      }
+    if (grp == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
+  } else {
+    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + R * part + col;
+    float* to = (float*)((char*)a.d_scratch + pl.part_at) + at * D + 4 * grp;
+#pragma unroll
+    for (int d = 0; d < DB; d++)
+#pragma unroll
+      for (int k = 0; k < A / 4; k++) *(f32x4*)(to + R * d + 256 / R * k) = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
+    float* st = (float*)((char*)a.d_scratch + pl.stat_at) + at * 2;
+    if (grp == 0) st[0] = top, st[1] = sum;
+  }
+}
+
+template <typename T, int D, int W, int R>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  packed_tile<T, D, W, R><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
+}
+
+template <typename T>
+rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  if (c->head_dim == 256) return go<T, 256, 8, 16>(c, a, p, s);
+  if (c->head_dim == 128) return go<T, 128, 4, 32>(c, a, p, s);
+  return go<T, 64, 4, 32>(c, a, p, s);
+}
+
+}  // namespace
+
+rkc_status rkc_packed_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  return c->dtype == RKC_BF16 ? go<__bf16>(c, a, p, s) : go<_Float16>(c, a, p, s);
+}
