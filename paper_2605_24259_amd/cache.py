@@ -120,11 +120,13 @@ class _Cached(RowOps):
 
     def _outputs(self, q, out):
         """(out, lse) of an attention: new ones, or `out` as given."""
+        torch = self._torch
         if out is None:
-            out = q.new_empty(q.shape)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or out.stride(2) != 1:
             raise ValueError("out: a tensor like q, the last dimension contiguous, is wanted")
-        return out, q.new_empty(q.shape[:2], dtype=self._torch.float32)
+        rows, heads, _ = q.shape
+        return out, torch.empty_strided((rows, heads), (heads, 1), dtype=torch.float32, device=self.device)
 
     def _call(self, f, name, args, stream):
         # the current stream of the cache's device; looked up by number, a twentieth of the cost of a Stream object

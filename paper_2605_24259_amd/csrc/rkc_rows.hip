@@ -5,7 +5,7 @@
 // element read and 2 (keys and values in 4 bits: 17/32) written, and for a decode step's few rows a chain of loads.
 // A lane has 16 elements of a head: the two runs of 8 that turn into each other, so that a rotation needs no other lane.
 // A workgroup has up to 16 rows, whose angles it finds once for all heads.
-// read: the other way, a lane 8 elements of a head.
+// read: the other way, a lane 8 elements of a head's key and value.
 #include <type_traits>
 
 #include "rkc_packed_dev.h"
@@ -127,7 +127,7 @@ __device__ __forceinline__ double inverse_root(double x) { return 1.0 / __builti
 // Norm and rotation of a lane's 16 elements.  W: 32 bits where the result is rounded to 16; 64 where it is rounded to 4,
 // as an element next to a border between two codes goes by its last bits, and should be held alike wherever it is computed.
 template <typename W, int L, int D, typename T>
-__device__ __forceinline__ void norm_turn(const Run<T>& in, const float (&w)[16], const rkc_rows& r, bool norm, bool turns, const Pair<W>* t, W (&y)[16]) {
+__device__ __forceinline__ void norm_turn(const Run<T>& in, const float* w0, const float* w1, const rkc_rows& r, bool norm, bool turns, const Pair<W>* t, W (&y)[16]) {
 #pragma unroll
   for (int k = 0; k < 8; k++) y[k] = (W)(float)in.a[k], y[8 + k] = (W)(float)in.b[k];
   if (norm) {
@@ -136,7 +136,7 @@ __device__ __forceinline__ void norm_turn(const Run<T>& in, const float (&w)[16]
     for (int k = 0; k < 16; k++) sum = __builtin_fma(y[k], y[k], sum);
     const W by = inverse_root(sum_of<L>(sum) * (W)(1.0 / D) + (W)r.eps);
 #pragma unroll
-    for (int k = 0; k < 16; k++) y[k] = y[k] * by * (W)w[k];
+    for (int k = 0; k < 8; k++) y[k] = y[k] * by * (W)w0[k], y[8 + k] = y[8 + k] * by * (W)w1[k];
   }
   if (!turns) return;
   if (r.interleaved) {
@@ -161,23 +161,22 @@ template <typename T, typename W> __device__ __forceinline__ typename Vec8<T>::t
   return __builtin_convertvector(x, typename Vec8<T>::t);
 }
 
-template <typename T> __device__ __forceinline__ void weights(const rkc_rows& r, const void* norm, int p0, int p1, float (&w)[16]) {
-#pragma unroll
-  for (int k = 0; k < 16; k++) {
-    const int i = 8 * (k < 8 ? p0 : p1) + (k & 7);
-    w[k] = !norm ? 1.f : r.norm_f32 ? ((const float*)norm)[i] : (float)((const T*)norm)[i];
-  }
+// A norm's weights into LDS, ones where there is none.
+template <typename T, int D> __device__ __forceinline__ void weights(const rkc_rows& r, const void* norm, float* to) {
+  for (int i = threadIdx.x; i < D; i += 64 * kWaves) to[i] = !norm ? 1.f : r.norm_f32 ? ((const float*)norm)[i] : (float)((const T*)norm)[i];
 }
 
-constexpr int rows_of(int D) { return D == 256 ? 8 : 16; }  // of a workgroup, at most
+constexpr int rows_of(int D) { return D == 256 ? 8 : 16; }  // of a storing workgroup, at most
+constexpr int kReadRows = 64, kReads = 2;                     // of a reading one; heads that a lane has on their way
 
 template <typename T, int D, typename C>
-__global__ __launch_bounds__(64 * kWaves) void rows_store(const C c, const rkc_rows r, int per, int parts) {
+__global__ __launch_bounds__(64 * kWaves, sizeof(C) == sizeof(rkc_packed) ? 3 : 4) void rows_store(const C c, const rkc_rows r, int per, int parts) {
   constexpr bool packed = sizeof(C) == sizeof(rkc_packed);
   typedef typename std::conditional<packed, double, float>::type W;  // of keys
   typedef typename Vec8<T>::t V8;
   constexpr int L = D / 16, N = 64 / L;  // lanes of a head, heads of a wave
   __shared__ __attribute__((aligned(16))) Pair<W> table[rows_of(D)][D / 2];
+  __shared__ __attribute__((aligned(16))) float qw[D], kw[D];
   __shared__ Place place[rows_of(D)];
   __shared__ __attribute__((aligned(16))) float most[kWaves][N][D / 8];
 
@@ -188,10 +187,33 @@ __global__ __launch_bounds__(64 * kWaves) void rows_store(const C c, const rkc_r
   const int turning = r.n_freq / 8;
   const bool turns = l < turning;
   const int p0 = !turns ? 2 * l : r.interleaved ? 2 * l : l, p1 = !turns || r.interleaved ? 2 * l + 1 : turning + l;
-  float qw[16], kw[16];
-  if (Q) weights<T>(r, r.d_q_norm, p0, p1, qw);
-  weights<T>(r, r.d_k_norm, p0, p1, kw);
 
+  // of a wave at a time: N heads of queries, then of keys and values; those of the next time are on their way
+  const int q_items = rows * Q, kv_items = rows * H, q_turns = (q_items + N - 1) / N, all = q_turns + (kv_items + N - 1) / N;
+  const int step = parts * kWaves;
+  struct Item {
+    int i, h;
+    bool in;
+    Run<T> x, v;
+  };
+  auto fetch = [&](int turn) {
+    Item t;
+    const bool queries = turn < q_turns;
+    const int item = (queries ? turn : turn - q_turns) * N + sub, n = queries ? q_items : kv_items, heads = queries ? Q : H;
+    t.in = item < n, t.i = min(item, n - 1) / heads, t.h = min(item, n - 1) - t.i * heads;
+    const T* from = queries ? (const T*)r.d_q + (row0 + t.i) * r.q_row_stride + t.h * r.q_head_stride
+                            : (const T*)r.d_k + (row0 + t.i) * r.k_row_stride + t.h * r.k_head_stride;
+    t.x = {*(const V8*)(from + 8 * p0), *(const V8*)(from + 8 * p1)};
+    if (!queries) {
+      const T* vf = (const T*)r.d_v + (row0 + t.i) * r.v_row_stride + t.h * r.v_head_stride;
+      t.v = {*(const V8*)(vf + 16 * l), *(const V8*)(vf + 16 * l + 8)};
+    }
+    return t;
+  };
+  int turn = part * kWaves + wave;
+  Item next;
+  if (turn < all) next = fetch(turn);
+  weights<T, D>(r, r.d_q_norm, qw), weights<T, D>(r, r.d_k_norm, kw);
   for (int i = wave; i < rows; i += kWaves) {
     const Place p = place_of(c, r, row0 + i, false);
     if (lane == 0) place[i] = p;
@@ -210,35 +232,29 @@ __global__ __launch_bounds__(64 * kWaves) void rows_store(const C c, const rkc_r
   }
   __syncthreads();
 
-  // of a wave at a time: N heads of queries, then of keys and values
-  const int q_items = rows * Q, kv_items = rows * H, q_turns = (q_items + N - 1) / N, all = q_turns + (kv_items + N - 1) / N;
-  for (int turn = part * kWaves + wave; turn < all; turn += parts * kWaves) {
+  for (; turn < all; turn += step) {
+    const Item now = next;
+    if (turn + step < all) next = fetch(turn + step);
+    const Place p = place[now.i];
+    const int i = now.i, h = now.h;
     if (turn < q_turns) {
-      const int item = turn * N + sub, i = min(item, q_items - 1) / Q, h = item - i * Q;
-      if (item < q_items && place[i].known) {
-        const T* from = (const T*)r.d_q + (row0 + i) * r.q_row_stride + h * r.q_head_stride;
-        const Run<T> in = {*(const V8*)(from + 8 * p0), *(const V8*)(from + 8 * p1)};
+      if (now.in && p.known) {
         Pair<float> t[8];
         if (turns) {
 #pragma unroll
           for (int k = 0; k < 8; k++) t[k] = {(float)table[i][8 * l + k].c, (float)table[i][8 * l + k].s};
         }
         float y[16];
-        norm_turn<float, L, D>(in, qw, r, r.d_q_norm, turns, t, y);
+        norm_turn<float, L, D>(now.x, qw + 8 * p0, qw + 8 * p1, r, r.d_q_norm, turns, t, y);
         T* to = (T*)r.d_q_out + (row0 + i) * r.q_out_row_stride + h * r.q_out_head_stride;
         *(V8*)(to + 8 * p0) = rounded<T>(y), *(V8*)(to + 8 * p1) = rounded<T>(y + 8);
       }
       continue;
     }
-    const int item = (turn - q_turns) * N + sub, i = min(item, kv_items - 1) / H, h = item - i * H;
-    const Place p = place[i];
-    if (item >= kv_items || p.block < 0) continue;  // the same for a head's lanes
-    const T* kf = (const T*)r.d_k + (row0 + i) * r.k_row_stride + h * r.k_head_stride;
-    const T* vf = (const T*)r.d_v + (row0 + i) * r.v_row_stride + h * r.v_head_stride;
-    const Run<T> in = {*(const V8*)(kf + 8 * p0), *(const V8*)(kf + 8 * p1)};
-    const Run<T> vin = {*(const V8*)(vf + 16 * l), *(const V8*)(vf + 16 * l + 8)};
+    if (!now.in || p.block < 0) continue;  // the same for a head's lanes
+    const Run<T> vin = now.v;
     W y[16];
-    norm_turn<W, L, D>(in, kw, r, r.d_k_norm, turns, &table[i][8 * l], y);
+    norm_turn<W, L, D>(now.x, kw + 8 * p0, kw + 8 * p1, r, r.d_k_norm, turns, &table[i][8 * l], y);
     if constexpr (!packed) {
       T* kt = key_at<T>(c, p, h);
       T* vt = value_at<T>(c, p, h);
@@ -280,8 +296,8 @@ __global__ __launch_bounds__(64 * kWaves) void rows_store(const C c, const rkc_r
 template <typename T, int D, typename C>
 __global__ __launch_bounds__(64 * kWaves) void rows_read(const C c, const rkc_rows r, int per, int parts) {
   constexpr bool packed = sizeof(C) == sizeof(rkc_packed);
-  constexpr int L = D / 8, N = 64 / L, U = 4;  // lanes of a head, heads of a wave, loads on their way
-  __shared__ Place place[16];
+  constexpr int E = 8, L = D / E, N = 64 / L, U = kReads;  // elements of a lane, lanes of a head, heads of a wave, heads on their way
+  __shared__ Place place[kReadRows];
   const int H = c.kv_heads, lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), l = lane % L, sub = lane / L;
   const int part = blockIdx.x % parts, row0 = blockIdx.x / parts * per, rows = min(per, r.n_rows - row0);
   for (int i = wave; i < rows; i += kWaves) {
@@ -289,32 +305,33 @@ __global__ __launch_bounds__(64 * kWaves) void rows_read(const C c, const rkc_ro
     if (lane == 0) place[i] = p;
   }
   __syncthreads();
-  // heads of keys, then of values, of a row after the other
-  const int items = rows * 2 * H, step = parts * kWaves * N;
+  // a head's key and value of a row by L lanes, N of them at a time
+  const int items = rows * H, step = parts * kWaves * N;
   for (int first = (part * kWaves + wave) * N + sub; first < items; first += U * step) {
-    u32x4 x[U];
+    u32x4 x[U][2];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int item = min(first + u * step, items - 1), i = item / (2 * H), h = item % (2 * H), v = h >= H;
+      const int item = min(first + u * step, items - 1), i = item / H, h = item - i * H;
       const Place p = place[i];
       if (p.block < 0) continue;
       if constexpr (packed) {
-        const Held from = held_at<D>(c, p, h - v * H);
-        const uint32_t codes = *(const uint32_t*)(from.codes + v * from.v_at + 4 * l);
-        const uint32_t scale = *(const uint8_t*)(from.scales + v * from.s_at + (l >> 2)), mark = *(const uint8_t*)from.scales;
-        x[u] = unpack8<T>(codes, scale_float(mark == kMark ? kMark : scale));
+        const Held from = held_at<D>(c, p, h);
+        const uint32_t k = *(const uint32_t*)(from.codes + E / 2 * l), v = *(const uint32_t*)(from.codes + from.v_at + E / 2 * l);
+        const uint32_t ks = *(const uint8_t*)(from.scales + E * l / 32), vs = *(const uint8_t*)(from.scales + from.s_at + E * l / 32);
+        const bool mark = *(const uint8_t*)from.scales == kMark;
+        x[u][0] = unpack8<T>(k, scale_float(mark ? kMark : ks)), x[u][1] = unpack8<T>(v, scale_float(mark ? kMark : vs));
       } else {
-        x[u] = *(const u32x4*)((v ? value_at<T>(c, p, h - H) : key_at<T>(c, p, h)) + 8 * l);
+        x[u][0] = *(const u32x4*)(key_at<T>(c, p, h) + 8 * l), x[u][1] = *(const u32x4*)(value_at<T>(c, p, h) + 8 * l);
       }
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const int item = first + u * step;
       if (item >= items) break;
-      const int i = item / (2 * H), h = item % (2 * H), v = h >= H;
+      const int i = item / H, h = item - i * H;
       if (place[i].block < 0) continue;
-      T* to = v ? (T*)r.d_v + (row0 + i) * r.v_row_stride + (h - H) * r.v_head_stride : (T*)r.d_k + (row0 + i) * r.k_row_stride + h * r.k_head_stride;
-      *(u32x4*)(to + 8 * l) = x[u];
+      *(u32x4*)((T*)r.d_k + (row0 + i) * r.k_row_stride + h * r.k_head_stride + 8 * l) = x[u][0];
+      *(u32x4*)((T*)r.d_v + (row0 + i) * r.v_row_stride + h * r.v_head_stride + 8 * l) = x[u][1];
     }
   }
 }
@@ -360,15 +377,18 @@ rkc_status rows_check(const rkc_rows* r, int n_seqs, int64_t cap, int heads, int
   return RKC_OK;
 }
 
-// Rows of a workgroup, and workgroups that share them: as many rows as leave four workgroups a CU, and a few rows' heads
-// over as many workgroups.
+// Rows of a workgroup, and workgroups that share them: as many rows, up to `most`, as leave four workgroups a CU, and a few
+// rows' heads over as many workgroups.  (12,300 rows of 48 heads stored, 8 rows a workgroup: 66 us; 2 rows 72, 16 rows 71.)
+// Reading, a workgroup has the rows whose heads its lanes take at once, twice: fewer rows are all start, and more keep their
+// loads waiting for the stores before them (258,000 rows of 4 heads of 256 elements, 4 rows: 281 us; 2 rows 369, 8 rows 292,
+// 64 rows 325; 157,000 of 8 heads of 64, 8 rows: 104; 4 rows 126, 16 rows 109).
 struct Cut {
   int per, parts;
   int64_t workgroups;
 };
 Cut cut_of(int rows, int most, int64_t turns_of_a_row) {
   Cut k = {1, 1, 0};
-  while (k.per < most && rows / (2 * k.per) >= 1024) k.per *= 2;
+  while (2 * k.per <= most && rows / (2 * k.per) >= 1024) k.per *= 2;
   const int64_t waves = (turns_of_a_row + kWaves - 1) / kWaves;
   if (k.per == 1) k.parts = (int)(1024 / rows < 1 ? 1 : 1024 / rows < waves ? 1024 / rows : waves);
   k.workgroups = (int64_t)((rows + k.per - 1) / k.per) * k.parts;
@@ -376,8 +396,9 @@ Cut cut_of(int rows, int most, int64_t turns_of_a_row) {
 }
 
 template <typename T, int D, typename C> rkc_status go(const C* c, const rkc_rows* r, bool read, hipStream_t s) {
-  const int Q = r->d_q ? r->q_heads : 0, H = c->kv_heads, n = 1024 / D, m = 512 / D;
-  const Cut k = cut_of(r->n_rows, rows_of(D), read ? (2 * H + m - 1) / m : (Q + n - 1) / n + (H + n - 1) / n);
+  const int Q = r->d_q ? r->q_heads : 0, H = c->kv_heads, n = 1024 / D, m = 512 / D, at_once = kReads * kWaves * m / H;
+  const Cut k = read ? cut_of(r->n_rows, at_once < kReadRows ? at_once : kReadRows, (H + m - 1) / m)
+                     : cut_of(r->n_rows, rows_of(D), (Q + n - 1) / n + (H + n - 1) / n);
   if (!rkc_fits(k.workgroups, 64 * kWaves)) return RKC_E_UNSUPPORTED;
   const dim3 grid((unsigned)k.workgroups), block(64 * kWaves);
   if (read) rows_read<T, D, C><<<grid, block, 0, s>>>(*c, *r, k.per, k.parts);

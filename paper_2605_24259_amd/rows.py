@@ -27,18 +27,23 @@ class RowOps:
 
     _store, _read = "rkc_store", "rkc_read"
 
-    def _heads_of(self, t, name, rows=None):
-        """A tensor of rows: its strides, of a dimension of one 0, as they say nothing."""
-        if t.dim() != 3 or t.shape[2] != self.head_dim or t.dtype is not self.dtype or t.get_device() != self._index or \
-                t.stride(2) != 1 or (rows is not None and (t.shape[0] != rows or t.shape[1] != self.kv_heads)):
-            raise ValueError(f"{name}: [{'rows' if rows is None else rows}, {'heads' if rows is None else self.kv_heads}, "
-                             f"{self.head_dim}] of {self.dtype} on {self.device}, the last dimension contiguous, is wanted, got "
+    def _heads_of(self, t, name, shape):
+        """Strides of a tensor of rows, of a dimension of one 0, as they say nothing."""
+        at, heads, last = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if last != 1 or t.shape != shape or t.dtype is not self.dtype or t.get_device() != self._index:
+            raise ValueError(f"{name}: {tuple(shape)} of {self.dtype} on {self.device}, the last dimension contiguous, is wanted, got "
                              f"{t.dtype} {tuple(t.shape)} on {t.device}")
-        n, h, _ = t.shape
-        return t.stride(0) if n > 1 else 0, t.stride(1) if h > 1 else 0
+        return at if shape[0] > 1 else 0, heads if shape[1] > 1 else 0
 
-    def _run_rows(self, f, r, stream):
-        st = getattr(self._lib, f)(self._c_ref, ctypes.byref(r), self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
+    def _norm_of(self, t, name, kind):
+        if t.dtype is not kind or (kind is not self.dtype and kind is not self._torch.float32) or t.get_device() != self._index or \
+                t.shape != (self.head_dim,) or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous tensor [{self.head_dim}] of {self.dtype} or float32 (both norms alike) on "
+                             f"{self.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _run_rows(self, f, args, stream):
+        st = getattr(self._lib, f)(self._c_ref, ctypes.byref(_Rows(*args)), self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
         if st != 0:
             raise RkcError(st, f)
 
@@ -62,60 +67,62 @@ class RowOps:
         Returns the queries (q_out or a new tensor), or None without q.  A cache of 4 bits rounds keys and values as they
         are written; keys are computed in 64 bits up to that.
         """
-        n, torch = k.shape[0], self._torch
-        r = _Rows()
-        r.k_row_stride, r.k_head_stride = self._heads_of(k, "k", n)
-        r.v_row_stride, r.v_head_stride = self._heads_of(v, "v", n)
-        r.n_rows, r.max_len, r.eps, r.interleaved, r.axes = n, self.max_len, eps, bool(interleaved), 1
-        r.d_k, r.d_v = k.data_ptr(), v.data_ptr()
-        r.d_row_offset, r.d_length = self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)
+        torch = self._torch
+        shape = (k.shape[0] if k.dim() else 0, self.kv_heads, self.head_dim)
+        n = shape[0]
+        k_at, k_heads = self._heads_of(k, "k", shape)
+        v_at, v_heads = self._heads_of(v, "v", shape)
+        offsets, lengths = self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)
+        f32, qn, kn = False, None, None
         if q_norm is not None or k_norm is not None:
             kind = (k_norm if q_norm is None else q_norm).dtype
-            for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-                if t is not None and (t.dtype is not kind or (kind is not self.dtype and kind is not torch.float32) or t.get_device() != self._index
-                                      or not t.is_contiguous() or tuple(t.shape) != (self.head_dim,)):
-                    raise ValueError(f"{name}: a contiguous tensor [{self.head_dim}] of {self.dtype} or float32 (both norms alike) on "
-                                     f"{self.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-            r.norm_f32 = kind is torch.float32
-            r.d_q_norm = None if q_norm is None else q_norm.data_ptr()
-            r.d_k_norm = None if k_norm is None else k_norm.data_ptr()
+            f32 = kind is torch.float32
+            if q_norm is not None:
+                qn = self._norm_of(q_norm, "q_norm", kind)
+            if k_norm is not None:
+                kn = self._norm_of(k_norm, "k_norm", kind)
+        pairs, freqs, axes, positions, axis_of = 0, None, 1, None, None
         if freq is not None:
-            if freq.dtype is not torch.float32 or freq.get_device() != self._index or freq.dim() != 1 or not freq.is_contiguous() or \
-                    freq.shape[0] % 8 or freq.shape[0] > self.head_dim // 2:
+            pairs = freq.shape[0] if freq.dim() == 1 else -1
+            if freq.dtype is not torch.float32 or freq.get_device() != self._index or pairs % 8 or not 0 <= 2 * pairs <= self.head_dim or \
+                    not freq.is_contiguous():
                 raise ValueError(f"freq: a contiguous float32 tensor of 8, 16, ... {self.head_dim // 2} values on {self.device} is wanted, "
                                  f"got {freq.dtype} {tuple(freq.shape)} on {freq.device}")
-            r.n_freq, r.d_freq = freq.shape[0], freq.data_ptr()
+            freqs = freq.data_ptr()
         if position is not None:
-            if position.dtype is not torch.int32 or position.get_device() != self._index or not position.is_contiguous() or \
-                    position.dim() not in (1, 2) or position.shape[-1] != n or (position.dim() == 2 and not 1 <= position.shape[0] <= MAX_AXES):
+            of = position.shape
+            if len(of) == 2:
+                axes = of[0]
+            if position.dtype is not torch.int32 or position.get_device() != self._index or len(of) not in (1, 2) or of[-1] != n or \
+                    not 1 <= axes <= MAX_AXES or not position.is_contiguous():
                 raise ValueError(f"position: a contiguous int32 tensor [{n}] or [up to {MAX_AXES}, {n}] on {self.device} is wanted, got "
-                                 f"{position.dtype} {tuple(position.shape)} on {position.device}")
-            r.d_position = position.data_ptr()
-            if position.dim() == 2:
-                r.axes = position.shape[0]
+                                 f"{position.dtype} {tuple(of)} on {position.device}")
+            positions = position.data_ptr()
         if axis is not None:
             if position is None or freq is None:
                 raise ValueError("axis: there are several axes only of given positions and frequencies")
-            r.d_axis = self._ints(axis, "axis", r.n_freq)
-        elif r.axes > 1 and freq is not None:
-            raise ValueError(f"position: of {r.axes} axes, axis has to say which one each of the {r.n_freq} pairs turns by")
-        elif r.axes > 1:
-            r.axes, r.d_position = 1, None  # nothing turns
-        if q is None:
-            if q_norm is not None or q_out is not None:
-                raise ValueError("q_norm and q_out are of queries, and there are none")
-        else:
-            if q.shape[0] != n:
-                raise ValueError(f"q: {q.shape[0]} rows, and {n} of k")
-            r.q_row_stride, r.q_head_stride = self._heads_of(q, "q")
-            with self._on(stream):
-                if q_out is None:
-                    q_out = q.new_empty(q.shape)
-                elif q_out.shape != q.shape:
-                    raise ValueError(f"q_out: {tuple(q_out.shape)}, and q is {tuple(q.shape)}")
-            r.q_out_row_stride, r.q_out_head_stride = self._heads_of(q_out, "q_out")
-            r.q_heads, r.d_q, r.d_q_out = q.shape[1], q.data_ptr(), q_out.data_ptr()
-        self._run_rows(self._store, r, stream)
+            axis_of = self._ints(axis, "axis", pairs)
+        elif axes > 1 and pairs:
+            raise ValueError(f"position: of {axes} axes, axis has to say which one each of the {pairs} pairs turns by")
+        elif axes > 1:
+            axes, positions = 1, None  # nothing turns
+        heads, queries, outs, q_at, q_heads, out_at, out_heads = 0, None, None, 0, 0, 0, 0
+        if q is not None:
+            heads = q.shape[1] if q.dim() == 3 else 0
+            shape = (n, heads, self.head_dim)
+            q_at, q_heads = self._heads_of(q, "q", shape)
+            if q_out is None:
+                with self._on(stream):
+                    q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                out_at, out_heads = heads * self.head_dim, self.head_dim
+            else:
+                out_at, out_heads = self._heads_of(q_out, "q_out", shape)
+            queries, outs = q.data_ptr(), q_out.data_ptr()
+        elif q_norm is not None or q_out is not None:
+            raise ValueError("q_norm and q_out are of queries, and there are none")
+        self._run_rows(self._store, (n, heads, self.max_len, pairs, axes, interleaved, f32, eps, k_at, k_heads, v_at, v_heads, q_at, q_heads,
+                                     out_at, out_heads, k.data_ptr(), v.data_ptr(), queries, outs, offsets, lengths, positions, axis_of,
+                                     freqs, qn, kn), stream)
         return q_out
 
     def read(self, row_offset, length, *, rows, k=None, v=None, stream=None):
@@ -126,15 +133,17 @@ class RowOps:
         rows        of the tensors, >= row_offset[seqs]; those behind the last sequence are left as they are
         k, v        take the rows (default: new tensors)
         """
-        r = _Rows()
-        with self._on(stream):
-            if k is None:
-                k = self._torch.empty(rows, self.kv_heads, self.head_dim, dtype=self.dtype, device=self.device)
-            if v is None:
-                v = self._torch.empty(rows, self.kv_heads, self.head_dim, dtype=self.dtype, device=self.device)
-        r.k_row_stride, r.k_head_stride = self._heads_of(k, "k", rows)
-        r.v_row_stride, r.v_head_stride = self._heads_of(v, "v", rows)
-        r.n_rows, r.max_len, r.d_k, r.d_v = rows, self.max_len, k.data_ptr(), v.data_ptr()
-        r.d_row_offset, r.d_length = self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)
-        self._run_rows(self._read, r, stream)
+        shape, torch = (rows, self.kv_heads, self.head_dim), self._torch
+        if k is None or v is None:
+            with self._on(stream):
+                strides = (self.kv_heads * self.head_dim, self.head_dim, 1)
+                if k is None:
+                    k = torch.empty_strided(shape, strides, dtype=self.dtype, device=self.device)
+                if v is None:
+                    v = torch.empty_strided(shape, strides, dtype=self.dtype, device=self.device)
+        k_at, k_heads = self._heads_of(k, "k", shape)
+        v_at, v_heads = self._heads_of(v, "v", shape)
+        self._run_rows(self._read, (rows, 0, self.max_len, 0, 1, 0, 0, 0.0, k_at, k_heads, v_at, v_heads, 0, 0, 0, 0, k.data_ptr(), v.data_ptr(),
+                                    None, None, self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)),
+                       stream)
         return k, v
