@@ -12,6 +12,8 @@
 // both for the next 32 slots are in flight while these are worked on.
 // A marked slot's scores are NaN by its key's first scale, and so only the rows that see it; values are always finite, so that
 // one that a row does not see meets a weight of zero and gives zero.
+#include <type_traits>
+
 #include "rkc_packed_dev.h"
 #include "rkc_tiles.h"
 
@@ -122,19 +124,17 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void packed_few(cons
   const uint32_t k_off = col * (D / 2) + quad * (D / 8), v_off = lane * (D / 8);
   const uint32_t ks_off = col * (D / 32) + quad * (D / 32) / 4 * (D >= 128) + (D == 64 ? quad >> 1 : 0);
   const uint32_t vs_off = v_slot * (D / 32) + v_quad * (D / 32) / 4 * (D >= 128) + (D == 64 ? v_quad >> 1 : 0);
-  auto scales = [](const char* p) { return NS == 2 ? (uint32_t) * (const uint16_t*)p : (uint32_t) * (const uint8_t*)p; };
+  typedef typename std::conditional<NS == 2, uint16_t, uint8_t>::type scales_t;
   auto load = [&](int i) {
     const int t0 = slot_of(i);
 #pragma unroll
     for (int u = 0; u < 2; u++) {
       const int at = run_of(t0, u) & in_page;
-      const char* b = held.base + block_of(c, page[u], bad) * held.block;
-      const char* kb = fixed(b + at * (D / 2));
-      const char* sb = fixed(b + held.key_scales + at * (D / 32));
-      kf[u] = *(const codes_t*)(kb + k_off);
-      vf[u] = *(const codes_t*)(kb + held.values + v_off);
-      ks[u] = scales(sb + ks_off);
-      vs[u] = scales(sb + (held.value_scales - held.key_scales) + vs_off);
+      const char* b = held.base + (uint64_t)(uint32_t)block_of(c, page[u], bad) * held.block;
+      const char* kb = b + at * (D / 2);
+      const char* sb = b + held.key_scales + at * (D / 32);
+      kf[u] = from_global<codes_t>(kb, k_off), vf[u] = from_global<codes_t>(kb + held.values, v_off);
+      ks[u] = from_global<scales_t>(sb, ks_off), vs[u] = from_global<scales_t>(sb + (held.value_scales - held.key_scales), vs_off);
     }
   };
   auto scale_k = [](uint32_t s, int k) { return scale_float(NS == 2 ? s >> 8 * (k / 4) & 255 : s); };
@@ -292,12 +292,13 @@ rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   rkc_plan p = {};
   const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
   p.few = M <= 16;
-  p.rows = p.few ? 16 : 128;
+  const int64_t wide = (int64_t)c->n_seqs * c->kv_heads * ((M + 255) / 256) * ((a->max_len + 255) / 256);
+  p.rows = p.few ? 16 : M <= 128 || c->head_dim == 64 || wide < 512 ? 128 : 256;
   p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
   const bool wide_head = c->head_dim == 256;
-  const int64_t want = wide_head ? 256 : p.few ? 10 * 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
+  const int64_t want = wide_head || p.rows == 256 ? 256 : p.few ? 10 * 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;

@@ -27,12 +27,18 @@ __device__ __forceinline__ float scale_float(uint32_t b) { return __uint_as_floa
 // Of a head of a cache of 4 bits as rkc_packed_as_cache has it: a block's keys' codes; values' codes and both scales lie behind.
 struct Codes {
   const char* base;
-  int64_t block;
+  uint32_t block;
   int values, key_scales, value_scales;  // bytes from the keys' codes on
 };
 template <int D> __device__ __forceinline__ Codes codes_of(const rkc_cache& c, int h) {
   const int n = code_bytes(c.page_tokens, D);
-  return {(const char*)c.d_k + h * c.k_head_stride, c.k_block_stride, n, 2 * n, 2 * n + scale_bytes(c.page_tokens, D)};
+  return {(const char*)c.d_k + h * c.k_head_stride, (uint32_t)c.k_block_stride, n, 2 * n, 2 * n + scale_bytes(c.page_tokens, D)};
+}
+
+// Memory at a lane's offset from a pointer in scalar registers, told to be global: a load of any memory would be waited for
+// with those of LDS.
+template <typename V> __device__ __forceinline__ V from_global(const char* p, uint32_t offset) {
+  return *(const __attribute__((address_space(1))) V*)((const __attribute__((address_space(1))) char*)fixed(p) + (uint32_t)here((int)offset));
 }
 
 // Two codes of a byte as T, times the scale: exact, as a scaled code has two bits of mantissa.
@@ -61,7 +67,7 @@ rkc_status rkc_packed_check(const rkc_packed* c);
 // The cache as the attention's shared code takes it: its counts, table and status, the pool as the keys.
 rkc_cache rkc_packed_as_cache(const rkc_packed* c);
 rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a);
-inline int rkc_packed_lanes(const rkc_cache* c, const rkc_plan* p) { return 64 * (p->few ? p->waves : p->rows == 256 || c->head_dim == 256 ? 8 : 4); }
+inline int rkc_packed_lanes(const rkc_cache* c, const rkc_plan* p) { return 64 * (p->few ? p->waves : p->rows == 256 ? 8 : 4); }
 rkc_status rkc_packed_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 rkc_status rkc_packed_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 

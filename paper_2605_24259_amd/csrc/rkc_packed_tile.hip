@@ -1,7 +1,7 @@
 // rkc_packed_tile.hip -- attention of many rows over a paged cache in 4 bits (chunks of prompts, larger trees).
 //
 // out = sum_j exp(x_j - m) v_j / sum_j exp(x_j - m) in one pass over the slots, m the running maximum of a row's scores.
-// A workgroup of W waves holds R W packed rows (rows x query heads of one key/value head), R of them in each wave as the
+// A workgroup of W waves holds 32 W packed rows (rows x query heads of one key/value head), 32 of them in each wave as the
 // columns of its matrix products, and goes over the slots that any of them sees in tiles of 64 (32 at 256 elements a
 // head).  A tile's codes and scales are loaded one tile ahead into registers, a thread's part of it each, and converted once
 // for all waves into 16 bits in LDS, while the tile before is worked on.  Tiles that every row sees skip the masks, waves whose
@@ -14,18 +14,14 @@
 
 namespace {
 
-template <int R> struct Acc;
-template <> struct Acc<32> { typedef f32x16 t; };
-template <> struct Acc<16> { typedef f32x4 t; };
-
-template <typename T, int D, int W, int R>
-__global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+template <typename T, int D, int W>
+__global__ __launch_bounds__(64 * W, D == 64 ? 3 : D == 256 && W == 4 ? 1 : 2) void packed_tile(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
-  // R rows a wave: products of R x R, A elements a lane; tiles of BK slots, kAhead of them on their way
-  typedef typename Acc<R>::t acc;
-  constexpr int A = R * R / 64, kRows = R * W, kThreads = 64 * W;
+  // 32 rows a wave: products of 32 x 32, A elements a lane; tiles of BK slots
+  typedef f32x16 acc;
+  constexpr int A = 16, kRows = 32 * W, kThreads = 64 * W;
   constexpr int BK = D == 256 ? 32 : 64;
-  constexpr int KT = BK / R, KC = D * R / 512, DB = D / R, NP = KT * A / 8;  // score blocks, key operands, output blocks, weight operands
+  constexpr int KT = BK / 32, KC = D / 16, DB = D / 32, NP = KT * 2;  // score blocks, key operands, output blocks, weight operands
   constexpr int E = BK * D / kThreads, PER = D / E, NC = E / 8;  // elements of a key, and of a value, per thread; threads of a slot; dwords
   constexpr int kTile = BK * D;
   __shared__ __attribute__((aligned(16))) T lds[2 * 2 * kTile];  // K and V of two tiles
@@ -38,7 +34,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
   // 334, documents 57 instead of 49; sequences before row tiles: 455 and 62.)
   const int h = blockIdx.x % H, split = blockIdx.x / H % pl.splits, b = blockIdx.x / (H * pl.splits);
   const int qt = pl.tiles - 1 - b % pl.tiles, s = pl.sorted ? seq_of_rank(c, a, b / pl.tiles) : b / pl.tiles;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), grp = lane / R, col = lane % R;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), grp = lane / 32, col = lane % 32;
   // which rows are the wave's: neighbours work in turns on one SIMD, also where a tile is not full
   const int part = W == 8 ? (wave & 3) * 2 + (wave >> 2) : wave;
   const Seq q = load_seq(c, a, s);
@@ -54,8 +50,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
-  const int m = min(m0 + R * part + col, M - 1), qi = m / G, qh = h * G + m % G;
-  const bool mine = m0 + R * part + col < M, rows = m0 + R * part < M;
+  const int m = min(m0 + 32 * part + col, M - 1), qi = m / G, qh = h * G + m % G;
+  const bool mine = m0 + 32 * part + col < M, rows = m0 + 32 * part < M;
   const Scale f = load_scale(a);
   Row row = load_row(a, q, s, qi);
   const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
@@ -64,7 +60,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
     const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + grp * 8;
 #pragma unroll
     for (int k = 0; k < KC; k++) {
-      qf[k] = *(const V8*)(p + 512 / R * k);
+      qf[k] = *(const V8*)(p + 16 * k);
       if (f.negate) qf[k] = negated(qf[k]);
     }
   }
@@ -77,7 +73,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
   int all_from = 0, any_from = 0;
   if (a.d_row_start) all_from = wave_max(row.start), any_from = wave_min(row.start);
   const int all_to = uni(row.end), pre = uni(row.prefix);  // a wave's first lane has its first row
-  const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, R - 1));
+  const int any_to = tree ? q.len : max(pre, __builtin_amdgcn_readlane(row.end, 31));
   if (lane == 0) lim[wave][0] = any_from, lim[wave][1] = any_to;
   __syncthreads();
   int g_any_from = lim[0][0], g_any_to = lim[0][1];
@@ -101,11 +97,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
   bool bad = false;
   // this thread's part of a tile: a wave's parts lie in 16 slots of one page
   static_assert(64 / PER <= 16, "runs");
-  const int mine_slot = tid / PER, lane_run = uni(mine_slot & ~15), part_of = tid % PER;
-  auto key_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : keys16_at<D>(r, c); };
-  auto val_in = [](int r, int c) { return R == 32 ? tile_at<D>(r, c) : vals16_at<D>(r, c); };
+  const int lane_run = uni(tid / PER & ~15);
+  // What follows from the thread's number is found anew where it is used, where 256 registers are not enough to keep it.
+  auto self = [&] { return D == 256 && W == 8 ? here(tid) : tid; };
   typedef uint32_t codes_t __attribute__((ext_vector_type(NC)));
-  const uint32_t c_off = (mine_slot & 15) * (D / 2) + part_of * (E / 2), s_off = (mine_slot & 15) * (D / 32) + part_of * E / 32;
   codes_t kf, vf;   // of the next tile
   uint32_t ks, vs;
   int page;         // of the one behind it
@@ -116,40 +111,52 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
   auto look_up = [&](int i) { page = page_of(table, shift, run_of(slot_of(i))); };
   auto load = [&](int i) {
     const int at = run_of(slot_of(i)) & in_page;
-    const char* b = held.base + block_of(c, page, bad) * held.block;
-    const char* kb = fixed(b + at * (D / 2));
-    const char* sb = fixed(b + held.key_scales + at * (D / 32));
-    kf = *(const codes_t*)(kb + c_off);
-    vf = *(const codes_t*)(kb + held.values + c_off);
-    ks = *(const uint8_t*)(sb + s_off);
-    vs = *(const uint8_t*)(sb + (held.value_scales - held.key_scales) + s_off);
+    const char* b = held.base + (uint64_t)(uint32_t)block_of(c, page, bad) * held.block;
+    const char* kb = b + at * (D / 2);
+    const char* sb = b + held.key_scales + at * (D / 32);
+    const int t = self() & (16 * PER - 1), c_off = t * (E / 2), s_off = t / PER * (D / 32) + t % PER * E / 32;
+    kf = from_global<codes_t>(kb, c_off), vf = from_global<codes_t>(kb + held.values, c_off);
+    ks = from_global<uint8_t>(sb, s_off), vs = from_global<uint8_t>(sb + (held.value_scales - held.key_scales), s_off);
   };
-  const int put_k = 2 * key_in(mine_slot, part_of * NC), put_v = 2 * (kTile + val_in(mine_slot, part_of * NC));
-  auto put = [&](int buf) {
-    const int pk = here(put_k + buf * 4 * kTile), pv = here(put_v + buf * 4 * kTile);
-    const float fk = scale_float(ks), fv = scale_float(min(vs, (uint32_t)kTopScale<T>));
+  // byte offset of this thread's part in a tile
+  auto put_at = [&] {
+    const int t = self();
+    return 2 * tile_at<D>(t / PER, t % PER * NC);
+  };
+  auto put_keys = [&](int buf) {
+    const int at = here(put_at() + buf * 4 * kTile);
+    const float f = scale_float(ks);
 #pragma unroll
-    for (int k = 0; k < NC; k++) {
-      *(u32x4*)((char*)lds + (pk ^ k << 4)) = unpack8<T>(kf[k], fk);
-      *(u32x4*)((char*)lds + (pv ^ k << 4)) = unpack8<T>(vf[k], fv);
-    }
+    for (int k = 0; k < NC; k++) *(u32x4*)((char*)lds + (at ^ k << 4)) = unpack8<T>(kf[k], f);
   };
-  // byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along
-  // a row) and by whole rows.  Element e = 4 x + y of a score block is slot 4 * (64 / R) x + 4 grp + y of its R.
-  const int vi = lane & 15, vr = 4 * grp + (vi >> 2), vc = R == 32 ? (lane >> 4 & 1) * 2 + ((vi & 3) >> 1) : (vi & 3) >> 1, ve = (vi & 1) * 4;
-  const int key_at = 2 * key_in(col, grp), val_at = 2 * (kTile + val_in(vr, vc) + ve);
+  // a scale that nobody wrote may be anything: what no row sees is to be finite
+  auto put_values = [&](int buf, const codes_t& codes, uint32_t scale) {
+    const int at = here(put_at() + 2 * kTile + buf * 4 * kTile);
+    const float f = scale_float(min(scale, (uint32_t)kTopScale<T>));
+#pragma unroll
+    for (int k = 0; k < NC; k++) *(u32x4*)((char*)lds + (at ^ k << 4)) = unpack8<T>(codes[k], f);
+  };
+  // Byte offsets of a lane's first key and first values of a tile; the others differ by an exclusive or (chunks along a row) and
+  // by whole rows.  Element e = 4 x + y of a score block is slot 8 x + 4 grp + y of its 32.
+  auto key_at = [&] {
+    const int t = self() & 63;
+    return 2 * tile_at<D>(t % 32, t / 32);
+  };
+  auto val_at = [&] {
+    const int t = self() & 63, i = t & 15;
+    return 2 * (kTile + tile_at<D>(4 * (t / 32) + (i >> 2), (t >> 4 & 1) * 2 + ((i & 3) >> 1)) + (i & 1) * 4);
+  };
   // whether any of the wave's rows sees anything of a tile, and whether all see all of it
   auto sees = [&](int t0) { return rows && ((t0 + BK > any_from && t0 < any_to) || t0 < pre); };
-  auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k * (1024 / R)) + 2 * R * D * u); };
-  // values of the 512 / R slots of weight operand i, columns R d .. R d + R - 1
+  auto keys = [&](int ka, int u, int k) { return *(const V8*)((const char*)lds + (ka ^ k * 32) + 64 * D * u); };
+  // values of the 16 slots of weight operand i, columns 32 d .. 32 d + 31
   auto vals = [&](int va, int i, int d) {
-    const char* at = (const char*)lds + i * (512 / R) * 2 * D;
-    const int x = va ^ d * 2 * R;
-    if constexpr (R == 32) return read_tr2<T>(at + x, at + (x ^ 32) + 16 * D);
-    else return read_tr2<T>(at + x, at + x + 32 * D);
+    const char* at = (const char*)lds + i * 32 * D;
+    const int x = va ^ d * 64;
+    return read_tr2<T>(at + x, at + (x ^ 32) + 16 * D);
   };
   auto scores = [&](acc(&sc)[KT], int buf) {
-    const int ka = here(buf * 4 * kTile + key_at);
+    const int ka = here(buf * 4 * kTile + key_at());
 #pragma unroll
     for (int u = 0; u < KT; u++)
 #pragma unroll
@@ -159,11 +166,26 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
 #pragma unroll
       for (int u = 0; u < KT; u++) sc[u] = mma(keys(ka, u, k), qf[k], sc[u]);
   };
-  auto slot_in = [](int u, int k) { return R * u + (k & 3) + 256 / R * (k >> 2); };  // less 4 grp
+  // A cap without a distance stays -1 / (exp(2 y) + 1), half of tanh(y) less a half: the exponent's factor and the maximum take
+  // up the rest, which saves an operation a score.
+  const bool short_cap = a.softcap > 0.f && !f.far && !a.d_slope;
+  const float times = short_cap ? 2.f * f.post : f.post, plus = short_cap ? f.post : 0.f;
+  auto each = [](acc(&sc)[KT], auto f) {
+#pragma unroll
+    for (int u = 0; u < KT; u++)
+#pragma unroll
+      for (int k = 0; k < A; k++) sc[u][k] = f(sc[u][k]);
+  };
+  auto slot_in = [](int u, int k) { return 32 * u + (k & 3) + 8 * (k >> 2); };  // less 4 grp
   // cap, distance, masks, and the maximum that the weights refer to
-  auto fold = [&](acc(&sc)[KT], uint32_t(&seen)[BK / 32], int t0) {
+  auto fold = [&](acc(&sc)[KT], int t0) {
     const bool whole = t0 + BK <= pre || (t0 >= all_from && t0 + BK <= all_to);
-    if (a.softcap > 0.f) cap_all(sc, f);
+    if (short_cap) {
+      each(sc, [&](float y) { return ex2(y * f.pre); });
+      each(sc, [&](float y) { return __builtin_amdgcn_rcpf(-1.f - y); });
+    } else if (a.softcap > 0.f) {
+      cap_all(sc, f);
+    }
     if (a.d_slope && t0 + BK <= all_to) {  // all slots lie before all rows: the part that is the same for a row's slots waits
       lift = slope * (float)(row.pos - t0 - 4 * grp) * f.post;
 #pragma unroll
@@ -187,9 +209,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
           sc[u][k] = __builtin_fmaf(-slope, fabsf(gap), sc[u][k]);
         }
     }
-#pragma unroll
-    for (int x = 0; x < BK / 32; x++) seen[x] = 0xffffffff;
     if (!whole) {
+      uint32_t seen[BK / 32];
 #pragma unroll
       for (int x = 0; x < BK / 32; x++) {
         const int j0 = t0 + 32 * x;
@@ -205,8 +226,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
     for (int u = 0; u < KT; u++)
 #pragma unroll
       for (int k = 0; k < A; k++) most = fmaxf(most, sc[u][k]);
-    most = most * f.post - lift;
-    most = R == 32 ? max32(most) : max32(max16(most));
+    most = __builtin_fmaf(most, times, plus) - lift;
+    most = max32(most);
     // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
     if (__any(most > top + (8.f + kRoom<T>))) {
       const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
@@ -217,48 +238,171 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
   };
   // Weight operand i.  The products' operands have the cache's type: the weights are rounded to it here, their sum is not.
   auto weights = [&](const acc(&sc)[KT], int i) {
-    const float mx = (top == -kInf ? 0.f : top) + lift;
+    const float mx = (top == -kInf ? 0.f : top) + lift - plus;
     f32x8 p;
 #pragma unroll
-    for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[(8 * i + k) / A][(8 * i + k) % A], f.post, -mx));
+    for (int k = 0; k < 8; k++) p[k] = ex2(__builtin_fmaf(sc[(8 * i + k) / A][(8 * i + k) % A], times, -mx));
     sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     return __builtin_convertvector(p, V8);
   };
 
-  if (n_tiles > 0) {
-    look_up(0);
-    load(0);
-    if (n_tiles > 1) look_up(1);
-    put(0);
-    if (n_tiles > 1) load(1);
-    if (n_tiles > 2) look_up(2);
-  }
-  for (int i = 0; i < n_tiles; i++) {
-    const int t0 = slot_of(i), buf = i & 1;
-    __syncthreads();  // tile i is in LDS, and no wave reads tile i - 1 any more
-    const int va = here(buf * 4 * kTile + val_at);
-    acc sc[KT];
-    uint32_t seen[BK / 32];
-    const bool has = sees(t0);
-    if (has) scores(sc, buf);
-    if (i + 1 < n_tiles) {
-      put(buf ^ 1);
-      if (i + 2 < n_tiles) load(i + 2);
-      if (i + 3 < n_tiles) look_up(i + 3);
+  // One tile after the other, all waves in the same step of it.
+  auto go_over = [&] {
+    if (n_tiles > 0) {
+      look_up(0);
+      load(0);
+      if (n_tiles > 1) look_up(1);
+      put_keys(0), put_values(0, vf, vs);
+      if (n_tiles > 1) load(1);
+      if (n_tiles > 2) look_up(2);
     }
-    if (has) {
-      fold(sc, seen, t0);
+    for (int i = 0; i < n_tiles; i++) {
+      const int t0 = slot_of(i), buf = i & 1;
+      __syncthreads();  // tile i is in LDS, and no wave reads tile i - 1 any more
+      const int va = here(buf * 4 * kTile + val_at());
+      acc sc[KT];
+      const bool has = sees(t0);
+      if (has) scores(sc, buf);
+      if (i + 1 < n_tiles) {
+        put_keys(buf ^ 1), put_values(buf ^ 1, vf, vs);
+        if (i + 2 < n_tiles) load(i + 2);
+        if (i + 3 < n_tiles) look_up(i + 3);
+      }
+      if (has) {
+        fold(sc, t0);
 #pragma unroll
-      for (int x = 0; x < NP; x++) {
-        const V8 pb = weights(sc, x);
+        for (int x = 0; x < NP; x++) {
+          const V8 pb = weights(sc, x);
 #pragma unroll
-        for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb, o[d]);
+          for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb, o[d]);
+        }
       }
     }
-  }
+  };
+
+  // Two waves to a SIMD in turns: while one multiplies (a tile's scores and the outputs of the one before), the other works on
+  // its scores.  The second four waves are one step behind.  A tile's keys are read in the two steps from step 2 i on, its
+  // values in the two behind them; so while tile i is multiplied, the keys of tile i + 1 and the values of tile i are put.
+  auto in_turns = [&] {
+    const bool behind = wave >= 4;
+    // Where a tile is converted and put, and the one behind it loaded: behind a step's products, which wait for LDS rather than
+    // for the wave's instructions; the loads, in scalar instructions for the most part, go with the weights unless a cap makes
+    // those the longer part (2,048 rows over 32,768 slots: 980 us, 1,166 with a cap; the other way round 1,012 and 1,205).  At
+    // 256 elements a head, where some registers are kept in memory and are waited for behind the loads, all of it goes before
+    // the weights (673 us for 2,048 rows of 16 heads over 16,384 slots, 901 behind the products).
+    constexpr bool early = D == 256;
+    const bool with_products = a.softcap > 0.f;
+    codes_t held_v;
+    uint32_t held_s;
+    auto take = [&](int i) {
+      if (i < n_tiles) load(i);
+      if (i + 1 < n_tiles) look_up(i + 1);
+    };
+    auto put = [&](int i) {
+      if (i + 1 < n_tiles) put_keys(i + 1 & 1);
+      if (i < n_tiles) put_values(i & 1, held_v, held_s);
+      held_v = vf, held_s = vs;
+      if (early) take(i + 2);
+    };
+    if (n_tiles) {
+      look_up(0);
+      take(0);
+      put_keys(0);
+      held_v = vf, held_s = vs;
+      take(1);
+    }
+    auto step = [&] {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    acc sc[KT];
+    V8 pb[NP];
+    bool had = false;  // weights of the tile before are there
+    auto outputs = [&](int i) {
+      const int va = here((i & 1) * 4 * kTile + val_at());
+#pragma unroll
+      for (int x = 0; x < NP; x++)
+#pragma unroll
+        for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb[x], o[d]);
+    };
+    // operands a few products ahead of their use
+    auto feed = [](int products) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+#pragma unroll
+      for (int k = 0; k < products; k++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+    };
+    auto multiply = [&](int i) {
+      const bool has = i < n_tiles && sees(slot_of(i));
+      if (has && had) {
+        scores(sc, i & 1);
+        outputs(i - 1);
+        feed(KT * KC + NP * DB);
+      } else if (has) {
+        scores(sc, i & 1);
+        feed(KT * KC);
+      } else if (had) {
+        outputs(i - 1);
+        feed(NP * DB);
+      }
+      had = has;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto weigh = [&](int i) {
+      if (!early) {
+        if (!with_products && i + 2 < n_tiles) load(i + 2);
+        if (i + 3 < n_tiles) look_up(i + 3);
+      }
+      if (had) {
+        fold(sc, slot_of(i));
+#pragma unroll
+        for (int x = 0; x < NP; x++) pb[x] = weights(sc, x);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // products at a higher priority: the other wave of the SIMD has instructions for every cycle
+    auto turn = [&](int i) {
+      step();
+      __builtin_amdgcn_s_setprio(2);
+      multiply(i);
+      if (!early && i < n_tiles) {
+        put(i);
+        if (with_products && i + 2 < n_tiles) load(i + 2);
+      }
+      __builtin_amdgcn_s_setprio(0);
+    };
+    if (!behind) {
+      for (int i = 0; i <= n_tiles; i++) {
+        turn(i);
+        step();
+        if (i < n_tiles) {
+          if (early) put(i);
+          weigh(i);
+        }
+      }
+    } else {
+      step();
+      if (early && n_tiles) put(0);
+      for (int i = 0; i <= n_tiles; i++) {
+        turn(i);
+        if (i < n_tiles) {
+          step();
+          if (early && i + 1 < n_tiles) put(i + 1);
+          weigh(i);
+        }
+      }
+    }
+    __syncthreads();
+  };
+  if constexpr (W == 8) in_turns();
+  else go_over();
   if (bad) flag(c, s, RKC_CS_BLOCK);
 
-  sum = R == 32 ? sum32(sum) : sum32(sum16(sum));
+  sum = sum32(sum);
   if (!mine) return;
   typedef T T4 __attribute__((ext_vector_type(4)));
   if (pl.splits == 1) {
@@ -270,32 +414,32 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void packed_tile(const rkc
       for (int k = 0; k < A / 4; k++) {
         f32x4 x = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]} * by;
         if (sum == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
-        *(T4*)(to + R * d + 256 / R * k) = __builtin_convertvector(x, T4);
+        *(T4*)(to + 32 * d + 8 * k) = __builtin_convertvector(x, T4);
       }
     if (grp == 0) a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = sum == 0.f ? -kInf : kLn2 * (top + lg2(sum));
   } else {
-    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + R * part + col;
+    const int64_t at = ((int64_t)((s * H + h) * pl.tiles + qt) * pl.splits + split) * kRows + 32 * part + col;
     float* to = (float*)((char*)a.d_scratch + pl.part_at) + at * D + 4 * grp;
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
-      for (int k = 0; k < A / 4; k++) *(f32x4*)(to + R * d + 256 / R * k) = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
+      for (int k = 0; k < A / 4; k++) *(f32x4*)(to + 32 * d + 8 * k) = f32x4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
     float* st = (float*)((char*)a.d_scratch + pl.stat_at) + at * 2;
     if (grp == 0) st[0] = top, st[1] = sum;
   }
 }
 
-template <typename T, int D, int W, int R>
+template <typename T, int D, int W>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  packed_tile<T, D, W, R><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  packed_tile<T, D, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 template <typename T>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  if (c->head_dim == 256) return go<T, 256, 8, 16>(c, a, p, s);
-  if (c->head_dim == 128) return go<T, 128, 4, 32>(c, a, p, s);
-  return go<T, 64, 4, 32>(c, a, p, s);
+  if (c->head_dim == 256) return p->rows == 256 ? go<T, 256, 8>(c, a, p, s) : go<T, 256, 4>(c, a, p, s);
+  if (c->head_dim == 128) return p->rows == 256 ? go<T, 128, 8>(c, a, p, s) : go<T, 128, 4>(c, a, p, s);
+  return go<T, 64, 4>(c, a, p, s);
 }
 
 }  // namespace
