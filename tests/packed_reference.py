@@ -1,8 +1,6 @@
 """Plain implementation of rows into a paged cache (norm, rotation, 4 bits) and back, in 64 bits on the CPU."""
 from __future__ import annotations
 
-import math
-
 import numpy as np
 
 from tests import cache_reference as ref
@@ -105,5 +103,25 @@ class Packed(ref.Case):
         self.k, self.v = (torch.from_numpy(x.transpose(0, 2, 1, 3).copy()) for x in (kv, vv))
 
 
-def scale_of(dim):
-    return 1 / math.sqrt(dim)
+    def attend_at_once(self):
+        """``attend`` for finite values, a head's rows at once."""
+        T, Q = self.q.shape[:2]
+        out, lse = np.zeros((T, Q, self.dim)), np.full((T, Q), -np.inf)
+        for s in range(len(self.lens)):
+            rows = slice(int(self.offset[s]), int(self.offset[s + 1]))
+            for h in range(self.kv_heads):
+                v = self.slots(self.v, s, h)
+                for head in range(h * self.group, (h + 1) * self.group):
+                    x, see = self.scores(s, head)
+                    x = np.where(see, x, -np.inf)
+                    m = x.max(-1, initial=-np.inf, keepdims=True)
+                    p = np.exp(x - np.where(m == -np.inf, 0, m))
+                    total = p.sum(-1, keepdims=True)
+                    with np.errstate(divide="ignore"):
+                        lse[rows, head] = (m + np.log(total))[:, 0]
+                    out[rows, head] = p @ v / np.where(total == 0, 1, total)
+        return out, lse
+
+    def slots(self, pool, s, h):
+        n, j = self.lens[s], np.arange(self.lens[s])
+        return pool[self.table[s].numpy()[j // self.page], j % self.page, h].double().numpy() if n else np.zeros((0, self.dim))

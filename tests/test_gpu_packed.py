@@ -91,6 +91,32 @@ def test_long_sequences_in_parts(rows, group, dim):
     check_attend(c, *run_attend(c))
 
 
+LONG = [  # dim, dtype, group, lens, rows, what else: more than 128 packed rows, row tiles x parts of 256 slots past 512
+    (128, "bfloat16", 4, [7000, 6001], [300, 257], {}), (128, "float16", 4, [7000, 6001], [300, 257], dict(softcap=20.0)),
+    (128, "bfloat16", 4, [7000, 6001], [300, 257], dict(softcap=300.0, bias=True)), (128, "float16", 2, [9000, 70], [600, 70], dict(bias=True)),
+    (256, "bfloat16", 4, [7000, 6001], [300, 257], {}), (256, "float16", 4, [7000, 6001], [300, 257], dict(softcap=30.0)),
+    (256, "bfloat16", 2, [9000, 70], [600, 70], dict(bias=True)), (128, "bfloat16", 5, [8192, 8000, 30, 5000], [64, 50, 30, 1], "tree"),
+    (256, "float16", 5, [8192, 8000, 30, 5000], [64, 50, 30, 1], "tree"), (128, "bfloat16", 4, [7000, 6001], [700, 500], "documents"),
+    (256, "bfloat16", 4, [7000, 6001], [700, 500], "documents"), (64, "bfloat16", 4, [7000, 6001], [300, 257], dict(softcap=20.0)),
+    (128, "bfloat16", 32, [5000, 900, 64, 1], [8, 8, 8, 1], "tree"), (128, "float16", 8, [20000, 3, 12000], [30, 3, 20], {}),
+    (256, "bfloat16", 8, [20000, 3, 12000], [12, 3, 16], {}), (64, "float16", 8, [20000, 3, 12000], [30, 3, 20], {})]
+
+
+@pytest.mark.parametrize("case", LONG)
+def test_many_rows_of_long_sequences(case):
+    """Both sizes of a workgroup, whole and cut sequences, short ones beside them."""
+    dim, dtype, group, lens, rows, what = case
+    say("case long", *case)
+    kw = dict(what) if isinstance(what, dict) else {}
+    if what == "tree":
+        kw = dict(parent=sum((bush(r, dim + r) for r in rows), []), bias=True)
+    elif what == "documents":
+        start = [x for n, r in zip(lens, rows) for x in [(n - r + i) // 333 * 333 if i % 9 else 1 << 30 for i in range(r)]]
+        kw = dict(row_start=start, prefix=[1000, 0])
+    c = ref.Packed(len(lens) + dim, lens, rows, dim=dim, group=group, dtype=dtype, page=64, **kw)
+    check_attend(c, *run_attend(c), want=c.attend_at_once())
+
+
 def test_strides_of_the_pool_and_of_rows():
     """A slice of a pool's heads, blocks apart, queries of a fused tensor and outputs among others."""
     import torch
