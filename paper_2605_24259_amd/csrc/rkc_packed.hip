@@ -20,7 +20,7 @@
 namespace {
 
 template <typename T, int D, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void packed_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+__global__ __launch_bounds__(64 * kWaves, 2) void packed_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
   constexpr int KC = D / 32, DB = D / 16;  // dwords of codes in a quarter of a slot, and key operands; output blocks
   constexpr int NS = D == 256 ? 2 : 1;     // scales of a quarter
@@ -298,7 +298,7 @@ rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
   const bool wide_head = c->head_dim == 256;
-  const int64_t want = wide_head || p.rows == 256 ? 256 : p.few ? 10 * 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
+  const int64_t want = p.few ? (wide_head ? 4 : 10) * 256 : wide_head || p.rows == 256 ? 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;
