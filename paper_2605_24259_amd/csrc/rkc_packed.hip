@@ -1,9 +1,12 @@
 // rkc_packed.hip -- attention over a paged cache in 4 bits: C ABI, choice of kernel, and the kernel of few rows (decode steps,
 // small trees).
 //
-// out = sum_j exp(x_j - m) v_j / sum_j exp(x_j - m), x the masked and capped scores, m their running maximum.  Up to 16
-// packed rows (rows x query heads of one key/value head) are the columns of a 16x16x32 matrix product, so every key and
-// value is read once for all of them; what bounds the kernel is that read.
+// out = sum_j exp(x_j - m) v_j / sum_j exp(x_j - m), x the masked and capped scores, m their running maximum.  16 packed
+// rows (rows x query heads of one key/value head) are the columns of a 16x16x32 matrix product, and a workgroup has one or two
+// blocks of 16, so that every key and value is read and converted once for all of them.  What bounds the kernel is that read:
+// 5.2 TB/s with 5 sequences of 250,000 to 262,144 slots, 8 heads of 128 elements (268 us; the 16-bit cache's 896), 4.4 TB/s
+// with 64 of 1 to 8,192 (67 us).  With two blocks two waves a SIMD are left, and the vector units' work on the scores counts
+// as much (32 packed rows over 40 sequences of 700 to 8,192 slots: 2.7 TB/s, 81 us).
 // A workgroup takes a chunk of one sequence's slots for one head, its waves take 32 slots at a time:
 //   K  a lane has a quarter of its slot's key (head_dim / 4 elements), which it makes the product's operand of by the
 //      conversion of two codes an instruction, exact with the scale in it;
@@ -19,49 +22,58 @@
 
 namespace {
 
-template <typename T, int D, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void packed_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
+template <typename T, int D, int kWaves, int NB>
+__global__ __launch_bounds__(64 * kWaves, D == 256 && NB == 2 ? 1 : 2) void packed_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
+  constexpr int kRows = 16 * NB;           // NB blocks of packed rows, a lane's column of each
   constexpr int KC = D / 32, DB = D / 16;  // dwords of codes in a quarter of a slot, and key operands; output blocks
   constexpr int NS = D == 256 ? 2 : 1;     // scales of a quarter
   constexpr int kTile = 32 * D;            // elements of a wave's V tile
-  constexpr int kJoin = 16 * D * 4;        // bytes of a wave's output tile at the join
+  constexpr int kJoin = 16 * D * 4;        // bytes of a wave's outputs of a block at the join
   constexpr int kLds = kTile * 2 > kJoin ? kTile * 2 : kJoin;
   __shared__ __attribute__((aligned(16))) char lds[kWaves * kLds];
-  __shared__ float stat[kWaves][16][2], total[16];
+  __shared__ float stat[kWaves][kRows][2], total[kRows];
 
   const int H = c.kv_heads, G = a.q_heads / H;
   // The parts of a sequence are neighbours, turned by a number of their own in each: XCDs take workgroups in turn, and
   // an XCD would else have the same parts of every sequence, the last ones of short sequences being empty.
-  const int u = blockIdx.x / pl.splits, h = u % H, s = u / H, split = (blockIdx.x % pl.splits + (u * 0x9e3779b1u >> 16)) % pl.splits;
+  // Row tiles of the same part are eight workgroups apart: on one XCD, whose cache has what the first of them read.
+  const int x = blockIdx.x / (8 * pl.tiles) * 8 + blockIdx.x % 8, qt = blockIdx.x / 8 % pl.tiles;
+  const int u = x / pl.splits, h = u % H, s = u / H, split = (x % pl.splits + (u * 0x9e3779b1u >> 16)) % pl.splits;
+  if (s >= c.n_seqs) return;
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), quad = lane >> 4, col = lane & 15;
   const Seq q = load_seq(c, a, s);
   if (!q.ok) {
-    if (split == 0 && h == 0 && threadIdx.x == 0) flag(c, s, RKC_CS_LENGTH);
+    if (split == 0 && h == 0 && qt == 0 && threadIdx.x == 0) flag(c, s, RKC_CS_LENGTH);
     return;
   }
-  const int M = q.n * G;
-  if (!M) return;
+  const int m0 = qt * kRows, M = q.n * G - m0;  // rows yet to be had by this tile and those behind it
+  if (M <= 0) return;
   const int c0 = split * pl.chunk, c1 = min(q.len, c0 + pl.chunk);
   if (split && c0 >= q.len) return;
   const int32_t* table = c.d_block_table + (int64_t)s * c.max_pages;
   const int shift = 31 - __builtin_clz(c.page_tokens), in_page = c.page_tokens - 1;
 
   const Scale f = load_scale(a);
-  const int mine_m = min(col, M - 1), qi = mine_m / G, qh = h * G + mine_m % G;
-  Row row = load_row(a, q, s, qi);
-  const float slope = a.d_slope ? a.d_slope[qh] * kLog2e / f.post : 0.f;
-  V8 qf[KC];  // a quarter of the row's query, as the keys'
-  {
-    const T* p = (const T*)a.d_q + (q.row0 + qi) * a.q_row_stride + qh * a.q_head_stride + quad * (D / 4);
+  int qi[NB], qh[NB];
+  Row row[NB];
+  float slope[NB];
+  V8 qf[NB][KC];  // a quarter of the rows' queries, as the keys'
+#pragma unroll
+  for (int n = 0; n < NB; n++) {
+    const int m = min(16 * n + col, M - 1);
+    qi[n] = (m0 + m) / G, qh[n] = h * G + (m0 + m) % G;
+    row[n] = load_row(a, q, s, qi[n]);
+    slope[n] = a.d_slope ? a.d_slope[qh[n]] * kLog2e / f.post : 0.f;
+    const T* p = (const T*)a.d_q + (q.row0 + qi[n]) * a.q_row_stride + qh[n] * a.q_head_stride + quad * (D / 4);
 #pragma unroll
     for (int k = 0; k < KC; k++) {
-      qf[k] = *(const V8*)(p + 8 * k);
-      if (f.negate) qf[k] = negated(qf[k]);
+      qf[n][k] = *(const V8*)(p + 8 * k);
+      if (f.negate) qf[n][k] = negated(qf[n][k]);
     }
   }
-  // a tree's rows are at most 16 here: lines as bits of a register, walked through the lanes' parents
-  uint32_t line = 0;
+  // a tree's rows are at most 32 here: lines as bits of a register, walked through the lanes' parents
+  uint32_t line[NB] = {};
   int depth_of = 0;  // depth of row `lane`
   if (a.d_parent && c1 > q.base) {
     int par = -1;
@@ -78,8 +90,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_few(const rkc_cache c, 
       if (at >= 0) mine |= 1u << at, at = up;
     }
     depth_of = __popc(mine) - 1;
-    line = (uint32_t)__shfl((int)mine, qi);
-    row.pos = q.base + __shfl(depth_of, qi);
+#pragma unroll
+    for (int n = 0; n < NB; n++) line[n] = (uint32_t)__shfl((int)mine, qi[n]), row[n].pos = q.base + __shfl(depth_of, qi[n]);
   } else if (a.d_parent && a.d_slope) {
     // distances need the rows' depths in every chunk
     int par = lane < q.n ? a.d_parent[q.row0 + lane] : -1;
@@ -89,21 +101,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_few(const rkc_cache c, 
       const int up = __shfl(par, at & 63);
       if (at >= 0) d++, at = up;
     }
-    row.pos = q.base + __shfl(d, qi);
+#pragma unroll
+    for (int n = 0; n < NB; n++) row[n].pos = q.base + __shfl(d, qi[n]);
   }
   // slots that all rows see, and slots that any sees
-  const int all_from = wave_max(row.start), all_to = wave_min(row.end), any_from = wave_min(row.start), all_pre = uni(row.prefix);
-  int any_to = wave_max(max(row.end, row.prefix));
+  int first = row[0].start, last = row[0].start, least = row[0].end, most_end = max(row[0].end, row[0].prefix);
+#pragma unroll
+  for (int n = 1; n < NB; n++) {
+    first = min(first, row[n].start), last = max(last, row[n].start);
+    least = min(least, row[n].end), most_end = max(most_end, row[n].end);
+  }
+  const int all_from = wave_max(last), all_to = wave_min(least), any_from = wave_min(first), all_pre = uni(row[0].prefix);
+  int any_to = wave_max(most_end);
   if (a.d_parent) any_to = q.len;
   const int end = min(c1, any_to);  // of what is looked at here: a chunk is a multiple of 32 slots
 
   const Codes held = codes_of<D>(c, h);
   T* tile = (T*)(lds + wave * kLds);
 
-  float top = -kInf, sum = 0.f;
-  f32x4 o[DB];
+  float top[NB], sum[NB];
+  f32x4 o[NB][DB];
 #pragma unroll
-  for (int d = 0; d < DB; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < NB; n++) {
+    top[n] = -kInf, sum[n] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; d++) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
   const rkc_tiles<32> tiles(c0, end, all_pre, any_from);
   const int n_tiles = tiles.n;
@@ -150,13 +173,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_few(const rkc_cache c, 
   }
   for (; i < n_tiles; i += kWaves) {
     const int t0 = slot_of(i);
-    f32x4 sc[2];
+    f32x4 sc[NB][2];
     const int pa = here(put_at), va = here(val_at);
 #pragma unroll
     for (int u = 0; u < 2; u++) {
-      sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KC; k++) sc[u] = mma16(__builtin_bit_cast(V8, unpack8<T>(kf[u][k], scale_k(ks[u], k))), qf[k], sc[u]);
+      for (int n = 0; n < NB; n++) sc[n][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KC; k++) {
+        const V8 key = __builtin_bit_cast(V8, unpack8<T>(kf[u][k], scale_k(ks[u], k)));
+#pragma unroll
+        for (int n = 0; n < NB; n++) sc[n][u] = mma16(key, qf[n][k], sc[n][u]);
+      }
       // a scale that nobody wrote may be anything: what no row sees is to be finite
 #pragma unroll
       for (int k = 0; k < KC; k++) {
@@ -165,114 +193,132 @@ __global__ __launch_bounds__(64 * kWaves, 2) void packed_few(const rkc_cache c, 
       }
     }
     const bool whole = t0 + 32 <= all_pre || (t0 >= all_from && t0 + 32 <= all_to);
-    if (a.softcap > 0.f) cap_all(sc, f);
-    if (a.d_slope) {
-      const float far = (float)(here(row.pos - t0) - quad * 4);
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        float gap = far - (float)(16 * (e >> 2) + (e & 3));
-        if (a.d_parent && t0 + 32 > q.base) {
-          const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
-          gap = at >= 0 ? (float)(row.pos - q.base - d) : gap;
-        }
-        sc[e >> 2][e & 3] = __builtin_fmaf(-slope, fabsf(gap), sc[e >> 2][e & 3]);
-      }
-    }
-    if (!whole) {
-      const int from = t0 - q.base;
-      const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line >> from : line << -from;
-      const uint32_t seen = seen_of(row, t0, drafted) >> 4 * quad;
-#pragma unroll
-      for (int e = 0; e < 8; e++) sc[e >> 2][e & 3] = masked(sc[e >> 2][e & 3], seen, 16 * (e >> 2) + (e & 3));
-    }
     auto vals = [&](int d) { return read_tr2<T>((const char*)tile + (va ^ d << 5), (const char*)tile + (va ^ d << 5) + 32 * D); };
     if (i + kWaves < n_tiles) {
       load(i + kWaves);
       if (i + 2 * kWaves < n_tiles) look_up(i + 2 * kWaves);
     }
-    float most = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-    most = max32(max16(most)) * f.post;
-    // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
-    if (__any(most > top + (8.f + kRoom<T>))) {
-      const float now = fmaxf(top, most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top - now);
-      top = now, sum *= by;
+    V8 pb[NB], pr[NB];
 #pragma unroll
-      for (int d = 0; d < DB; d++) o[d] *= by;
+    for (int n = 0; n < NB; n++) {
+      if (a.softcap > 0.f) cap_all(sc[n], f);
+      if (a.d_slope) {
+        const float far = (float)(here(row[n].pos - t0) - quad * 4);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          float gap = far - (float)(16 * (e >> 2) + (e & 3));
+          if (a.d_parent && t0 + 32 > q.base) {
+            const int at = t0 + quad * 4 + 16 * (e >> 2) + (e & 3) - q.base, d = __shfl(depth_of, at & 63);
+            gap = at >= 0 ? (float)(row[n].pos - q.base - d) : gap;
+          }
+          sc[n][e >> 2][e & 3] = __builtin_fmaf(-slope[n], fabsf(gap), sc[n][e >> 2][e & 3]);
+        }
+      }
+      if (!whole) {
+        const int from = t0 - q.base;
+        const uint32_t drafted = from >= 32 || from <= -32 ? 0 : from >= 0 ? line[n] >> from : line[n] << -from;
+        const uint32_t seen = seen_of(row[n], t0, drafted) >> 4 * quad;
+#pragma unroll
+        for (int e = 0; e < 8; e++) sc[n][e >> 2][e & 3] = masked(sc[n][e >> 2][e & 3], seen, 16 * (e >> 2) + (e & 3));
+      }
+      float most = fmaxf(fmaxf(fmaxf(sc[n][0][0], sc[n][0][1]), fmaxf(sc[n][0][2], sc[n][0][3])),
+                         fmaxf(fmaxf(sc[n][1][0], sc[n][1][1]), fmaxf(sc[n][1][2], sc[n][1][3])));
+      most = max32(max16(most)) * f.post;
+      // weights up to 2^8 are let stand: the maximum moves, and the outputs are rescaled, in few tiles only
+      if (__any(most > top[n] + (8.f + kRoom<T>))) {
+        const float now = fmaxf(top[n], most - kRoom<T>), by = now == -kInf ? 1.f : ex2(top[n] - now);
+        top[n] = now, sum[n] *= by;
+#pragma unroll
+        for (int d = 0; d < DB; d++) o[n][d] *= by;
+      }
+      const float m = top[n] == -kInf ? 0.f : top[n];
+      f32x8 p;
+#pragma unroll
+      for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[n][e >> 2][e & 3], f.post, -m));
+      sum[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      // The products' operands have 16 bits.  Of one block a weight is the sum of two of them, with at least twice its bits, as the
+      // matrix units wait for the read anyway; of two it is rounded, as in the kernel of many rows.
+      pb[n] = __builtin_convertvector(p, V8);
+      if (NB == 1) pr[n] = __builtin_convertvector(p - __builtin_convertvector(pb[n], f32x8), V8);
     }
-    const float m = top == -kInf ? 0.f : top;
-    f32x8 p;
-#pragma unroll
-    for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[e >> 2][e & 3], f.post, -m));
-    sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    // the products' operands have 16 bits: a weight is the sum of two of them, with at least twice its bits
-    const V8 pb = __builtin_convertvector(p, V8), pr = __builtin_convertvector(p - __builtin_convertvector(pb, f32x8), V8);
 #pragma unroll
     for (int d = 0; d < DB; d++) {
       const V8 vt = vals(d);
-      o[d] = mma16(vt, pr, mma16(vt, pb, o[d]));
+#pragma unroll
+      for (int n = 0; n < NB; n++) {
+        o[n][d] = mma16(vt, pb[n], o[n][d]);
+        if (NB == 1) o[n][d] = mma16(vt, pr[n], o[n][d]);
+      }
     }
   }
 
   if (bad) flag(c, s, RKC_CS_BLOCK);
 
-  // join the waves; one that saw nothing of a row has a sum of 0
-  sum = sum32(sum16(sum));
-  if (quad == 0) stat[wave][col][0] = top, stat[wave][col][1] = sum;
-  __syncthreads();
-  float m_all = -kInf, l_all = 0.f;
+  // join the waves, a block of rows after the other; one that saw nothing of a row has a sum of 0
+  const int unit = u * pl.tiles + qt;
 #pragma unroll
-  for (int w = 0; w < kWaves; w++) m_all = fmaxf(m_all, stat[w][col][0]);
-#pragma unroll
-  for (int w = 0; w < kWaves; w++) l_all += stat[w][col][1] == 0.f ? 0.f : stat[w][col][1] * ex2(stat[w][col][0] - m_all);
-  {
-    const float by = ex2(top - m_all);
-    float* to = (float*)(lds + wave * kLds) + col * D + quad * 4;
-    // 16 rows of D floats: rotated so that the rows' 16-byte pieces do not share banks
-#pragma unroll
-    for (int d = 0; d < DB; d++) *(f32x4*)(to + 16 * ((d + col) % DB)) = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * by;
+  for (int n = 0; n < NB; n++) {
+    sum[n] = sum32(sum16(sum[n]));
+    if (quad == 0) stat[wave][16 * n + col][0] = top[n], stat[wave][16 * n + col][1] = sum[n];
   }
-  const int unit = s * H + h;
-  if (wave == 0 && quad == 0) {
-    total[col] = l_all;
-    if (pl.splits > 1) {
-      float* st = (float*)((char*)a.d_scratch + pl.stat_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + col) * 2;
-      st[0] = m_all, st[1] = l_all;
-    } else if (col < M) {
-      a.d_lse[(int64_t)(q.row0 + qi) * a.q_heads + qh] = l_all == 0.f ? -kInf : kLn2 * (m_all + lg2(l_all));
+#pragma unroll
+  for (int n = 0; n < NB; n++) {
+    if (16 * n >= M) break;
+    __syncthreads();  // of the first block: the sums are there; of the others: the one before is written
+    float m_all = -kInf, l_all = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) m_all = fmaxf(m_all, stat[w][16 * n + col][0]);
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) l_all += stat[w][16 * n + col][1] == 0.f ? 0.f : stat[w][16 * n + col][1] * ex2(stat[w][16 * n + col][0] - m_all);
+    {
+      const float by = ex2(top[n] - m_all);
+      float* to = (float*)(lds + wave * kLds) + col * D + quad * 4;
+      // 16 rows of D floats: rotated so that the rows' 16-byte pieces do not share banks
+#pragma unroll
+      for (int d = 0; d < DB; d++) *(f32x4*)(to + 16 * ((d + col) % DB)) = sum[n] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[n][d] * by;
     }
-  }
-  __syncthreads();
-  for (int x = threadIdx.x; x < M * (D / 4); x += 64 * kWaves) {
-    const int m = x / (D / 4), b = x % (D / 4), d = b >> 2;
-    const float* from = (const float*)lds + m * D + 16 * ((d + m) % DB) + (b & 3) * 4;
-    f32x4 y = *(const f32x4*)from;
+    if (wave == 0 && quad == 0) {
+      total[16 * n + col] = l_all;
+      if (pl.splits > 1) {
+        float* st = (float*)((char*)a.d_scratch + pl.stat_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + 16 * n + col) * 2;
+        st[0] = m_all, st[1] = l_all;
+      } else if (16 * n + col < M) {
+        a.d_lse[(int64_t)(q.row0 + qi[n]) * a.q_heads + qh[n]] = l_all == 0.f ? -kInf : kLn2 * (m_all + lg2(l_all));
+      }
+    }
+    __syncthreads();
+    for (int y4 = threadIdx.x; y4 < min(16, M - 16 * n) * (D / 4); y4 += 64 * kWaves) {
+      const int r = y4 / (D / 4), m = 16 * n + r, b = y4 % (D / 4), d = b >> 2;
+      const float* from = (const float*)lds + r * D + 16 * ((d + r) % DB) + (b & 3) * 4;
+      f32x4 y = *(const f32x4*)from;
 #pragma unroll
-    for (int w = 1; w < kWaves; w++) y += *(const f32x4*)((const char*)from + w * kLds);
-    if (pl.splits == 1) {
-      const float l = total[m];
-      const float by = l == 0.f ? 0.f : 1.f / l;
-      T* to = (T*)a.d_out + (q.row0 + m / G) * a.out_row_stride + (h * G + m % G) * a.out_head_stride + b * 4;
-      typedef T T4 __attribute__((ext_vector_type(4)));
-      *(T4*)to = __builtin_convertvector(y * by, T4);
-    } else {
-      *(f32x4*)((float*)((char*)a.d_scratch + pl.part_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + m) * D + b * 4) = y;
+      for (int w = 1; w < kWaves; w++) y += *(const f32x4*)((const char*)from + w * kLds);
+      if (pl.splits == 1) {
+        const float l = total[m];
+        const float by = l == 0.f ? 0.f : 1.f / l;
+        T* to = (T*)a.d_out + (q.row0 + (m0 + m) / G) * a.out_row_stride + (h * G + (m0 + m) % G) * a.out_head_stride + b * 4;
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        *(T4*)to = __builtin_convertvector(y * by, T4);
+      } else {
+        *(f32x4*)((float*)((char*)a.d_scratch + pl.part_at) + ((int64_t)(unit * pl.splits + split) * pl.rows + m) * D + b * 4) = y;
+      }
     }
   }
 }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, int NB>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
-  packed_few<T, D, W><<<dim3(p->units * p->splits), dim3(64 * W), 0, s>>>(*c, *a, *p);
+  packed_few<T, D, W, NB><<<dim3(rkc_packed_few_workgroups(p)), dim3(64 * W), 0, s>>>(*c, *a, *p);
   return hipGetLastError() == hipSuccess ? RKC_OK : RKC_E_HIP;
 }
 
 template <typename T, int D>
 rkc_status go(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s) {
+  if (p->rows == 32) return go<T, D, 4, 2>(c, a, p, s);
   if constexpr (D <= 128) {
-    if (p->waves == 8) return go<T, D, 8>(c, a, p, s);
+    if (p->waves == 8) return go<T, D, 8, 1>(c, a, p, s);
   }
-  return go<T, D, 4>(c, a, p, s);
+  return go<T, D, 4, 1>(c, a, p, s);
 }
 
 template <typename T>
@@ -286,30 +332,40 @@ rkc_status rkc_packed_few(const rkc_cache* c, const rkc_attention* a, const rkc_
   return c->dtype == RKC_BF16 ? go<__bf16>(c, a, p, s) : go<_Float16>(c, a, p, s);
 }
 
-// As rkc_attend_plan: up to 16 packed rows go to the kernel that reads the cache as fast as it can, more to the one that keeps
-// the matrix units busy, and a sequence is cut where sequences, heads and row tiles do not fill the card's 256 CUs.
+// Which kernel and how a sequence is cut.  Up to 96 packed rows (trees of up to 32 rows) go to the kernel that reads the cache as
+// fast as it can, 16 or tiles of 32 rows a workgroup, more to the one that keeps the matrix units busy (40 trees over 700 to
+// 8,192 slots, 8 heads of 128 elements: 32 packed rows 81 us, by the other kernel 186; 64 124 and 190; 96 166 and 203; 128 182
+// and 190, of 64 elements 135 and 114).  There 256 rows a workgroup halve what is converted and read of LDS per product, where
+// such tiles, counted with 256 slots each, are twice the card's CUs: fewer leave CUs idle.  A sequence is cut where sequences,
+// heads and row tiles do not fill the card a few times over.
 rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   rkc_plan p = {};
   const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
-  p.few = M <= 16;
+  p.few = M <= 32 || (M <= 96 && (!a->d_parent || a->max_rows <= 32));
   const int64_t wide = (int64_t)c->n_seqs * c->kv_heads * ((M + 255) / 256) * ((a->max_len + 255) / 256);
-  p.rows = p.few ? 16 : M <= 128 || c->head_dim == 64 || wide < 512 ? 128 : 256;
-  p.tiles = p.few ? 1 : (int)((M + p.rows - 1) / p.rows);
+  p.rows = p.few ? (M <= 16 ? 16 : 32) : M <= 128 || c->head_dim == 64 || wide < 512 ? 128 : 256;
+  p.tiles = (int)((M + p.rows - 1) / p.rows);
+  if (p.tiles < 1) p.tiles = 1;
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
+  // Workgroups wanted: of few rows ten a CU (64 sequences of up to 8,192 slots, 8 heads: 67 us, with four 76), of heads of 256
+  // elements four (32 sequences, 4 heads: 53 us, with one 67); of many as many as a CU holds.
   const bool wide_head = c->head_dim == 256;
   const int64_t want = p.few ? (wide_head ? 4 : 10) * 256 : wide_head || p.rows == 256 ? 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;
   int64_t chunk = (a->max_len + cut - 1) / cut;
   chunk = (chunk + grain - 1) / grain * grain;
+  // Of few rows no less than four tiles a wave, and up to 512 slots of many none: starts and the join cost more than that saves.
   const int64_t least = p.few && !wide_head ? 512 : grain;
   if (chunk < least) chunk = least;
   if (!p.few && a->max_len <= 512 && (c->head_dim < 256 || units >= 32)) chunk = 512;
-  p.waves = p.few && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
+  // Short sequences whole, by eight waves: no second kernel for the join.
+  p.waves = M <= 16 && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
   if (p.waves == 8) chunk = a->max_len < 32 ? 32 : (a->max_len + 31) / 32 * 32;
   p.chunk = (int)chunk;
   p.splits = (int)((a->max_len + chunk - 1) / chunk);
   if (p.splits < 1) p.splits = 1;
+  // More workgroups than the card holds at once: the longest go first, so that none starts late.
   p.sorted = !p.few && c->n_seqs > 1 && c->n_seqs <= 64 && units * p.splits > want;
   if (p.splits > 1) {
     const size_t rows = (size_t)units * p.splits * p.rows;
@@ -343,7 +399,7 @@ rkc_status rkc_packed_attend(const rkc_packed* c, const rkc_attention* a, void* 
   if (a->max_rows == 0) p.splits = 1, p.bytes = 0;  // sequences that have rows all the same are told of
   // rows of tiles are counted in 32 bits
   if ((int64_t)c->n_seqs * c->kv_heads * p.tiles * p.rows > 0x7fffffff) return RKC_E_UNSUPPORTED;
-  if (!rkc_fits((int64_t)p.units * p.splits, rkc_packed_lanes(&x, &p)) || (p.splits > 1 && !rkc_join_fits(&x, a, &p))) return RKC_E_UNSUPPORTED;
+  if (!rkc_fits(p.few ? rkc_packed_few_workgroups(&p) : (int64_t)p.units * p.splits, rkc_packed_lanes(&x, &p)) || (p.splits > 1 && !rkc_join_fits(&x, a, &p))) return RKC_E_UNSUPPORTED;
   if (p.bytes) {
     if (!a->d_scratch || a->scratch_bytes < p.bytes) return RKC_E_SCRATCH;
     if ((uintptr_t)a->d_scratch & 255) return RKC_E_ALIGN;

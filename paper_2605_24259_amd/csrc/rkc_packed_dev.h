@@ -68,6 +68,11 @@ rkc_status rkc_packed_check(const rkc_packed* c);
 rkc_cache rkc_packed_as_cache(const rkc_packed* c);
 rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a);
 inline int rkc_packed_lanes(const rkc_cache* c, const rkc_plan* p) { return 64 * (p->few ? p->waves : p->rows == 256 ? 8 : 4); }
+// Workgroups of the kernel of few rows: eight at a time for each row tile.
+inline int64_t rkc_packed_few_workgroups(const rkc_plan* p) {
+  const int64_t n = (int64_t)p->units / p->tiles * p->splits;
+  return p->tiles == 1 ? n : (n + 7) / 8 * 8 * p->tiles;
+}
 rkc_status rkc_packed_few(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 rkc_status rkc_packed_tile(const rkc_cache* c, const rkc_attention* a, const rkc_plan* p, hipStream_t s);
 

@@ -91,6 +91,27 @@ def test_long_sequences_in_parts(rows, group, dim):
     check_attend(c, *run_attend(c))
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,rows,form", [(1, 20, "tree"), (1, 32, "tree"), (3, 11, "tree"), (2, 32, "tree"), (4, 24, "tree"), (1, 33, "tree"),
+                                             (3, 31, "chunk"), (1, 90, "chunk"), (1, 33, "chunk"), (2, 20, "documents"), (3, 32, "documents"),
+                                             (17, 1, "chunk"), (48, 2, "tree"), (1, 97, "chunk")])
+def test_middling_rows(dim, group, rows, form):
+    """One and more tiles of 32 packed rows, the last one in part, sequences of fewer rows and tiles beside them."""
+    say("case middling", dim, group, rows, form)
+    lens, ns = [rows, rows + 13, 2 * rows + 700, 5, 0, 1500], [rows, rows, rows // 2, min(rows, 5), 0, 1]
+    kw = {}
+    if form == "tree":
+        kw = dict(parent=sum((bush(n, n + dim) for n in ns), []), bias=rows % 2 == 0)
+    elif form == "documents":
+        kw = dict(row_start=[(n - r + i) // 33 * 33 if i % 9 else 1 << 30 for n, r in zip(lens, ns) for i in range(r)], prefix=[15, 0, 40, 0, 0, 0])
+    else:
+        kw = dict(bias=rows % 2 == 1)
+    c = ref.Packed(rows + dim, lens, ns, dim=dim, group=group, kv_heads=2, dtype="float16" if group % 2 else "bfloat16",
+                   softcap=15.0 if rows == 32 else 0.0, **kw)
+    out, lse = run_attend(c)
+    check_attend(c, out, lse, want=c.attend_at_once())
+
+
 LONG = [  # dim, dtype, group, lens, rows, what else: more than 128 packed rows, row tiles x parts of 256 slots past 512
     (128, "bfloat16", 4, [7000, 6001], [300, 257], {}), (128, "float16", 4, [7000, 6001], [300, 257], dict(softcap=20.0)),
     (128, "bfloat16", 4, [7000, 6001], [300, 257], dict(softcap=300.0, bias=True)), (128, "float16", 2, [9000, 70], [600, 70], dict(bias=True)),
