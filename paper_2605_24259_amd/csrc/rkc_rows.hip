@@ -121,8 +121,11 @@ template <int L, typename W> __device__ __forceinline__ W sum_of(W x) {
 template <typename W> struct Pair { W c, s; };
 template <typename T> struct Run { typename Vec8<T>::t a, b; };  // a lane's two runs of 8 elements
 
-__device__ __forceinline__ float inverse_root(float x) { return 1.f / __builtin_sqrtf(x); }
+// 1 / sqrt(x): of the hardware, within a unit or two of the last place, in 32 bits, where the result is rounded to 16 behind it.
+__device__ __forceinline__ float inverse_root(float x) { return __builtin_amdgcn_rsqf(x); }
 __device__ __forceinline__ double inverse_root(double x) { return 1.0 / __builtin_sqrt(x); }
+__device__ __forceinline__ float mad(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double mad(double a, double b, double c) { return __builtin_fma(a, b, c); }
 
 // Norm and rotation of a lane's 16 elements.  W: 32 bits where the result is rounded to 16; 64 where it is rounded to 4,
 // as an element next to a border between two codes goes by its last bits, and should be held alike wherever it is computed.
@@ -133,7 +136,7 @@ __device__ __forceinline__ void norm_turn(const Run<T>& in, const float* w0, con
   if (norm) {
     W sum = 0;
 #pragma unroll
-    for (int k = 0; k < 16; k++) sum = __builtin_fma(y[k], y[k], sum);
+    for (int k = 0; k < 16; k++) sum = mad(y[k], y[k], sum);
     const W by = inverse_root(sum_of<L>(sum) * (W)(1.0 / D) + (W)r.eps);
 #pragma unroll
     for (int k = 0; k < 8; k++) y[k] = y[k] * by * (W)w0[k], y[8 + k] = y[8 + k] * by * (W)w1[k];
@@ -143,13 +146,13 @@ __device__ __forceinline__ void norm_turn(const Run<T>& in, const float* w0, con
 #pragma unroll
     for (int k = 0; k < 8; k++) {
       const W a = y[2 * k], b = y[2 * k + 1], c = t[k].c, s = t[k].s;
-      y[2 * k] = __builtin_fma(a, c, -(b * s)), y[2 * k + 1] = __builtin_fma(a, s, b * c);
+      y[2 * k] = mad(a, c, -(b * s)), y[2 * k + 1] = mad(a, s, b * c);
     }
   } else {
 #pragma unroll
     for (int k = 0; k < 8; k++) {
       const W a = y[k], b = y[8 + k], c = t[k].c, s = t[k].s;
-      y[k] = __builtin_fma(a, c, -(b * s)), y[8 + k] = __builtin_fma(a, s, b * c);
+      y[k] = mad(a, c, -(b * s)), y[8 + k] = mad(a, s, b * c);
     }
   }
 }
@@ -377,10 +380,11 @@ rkc_status rows_check(const rkc_rows* r, int n_seqs, int64_t cap, int heads, int
   return RKC_OK;
 }
 
-// Rows of a workgroup, and workgroups that share them: as many rows, up to `most`, as leave four workgroups a CU, and a few
-// rows' heads over as many workgroups.  (12,300 rows of 48 heads stored, 8 rows a workgroup: 66 us; 2 rows 72, 16 rows 71.)
+// Rows of a workgroup, and workgroups that share them: as many rows, up to `most`, as give its waves four turns and leave four
+// workgroups a CU, and a few rows' heads over as many workgroups.  (13,000 rows of 48 heads of 128 elements stored, 4 rows a
+// workgroup: 60.7 us; 2 rows 72, 8 rows 63.6, 16 rows 71.)
 // Reading, a workgroup has the rows whose heads its lanes take at once, twice: fewer rows are all start, and more keep their
-// loads waiting for the stores before them (258,000 rows of 4 heads of 256 elements, 4 rows: 281 us; 2 rows 369, 8 rows 292,
+// loads waiting for the stores before them (277,000 rows of 4 heads of 256 elements, 4 rows: 281 us; 2 rows 369, 8 rows 292,
 // 64 rows 325; 157,000 of 8 heads of 64, 8 rows: 104; 4 rows 126, 16 rows 109).
 struct Cut {
   int per, parts;
@@ -388,7 +392,7 @@ struct Cut {
 };
 Cut cut_of(int rows, int most, int64_t turns_of_a_row) {
   Cut k = {1, 1, 0};
-  while (2 * k.per <= most && rows / (2 * k.per) >= 1024) k.per *= 2;
+  while (2 * k.per <= most && rows / (2 * k.per) >= 1024 && k.per * turns_of_a_row < 4 * kWaves) k.per *= 2;
   const int64_t waves = (turns_of_a_row + kWaves - 1) / kWaves;
   if (k.per == 1) k.parts = (int)(1024 / rows < 1 ? 1 : 1024 / rows < waves ? 1024 / rows : waves);
   k.workgroups = (int64_t)((rows + k.per - 1) / k.per) * k.parts;
