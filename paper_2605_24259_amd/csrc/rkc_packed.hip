@@ -22,6 +22,17 @@
 
 namespace {
 
+// The sequence of rank r by length, the longest first, of at most 64, as seq_of_rank finds it, in three instructions a sequence:
+// lengths and lanes in one number, so that none are alike.
+__device__ __forceinline__ int seq_by_length(const rkc_cache& c, const rkc_attention& a, int r) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t key = lane < c.n_seqs ? (uint32_t)a.d_length[lane] << 6 | (63 - lane) : 0;
+  int rank = 0;
+#pragma unroll 8
+  for (int k = 0; k < c.n_seqs; k++) rank += (uint32_t)__builtin_amdgcn_readlane((int)key, k) > key;
+  return uni(__builtin_ctzll(__ballot(lane < c.n_seqs && rank == r)));
+}
+
 template <typename T, int D, int kWaves, int NB>
 __global__ __launch_bounds__(64 * kWaves, D == 256 && NB == 2 ? 1 : 2) void packed_few(const rkc_cache c, const rkc_attention a, const rkc_plan pl) {
   typedef typename Vec8<T>::t V8;
@@ -39,8 +50,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && NB == 2 ? 1 : 2) void pack
   // an XCD would else have the same parts of every sequence, the last ones of short sequences being empty.
   // Row tiles of the same part are eight workgroups apart: on one XCD, whose cache has what the first of them read.
   const int x = blockIdx.x / (8 * pl.tiles) * 8 + blockIdx.x % 8, qt = blockIdx.x / 8 % pl.tiles;
-  const int u = x / pl.splits, h = u % H, s = u / H, split = (x % pl.splits + (u * 0x9e3779b1u >> 16)) % pl.splits;
-  if (s >= c.n_seqs) return;
+  const int rank = x / pl.splits / H, h = x / pl.splits % H;
+  if (rank >= c.n_seqs) return;
+  // Of whole sequences the longer half goes first, from the longest on, and the other from the shortest on: a CU's second
+  // workgroup then is the shorter, the longer its first one is.
+  const int half = (c.n_seqs + 1) / 2, s = pl.sorted ? seq_by_length(c, a, rank < half ? rank : c.n_seqs - 1 - (rank - half)) : rank;
+  const int u = s * H + h, split = (x % pl.splits + (u * 0x9e3779b1u >> 16)) % pl.splits;
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), quad = lane >> 4, col = lane & 15;
   const Seq q = load_seq(c, a, s);
   if (!q.ok) {
@@ -348,8 +363,8 @@ rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   if (p.tiles < 1) p.tiles = 1;
   const int64_t units = (int64_t)c->n_seqs * c->kv_heads * p.tiles;
   p.units = (int)units;
-  // Workgroups wanted: of few rows ten a CU (64 sequences of up to 8,192 slots, 8 heads: 67 us, with four 76), of heads of 256
-  // elements four (32 sequences, 4 heads: 53 us, with one 67); of many as many as a CU holds.
+  // Workgroups wanted: of few rows ten a CU (5 sequences of 250,000 to 262,144 slots, 8 heads: 268 us, with four 307), of heads
+  // of 256 elements four (32 sequences of up to 8,192 slots, 4 heads: 53 us, with one 67); of many as many as a CU holds.
   const bool wide_head = c->head_dim == 256;
   const int64_t want = p.few ? (wide_head ? 4 : 10) * 256 : wide_head || p.rows == 256 ? 256 : 2 * 256, grain = p.few || wide_head ? 128 : 256;
   const int64_t cut = units ? (want + units - 1) / units : 1;
@@ -359,14 +374,17 @@ rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   const int64_t least = p.few && !wide_head ? 512 : grain;
   if (chunk < least) chunk = least;
   if (!p.few && a->max_len <= 512 && (c->head_dim < 256 || units >= 32)) chunk = 512;
-  // Short sequences whole, by eight waves: no second kernel for the join.
-  p.waves = M <= 16 && c->head_dim <= 128 && a->max_len <= 1536 ? 8 : 4;
+  // Whole sequences, by eight waves, where they are short or as many as the card holds at once: no second kernel for the join
+  // (64 sequences, 8 heads of 128 elements: of 2,500 slots each 42 us, in parts 51; of 4,096 63 and 74).
+  p.waves = M <= 16 && c->head_dim <= 128 && a->max_len <= (units < 512 ? 1536 : 8192) ? 8 : 4;
   if (p.waves == 8) chunk = a->max_len < 32 ? 32 : (a->max_len + 31) / 32 * 32;
   p.chunk = (int)chunk;
   p.splits = (int)((a->max_len + chunk - 1) / chunk);
   if (p.splits < 1) p.splits = 1;
-  // More workgroups than the card holds at once: the longest go first, so that none starts late.
-  p.sorted = !p.few && c->n_seqs > 1 && c->n_seqs <= 64 && units * p.splits > want;
+  // More workgroups than the card holds at once: the longest go first, so that none starts late.  Whole sequences of few rows, two
+  // a CU, are paired, long ones with short ones, but for short ones, where finding the order, 1.7 us, is more than it saves (64 of
+  // 1 to 8,192 slots: 65 us, in the table's order 78, in parts 78).
+  p.sorted = c->n_seqs > 1 && c->n_seqs <= 64 && (p.few ? p.splits == 1 && units > 256 && a->max_len > 1024 : units * p.splits > want);
   if (p.splits > 1) {
     const size_t rows = (size_t)units * p.splits * p.rows;
     p.part_at = 0;

@@ -112,6 +112,20 @@ def test_middling_rows(dim, group, rows, form):
     check_attend(c, out, lse, want=c.attend_at_once())
 
 
+@pytest.mark.parametrize("dim,seqs,longest", [(64, 64, 1500), (128, 33, 1100), (64, 3, 1300), (128, 61, 40), (64, 70, 1200), (64, 40, 2100)])
+def test_many_sequences(dim, seqs, longest):
+    """Of unlike lengths, whole and in parts, in the order of their lengths and not; equal ones and empty ones among them."""
+    say("case sequences", dim, seqs, longest)
+    rng = np.random.default_rng(dim + seqs)
+    lens = [int(x) for x in rng.integers(1, longest, seqs)]
+    lens[:3], lens[-1] = [longest, 1, lens[-1]], longest
+    rows = [1] * seqs
+    if seqs > 5:
+        lens[4], rows[4] = 0, 0
+    c = ref.Packed(seqs, lens, rows, dim=dim, group=2, kv_heads=16, page=64)
+    check_attend(c, *run_attend(c, max_len=longest), want=c.attend_at_once())
+
+
 LONG = [  # dim, dtype, group, lens, rows, what else: more than 128 packed rows, row tiles x parts of 256 slots past 512
     (128, "bfloat16", 4, [7000, 6001], [300, 257], {}), (128, "float16", 4, [7000, 6001], [300, 257], dict(softcap=20.0)),
     (128, "bfloat16", 4, [7000, 6001], [300, 257], dict(softcap=300.0, bias=True)), (128, "float16", 2, [9000, 70], [600, 70], dict(bias=True)),
