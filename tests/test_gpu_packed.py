@@ -112,7 +112,7 @@ def test_middling_rows(dim, group, rows, form):
     check_attend(c, out, lse, want=c.attend_at_once())
 
 
-@pytest.mark.parametrize("dim,seqs,longest", [(64, 64, 1500), (128, 33, 1100), (64, 3, 1300), (128, 61, 40), (64, 70, 1200), (64, 40, 2100)])
+@pytest.mark.parametrize("dim,seqs,longest", [(64, 33, 1100), (128, 33, 300), (64, 3, 1300), (128, 61, 40), (64, 70, 100)])
 def test_many_sequences(dim, seqs, longest):
     """Of unlike lengths, whole and in parts, in the order of their lengths and not; equal ones and empty ones among them."""
     say("case sequences", dim, seqs, longest)
