@@ -87,15 +87,15 @@ class _Cached(RowOps):
         self.block_table = block_table
         self.status = torch.zeros(block_table.shape[0], dtype=torch.int32, device=self.device)
 
-    def _finish(self, c):
-        """The library's struct and the sizes in it."""
-        self._c, self._c_ref = c, ctypes.byref(c)
+    def _finish(self, c, store, read):
+        """The library's struct and the sizes in it, its functions for rows."""
+        self._c, self._c_ref, self._store, self._read = c, ctypes.byref(c), store, read
         self.n_seqs, self.kv_heads, self.head_dim = int(c.n_seqs), int(c.kv_heads), int(c.head_dim)
         self.max_len = int(c.max_pages) * int(c.page_tokens)
 
     def _ints(self, t, name, n):
         """Address of a contiguous int32 tensor of n values on the cache's device."""
-        if t.dtype is not self._int32 or t.get_device() != self._index or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        if t.dtype is not self._int32 or t.get_device() != self._index or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous int32 tensor of {n} values on {self.device} is wanted, got {t.dtype} "
                              f"{tuple(t.shape)} on {t.device}")
         return t.data_ptr()
@@ -179,7 +179,7 @@ class PagedCache(_Cached):
         c.k_block_stride, c.k_slot_stride, c.k_head_stride = k.stride()[:3]
         c.v_block_stride, c.v_slot_stride, c.v_head_stride = v.stride()[:3]
         c.d_k, c.d_v, c.d_block_table, c.d_status = k.data_ptr(), v.data_ptr(), block_table.data_ptr(), self.status.data_ptr()
-        self._finish(c)
+        self._finish(c, self._lib.rkc_store, self._lib.rkc_read)
 
     def _account(self, t, name, dtype, max_len):
         """Strides of an account (or of its positions)."""

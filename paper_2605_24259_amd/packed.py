@@ -9,7 +9,8 @@ A claim that is demoted, or a batch too large for the pool, can be held in 17 bi
     k, v = cache.read(row_offset, length, rows=n)                                        # back to 16 bits
 
 The 4 bits are those of the microscaling formats: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, times a power of two for
-each 32 elements of a head.  A head's slot whose key or value has an element that is not finite reads back as NaN.
+each 32 elements of a head.  A head's slot whose key or value has an element that is not finite reads back as NaN.  As with
+``PagedCache``, nothing waits for the GPU, and there are no gradients.
 """
 from __future__ import annotations
 
@@ -55,8 +56,6 @@ class PackedCache(_Cached):
     status       [seqs] int32, as of ``PagedCache``
     """
 
-    _store, _read = "rkc_packed_store", "rkc_packed_read"
-
     @staticmethod
     def pool(blocks, page_tokens, kv_heads, head_dim, device="cuda"):
         """A pool of zeros."""
@@ -87,20 +86,25 @@ class PackedCache(_Cached):
         c.block_stride = pool.stride(0) if c.n_blocks > 1 else 0
         c.head_stride = pool.stride(1) if c.kv_heads > 1 else 0
         c.d_pool, c.d_block_table, c.d_status = pool.data_ptr(), block_table.data_ptr(), self.status.data_ptr()
-        self._finish(c)
+        self._finish(c, self._lib.rkc_packed_store, self._lib.rkc_packed_read)
 
     def attend(self, q, row_offset, length, *, max_rows, max_len=None, scale=None, softcap=0.0, slope=None, prefix=None,
                row_start=None, parent=None, out=None, stream=None):
         """Attention of new rows, whose own keys and values are in the last slots of their sequences already: as
         ``PagedCache.attend``, over the values that the 4 bits stand for.  Returns (out, lse)."""
         head, q_strides, tail = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
-        with self._on(stream):
-            out, lse = self._outputs(q, out)
-            a = _Attention(*head, 1.0, 0, *q_strides, out.stride(0), out.stride(1), 0, 0, *tail, out.data_ptr(), lse.data_ptr())
-            ref = ctypes.byref(a)
-            need = self._lib.rkc_packed_attend_scratch_bytes(self._c_ref, ref)
-            if need:
-                scratch = self._scratch(need)
-                a.d_scratch, a.scratch_bytes = scratch.data_ptr(), need
-            self._call(self._lib.rkc_packed_attend, "rkc_packed_attend", ref, stream)
+        if stream is not None:
+            with self._on(stream):
+                return self._run_attend(q, head, q_strides, tail, out, stream)
+        return self._run_attend(q, head, q_strides, tail, out, None)
+
+    def _run_attend(self, q, head, q_strides, tail, out, stream):
+        out, lse = self._outputs(q, out)
+        a = _Attention(*head, 1.0, 0, *q_strides, out.stride(0), out.stride(1), 0, 0, *tail, out.data_ptr(), lse.data_ptr())
+        ref = ctypes.byref(a)
+        need = self._lib.rkc_packed_attend_scratch_bytes(self._c_ref, ref)
+        if need:
+            scratch = self._scratch(need)
+            a.d_scratch, a.scratch_bytes = scratch.data_ptr(), need
+        self._call(self._lib.rkc_packed_attend, "rkc_packed_attend", ref, stream)
         return out, lse

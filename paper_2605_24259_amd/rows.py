@@ -22,10 +22,8 @@ class _Rows(ctypes.Structure):
 
 
 class RowOps:
-    """``store`` and ``read`` of a cache with the fields of ``PagedCache``; ``_store`` and ``_read`` name the library's
+    """``store`` and ``read`` of a cache with the fields of ``PagedCache``; ``_store`` and ``_read`` are the library's
     functions."""
-
-    _store, _read = "rkc_store", "rkc_read"
 
     def _heads_of(self, t, name, shape):
         """Strides of a tensor of rows, of a dimension of one 0, as they say nothing."""
@@ -35,6 +33,9 @@ class RowOps:
                              f"{t.dtype} {tuple(t.shape)} on {t.device}")
         return at if shape[0] > 1 else 0, heads if shape[1] > 1 else 0
 
+    def _new_rows(self, shape):
+        return self._torch.empty_strided(shape, (self.kv_heads * self.head_dim, self.head_dim, 1), dtype=self.dtype, device=self.device)
+
     def _norm_of(self, t, name, kind):
         if t.dtype is not kind or (kind is not self.dtype and kind is not self._torch.float32) or t.get_device() != self._index or \
                 t.shape != (self.head_dim,) or not t.is_contiguous():
@@ -43,9 +44,9 @@ class RowOps:
         return t.data_ptr()
 
     def _run_rows(self, f, args, stream):
-        st = getattr(self._lib, f)(self._c_ref, ctypes.byref(_Rows(*args)), self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
+        st = f(self._c_ref, ctypes.byref(_Rows(*args)), self._raw_stream(self._index) if stream is None else _stream_ptr(stream))
         if st != 0:
-            raise RkcError(st, f)
+            raise RkcError(st, f.__name__)
 
     def store(self, k, v, row_offset, length, *, q=None, q_norm=None, k_norm=None, eps=1e-6, freq=None, position=None, axis=None,
               interleaved=False, q_out=None, stream=None):
@@ -112,8 +113,11 @@ class RowOps:
             shape = (n, heads, self.head_dim)
             q_at, q_heads = self._heads_of(q, "q", shape)
             if q_out is None:
-                with self._on(stream):
+                if stream is None:  # a context, even an empty one, costs a fifth of a tensor
                     q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                else:
+                    with self._on(stream):
+                        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
                 out_at, out_heads = heads * self.head_dim, self.head_dim
             else:
                 out_at, out_heads = self._heads_of(q_out, "q_out", shape)
@@ -135,12 +139,11 @@ class RowOps:
         """
         shape, torch = (rows, self.kv_heads, self.head_dim), self._torch
         if k is None or v is None:
-            with self._on(stream):
-                strides = (self.kv_heads * self.head_dim, self.head_dim, 1)
-                if k is None:
-                    k = torch.empty_strided(shape, strides, dtype=self.dtype, device=self.device)
-                if v is None:
-                    v = torch.empty_strided(shape, strides, dtype=self.dtype, device=self.device)
+            if stream is not None:
+                with self._on(stream):
+                    k, v = self._new_rows(shape) if k is None else k, self._new_rows(shape) if v is None else v
+            else:
+                k, v = self._new_rows(shape) if k is None else k, self._new_rows(shape) if v is None else v
         k_at, k_heads = self._heads_of(k, "k", shape)
         v_at, v_heads = self._heads_of(v, "v", shape)
         self._run_rows(self._read, (rows, 0, self.max_len, 0, 1, 0, 0, 0.0, k_at, k_heads, v_at, v_heads, 0, 0, 0, 0, k.data_ptr(), v.data_ptr(),
