@@ -336,13 +336,15 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : D == 256 && W == 4 ? 1 : 2) v
 #pragma unroll
         for (int d = 0; d < DB; d++) o[d] = mma(vals(va, x, d), pb[x], o[d]);
     };
-    // operands a few products ahead of their use
-    auto feed = [](int products) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+    // Operands a few products ahead of their use: one read a key, two a value (12 ahead and two of either: 2,048 rows over 32,768
+    // slots 989 us instead of 975, 16 ahead 1,213).
+    auto feed = [](int keys, int values) {
+      __builtin_amdgcn_sched_group_barrier(0x100, D == 256 ? 12 : 6, 0);
 #pragma unroll
-      for (int k = 0; k < products; k++) {
+      for (int k = 0; k < keys + values; k++) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        if (D < 256 && k < keys) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       }
     };
     auto multiply = [&](int i) {
@@ -350,13 +352,13 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : D == 256 && W == 4 ? 1 : 2) v
       if (has && had) {
         scores(sc, i & 1);
         outputs(i - 1);
-        feed(KT * KC + NP * DB);
+        feed(KT * KC, NP * DB);
       } else if (has) {
         scores(sc, i & 1);
-        feed(KT * KC);
+        feed(KT * KC, 0);
       } else if (had) {
         outputs(i - 1);
-        feed(NP * DB);
+        feed(0, NP * DB);
       }
       had = has;
       __builtin_amdgcn_sched_barrier(0);
