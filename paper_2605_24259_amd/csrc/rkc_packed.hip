@@ -4,8 +4,8 @@
 // out = sum_j exp(x_j - m) v_j / sum_j exp(x_j - m), x the masked and capped scores, m their running maximum.  16 packed
 // rows (rows x query heads of one key/value head) are the columns of a 16x16x32 matrix product, and a workgroup has one or two
 // blocks of 16, so that every key and value is read and converted once for all of them.  What bounds the kernel is that read:
-// 5.2 TB/s with 5 sequences of 250,000 to 262,144 slots, 8 heads of 128 elements (268 us; the 16-bit cache's 896), 4.4 TB/s
-// with 64 of 1 to 8,192 (67 us).  With two blocks two waves a SIMD are left, and the vector units' work on the scores counts
+// 5.3 TB/s with 5 sequences of 250,000 to 262,144 slots, 8 heads of 128 elements (266 us; the 16-bit cache's 896), 4.7 TB/s
+// with 64 of 1 to 8,192 (62 us).  With two blocks two waves a SIMD are left, and the vector units' work on the scores counts
 // as much (32 packed rows over 40 sequences of 700 to 8,192 slots: 2.7 TB/s, 81 us).
 // A workgroup takes a chunk of one sequence's slots for one head, its waves take 32 slots at a time:
 //   K  a lane has a quarter of its slot's key (head_dim / 4 elements), which it makes the product's operand of by the

@@ -2,10 +2,12 @@
 //
 // store: y = x w / sqrt(mean(x^2) + eps) for each head of queries and keys, then pairs (a, b) -> (a cos t - b sin t,
 // a sin t + b cos t) with t = frequency x position, in one pass over the rows.  What bounds it is the traffic, 2 bytes an
-// element read and 2 (keys and values in 4 bits: 17/32) written, and for a decode step's few rows a chain of loads.
+// element read and 2 (keys and values in 4 bits: 17/32) written: 13,400 rows of 48 heads of 128 elements 67 us, 4.9 TB/s, 0.94
+// of a large copy's rate; 14,100 into 4 bits 71 us, 4.2 TB/s; and for a decode step's 64 rows a chain of loads, 4.8 and 5.3 us.
 // A lane has 16 elements of a head: the two runs of 8 that turn into each other, so that a rotation needs no other lane.
 // A workgroup has up to 16 rows, whose angles it finds once for all heads.
-// read: the other way, a lane 8 elements of a head's key and value.
+// read: the other way, a lane 8 elements of a head's key and value: 277,000 rows of 4 heads of 256 elements 281 us, 5.1 TB/s,
+// a large copy's rate.
 #include <type_traits>
 
 #include "rkc_packed_dev.h"
