@@ -397,7 +397,7 @@ Cut cut_of(int rows, int most, int64_t turns_of_a_row) {
   while (2 * k.per <= most && rows / (2 * k.per) >= 1024 && k.per * turns_of_a_row < 4 * kWaves) k.per *= 2;
   const int64_t waves = (turns_of_a_row + kWaves - 1) / kWaves;
   if (k.per == 1) k.parts = (int)(1024 / rows < 1 ? 1 : 1024 / rows < waves ? 1024 / rows : waves);
-  k.workgroups = (int64_t)((rows + k.per - 1) / k.per) * k.parts;
+  k.workgroups = ((int64_t)rows + k.per - 1) / k.per * k.parts;
   return k;
 }
 

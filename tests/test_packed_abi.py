@@ -154,7 +154,7 @@ def test_scratch(lib):  # noqa: F811
 def test_too_many_lanes(lib):  # noqa: F811
     """Sizes past what the runtime launches are refused, and smaller ones are not (without a GPU: its error)."""
     on_cpu()
-    _, p, r, a = fine()
+    _, p, _, a = fine()
     p.n_seqs, p.kv_heads, p.max_pages, p.page_tokens, p.head_stride = 1 << 20, 16, 2, 1024, 1024 * 136
     p.block_stride = 16 * p.head_stride
     a.n_rows, a.q_heads, a.max_rows, a.max_len = 1 << 20, 16, 1, 2048
@@ -163,10 +163,19 @@ def test_too_many_lanes(lib):  # noqa: F811
     assert call(lib, "rkc_packed_attend", p, a) == -4
     p.kv_heads = a.q_heads = 1
     assert call(lib, "rkc_packed_attend", p, a) == -6
-    r.n_rows = 0x7fffffff
-    r.d_position, r.d_axis = 0, 0
-    for n in ("rkc_packed_store", "rkc_packed_read"):
-        assert call(lib, n, p, r) == -6
+
+
+@pytest.mark.parametrize("rows,status", [(0x7fffffff, -4), (0x7ffffff0, -4), (1 << 20, -6)])
+def test_too_many_rows(lib, rows, status):  # noqa: F811
+    """A workgroup of 256 lanes has 64 rows at most: 2^31 rows are 2^33 lanes, past the 2^32 of a launch, whatever is added to
+    the rows on the way to their workgroups; 2^20 rows are not (without a GPU: its error)."""
+    on_cpu()
+    c, p, r, _ = fine()
+    r.n_rows, r.q_heads, r.d_position, r.d_axis = rows, 1, 0, 0
+    for heads in (1, 2):
+        c.kv_heads = p.kv_heads = heads
+        for name, x in (("rkc_store", c), ("rkc_read", c), ("rkc_packed_store", p), ("rkc_packed_read", p)):
+            assert call(lib, name, x, r) == status, (name, heads)
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
