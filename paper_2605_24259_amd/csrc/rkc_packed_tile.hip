@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : D == 256 && W == 4 ? 1 : 2) v
     const bool behind = wave >= 4;
     // Where a tile is converted and put, and the one behind it loaded: behind a step's products, which wait for LDS rather than
     // for the wave's instructions; the loads, in scalar instructions for the most part, go with the weights unless a cap makes
-    // those the longer part (the other way round 3 % slower without a cap and 3 % with one).  At 256 elements a head, where some
+    // those the longer part (exchanged, 3 % slower without a cap and with one).  At 256 elements a head, where some
     // registers are kept in memory and are waited for behind the loads, all of it goes before the weights (637 us for 2,048 rows
     // of 16 heads over 16,384 slots, 857 behind the products).
     constexpr bool early = D == 256;
