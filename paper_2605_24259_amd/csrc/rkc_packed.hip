@@ -374,9 +374,15 @@ rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   const int64_t least = p.few && !wide_head ? 512 : grain;
   if (chunk < least) chunk = least;
   if (!p.few && a->max_len <= 512 && (c->head_dim < 256 || units >= 32)) chunk = 512;
-  // Whole sequences, by eight waves, where they are short or as many as the card holds at once: no second kernel for the join
-  // (64 sequences, 8 heads of 128 elements: of 2,500 slots each 42 us, in parts 51; of 4,096 63 and 74).
-  p.waves = M <= 16 && c->head_dim <= 128 && a->max_len <= (units < 512 ? 1536 : 8192) ? 8 : 4;
+  // Whole sequences, by eight waves, need no second kernel for the join.  They pay where they are short, and longer ones where their
+  // units fill rounds of the 512 workgroups that the card holds: one to three quarters, or several (8 heads of 128 elements, all of
+  // 8,192 slots / of 1 to 8,192, in us:  384 units whole 93 / 55, in parts 100 / 62;  480 106 / 61 and 118 / 71;  512 112 / 64 and
+  // 122 / 78;  1,280 262 / 147 and 269 / 155;  but 256 58 / 51 and 72 / 42;  320 89 / 58 and 83 / 55;  520 143 / 80 and 126 / 78;  768 162 / 114
+  // and 171 / 104).  Between such rounds sequences of up to 4,096 slots are as fast either way or faster (520 77 / 45 and 73 / 47; 768
+  // 84 / 62 and 96 / 59; 1,024 111 / 73 and 122 / 79).  A long sequence among short ones, which the host cannot see, takes 6 us for each
+  // 1,000 slots if whole: one of 8,192 among 63 of 100 52 us, in parts 24; of more slots the odds get worse.
+  const int64_t whole = M > 16 || wide_head ? -1 : (units >= 384 && units <= 512) || units >= 1280 ? 8192 : units > 512 ? 4096 : 1536;
+  p.waves = a->max_len <= whole ? 8 : 4;
   if (p.waves == 8) chunk = a->max_len < 32 ? 32 : (a->max_len + 31) / 32 * 32;
   p.chunk = (int)chunk;
   p.splits = (int)((a->max_len + chunk - 1) / chunk);
