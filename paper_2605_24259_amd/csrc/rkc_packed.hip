@@ -347,16 +347,13 @@ rkc_status rkc_packed_few(const rkc_cache* c, const rkc_attention* a, const rkc_
   return c->dtype == RKC_BF16 ? go<__bf16>(c, a, p, s) : go<_Float16>(c, a, p, s);
 }
 
-// Which kernel and how a sequence is cut.  Up to 96 packed rows (trees of up to 32 rows) go to the kernel that reads the cache as
-// fast as it can, 16 or tiles of 32 rows a workgroup, more to the one that keeps the matrix units busy (40 trees over 700 to
-// 8,192 slots, 8 heads of 128 elements: 32 packed rows 81 us, by the other kernel 186; 64 124 and 190; 96 166 and 203; 128 182
-// and 190, of 64 elements 135 and 114).  There 256 rows a workgroup halve what is converted and read of LDS per product, where
-// such tiles, counted with 256 slots each, are twice the card's CUs: fewer leave CUs idle.  A sequence is cut where sequences,
-// heads and row tiles do not fill the card a few times over.
-rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
+// How a sequence is cut for one of the kernels.  That of few rows has 16 rows a workgroup or tiles of 32.  In the other 256 rows a
+// workgroup halve what is converted and read of LDS per product, where such tiles, counted with 256 slots each, are twice the card's
+// CUs: fewer leave CUs idle.  A sequence is cut where sequences, heads and row tiles do not fill the card a few times over.
+static rkc_plan cut_plan(const rkc_cache* c, const rkc_attention* a, bool few) {
   rkc_plan p = {};
   const int64_t G = a->q_heads / c->kv_heads, M = a->max_rows * G;
-  p.few = M <= 32 || (M <= 96 && (!a->d_parent || a->max_rows <= 32));
+  p.few = few;
   const int64_t wide = (int64_t)c->n_seqs * c->kv_heads * ((M + 255) / 256) * ((a->max_len + 255) / 256);
   p.rows = p.few ? (M <= 16 ? 16 : 32) : M <= 128 || c->head_dim == 64 || wide < 512 ? 128 : 256;
   p.tiles = (int)((M + p.rows - 1) / p.rows);
@@ -398,6 +395,32 @@ rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
     p.bytes = (p.stat_at + rows * 8 + 255) & ~(size_t)255;
   }
   return p;
+}
+
+// Nanoseconds of a plan's kernel where all sequences are as long as they may be: rounds of the workgroups that the card holds, each a
+// start and so much for 128 slots.  Fitted to 118 sizes (1 to 64 sequences of 500 to 32,768 slots, 20 to 96 packed rows, both kernels).
+static int64_t cost_of(const rkc_cache* c, const rkc_plan* p) {
+  const int d = c->head_dim == 64 ? 0 : c->head_dim == 128 ? 1 : 2;
+  static const int few[3][2] = {{7400, 750}, {8000, 1700}, {13000, 2000}}, many[3][2] = {{10000, 2400}, {8000, 4000}, {10000, 6400}};
+  const int* of = p->few ? few[d] : many[d];
+  const int64_t held = d == 2 ? 256 : 512, rounds = ((int64_t)p->units * p->splits + held - 1) / held;
+  return rounds * (of[0] + (int64_t)of[1] * p->chunk / 128);
+}
+
+// Which kernel.  Up to 16 packed rows go to the one that reads the cache as fast as it can, more than 96, and trees of more than 32
+// rows, to the one that keeps the matrix units busy.  Between, the first has a tile of 32 rows a workgroup and the second one of 128,
+// a quarter of it empty or more, but reads the cache once: the cheaper by cost_of, a sixteenth in favour of the first, whose smaller parts
+// even out unlike lengths.  (Few rows and many, in us: 64 packed rows of 8 heads of 128 elements, 4 sequences of 500 slots 14 and 20,
+// 64 of 1,000 66 and 43, 64 of 4,096 150 and 135, 8 of 32,768 142 and 145, 40 of 700 to 8,192 123 and 192; 32 rows 14 and 19, 39 and
+// 37, 97 and 123, 99 and 128, 84 and 192; 96 rows 14 and 21, 93 and 46, 196 and 141, 181 and 151, 166 and 202.  Of those 118 sizes
+// none takes more than 1.11 times the other kernel's time.)
+rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
+  const int64_t M = (int64_t)a->max_rows * (a->q_heads / c->kv_heads);
+  if (M <= 16) return cut_plan(c, a, true);
+  const rkc_plan many = cut_plan(c, a, false);
+  if (M > 96 || (a->d_parent && a->max_rows > 32)) return many;
+  const rkc_plan few = cut_plan(c, a, true);
+  return cost_of(c, &few) / 16 * 15 <= cost_of(c, &many) ? few : many;
 }
 
 extern "C" {

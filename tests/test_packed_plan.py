@@ -48,3 +48,37 @@ def test_whole_sequences_go_by_how_full_rounds_are(lib, dim):  # noqa: F811
 
 def test_wide_heads_are_never_whole_by_eight_waves(lib):  # noqa: F811
     assert not any(whole(lib, seqs, 8, 256, n) for seqs in (1, 64, 160) for n in (100, 1536, 8192))
+
+
+
+# sequences, heads, elements of a head, packed rows (in groups of 4), slots, and whether the kernel of few rows was the faster, by a tenth or more
+BETWEEN = [
+    (4, 8, 64, 32, 500, True), (4, 8, 64, 96, 500, True), (64, 8, 64, 48, 1000, False), (64, 8, 64, 96, 1000, False), (16, 8, 64, 96, 4096, False),
+    (1, 8, 64, 20, 32768, True), (1, 8, 64, 96, 32768, False), (8, 8, 64, 32, 32768, True), (8, 8, 64, 96, 32768, False), (64, 8, 64, 32, 4096, True),
+    (64, 8, 64, 96, 4096, False), (40, 8, 64, 32, 8192, True), (40, 8, 64, 64, 8192, True),
+    (4, 8, 128, 20, 500, True), (4, 8, 128, 96, 500, True), (64, 8, 128, 48, 1000, False), (64, 8, 128, 96, 1000, False), (16, 8, 128, 20, 4096, True),
+    (16, 8, 128, 64, 4096, False), (1, 8, 128, 32, 32768, True), (1, 8, 128, 96, 32768, False), (8, 8, 128, 32, 32768, True), (8, 8, 128, 96, 32768, False),
+    (64, 8, 128, 32, 4096, True), (64, 8, 128, 64, 4096, False), (64, 8, 128, 96, 4096, False), (40, 8, 128, 32, 8192, True), (40, 8, 128, 64, 8192, True),
+    (4, 4, 256, 48, 500, True), (4, 4, 256, 96, 500, True), (64, 4, 256, 48, 1000, False), (64, 4, 256, 96, 1000, False), (16, 4, 256, 64, 4096, False),
+    (1, 4, 256, 32, 32768, False), (1, 4, 256, 96, 32768, False), (8, 4, 256, 32, 32768, True), (8, 4, 256, 64, 32768, True), (8, 4, 256, 96, 32768, False),
+    (64, 4, 256, 32, 4096, True), (64, 4, 256, 64, 4096, True), (64, 4, 256, 96, 4096, False), (16, 4, 256, 32, 8192, True),
+    (40, 8, 128, 96, 8192, True), (16, 4, 256, 64, 8192, True)]
+
+
+@pytest.mark.parametrize("seqs,heads,dim,packed,slots,few", BETWEEN)
+def test_the_faster_kernel_is_taken(lib, seqs, heads, dim, packed, slots, few):  # noqa: F811
+    """17 to 96 packed rows, where either kernel may be the faster."""
+    p = plan_of(lib, seqs, heads, dim, 4, packed // 4, slots, tree=True)
+    assert bool(p.few) == few and p.rows == (32 if few else 128) and p.tiles == -(-packed // p.rows)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("seqs,slots", [(1, 1), (4, 500), (64, 1000), (64, 8192), (1, 1 << 20)])
+def test_packed_rows_of_either_kernel(lib, dim, seqs, slots):  # noqa: F811
+    """Up to 16 by the one; more than 96, and trees of more than 32 rows, by the other."""
+    for rows, group in ((1, 1), (1, 16), (16, 1), (4, 4)):
+        p = plan_of(lib, seqs, 8, dim, group, rows, slots, tree=True)
+        assert p.few and p.rows == 16 and p.tiles == 1
+    for rows, group, tree in ((97, 1, False), (1, 97, False), (300, 1, False), (33, 1, True), (48, 2, True), (256, 4, True)):
+        p = plan_of(lib, seqs, 8, dim, group, rows, slots, tree)
+        assert not p.few and p.rows in (128, 256) and p.tiles == -(-rows * group // p.rows)
