@@ -73,6 +73,14 @@ def load():
         vp, i32 = ctypes.c_void_p, ctypes.c_int32
         bp = ctypes.POINTER(Batch)
         lib.rkc_abi_version.restype = i32
+        if lib.rkc_abi_version() != ABI_VERSION:
+            raise RuntimeError(f"{LIB_PATH} implements ABI {lib.rkc_abi_version()}, this binding "
+                               f"ABI {ABI_VERSION}; rebuild the library")
+        from . import cache, packed
+        # functions that were added to the same ABI
+        missing = [n for n in (*EXPORTS, *cache.CACHE_EXPORTS, *packed.PACKED_EXPORTS) if not hasattr(lib, n)]
+        if missing:
+            raise RuntimeError(f"{LIB_PATH} lacks {', '.join(missing)}; rebuild the library")
         lib.rkc_scratch_bytes.argtypes = [bp]
         lib.rkc_scratch_bytes.restype = ctypes.c_size_t
         lib.rkc_replay_batch.argtypes = [bp, vp]
@@ -85,12 +93,8 @@ def load():
         lib.rkc_query_telemetry.restype = ctypes.c_int
         lib.rkc_status_string.argtypes = [ctypes.c_int]
         lib.rkc_status_string.restype = ctypes.c_char_p
-        from . import cache, packed
         cache.declare(lib)
         packed.declare(lib)
-        if lib.rkc_abi_version() != ABI_VERSION:
-            raise RuntimeError(f"{LIB_PATH} implements ABI {lib.rkc_abi_version()}, this binding "
-                               f"ABI {ABI_VERSION}; rebuild the library")
         _lib = lib
     return _lib
 
