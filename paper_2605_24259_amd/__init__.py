@@ -69,6 +69,7 @@ def load():
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is not built; run paper_2605_24259_amd.build.build()")
+        import torch  # noqa: F401  (first: the library is to take the HIP runtime that torch brings, not a second one)
         lib = ctypes.CDLL(LIB_PATH)
         vp, i32 = ctypes.c_void_p, ctypes.c_int32
         bp = ctypes.POINTER(Batch)

@@ -2,7 +2,7 @@
 keeps the plain implementation small.  Tolerances as in test_gpu_cache.py."""
 import numpy as np
 import pytest
-import torch  # (before the library, which takes the HIP runtime that is there)
+import torch
 
 from tests import packed_reference as ref
 from tests.gpu_util import say

@@ -1,5 +1,7 @@
-"""Loading the library: one that is older than the binding is told of as such."""
+"""Loading the library: one that is older than the binding is told of as such, and there is one HIP runtime in the process."""
+import os
 import subprocess
+import sys
 
 import pytest
 
@@ -24,3 +26,12 @@ def test_an_older_library_is_to_be_rebuilt(tmp_path, monkeypatch, version, what)
         rkc.load()
     assert path in str(e.value) and rkc._lib is None
     assert ("ABI 4" in str(e.value)) == (version == 4) and ("lacks rkc_" in str(e.value)) == (version == 5)
+
+
+def test_one_hip_runtime_whatever_comes_first():
+    """The library takes the HIP runtime that torch brings, also where it is loaded before torch: with two in the process, streams
+    and memory of the one mean nothing to the other."""
+    code = ("import paper_2605_24259_amd as rkc\nrkc.load()\nimport torch\n"
+            "print(len({x.split()[-1] for x in open('/proc/self/maps') if 'libamdhip64' in x}))")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    assert subprocess.check_output([sys.executable, "-c", code], text=True, cwd=root).strip() == "1"
