@@ -45,6 +45,7 @@ typedef struct rkc_packed {
 
 /* Rows: host struct.  Rows of sequence s are [d_row_offset[s], d_row_offset[s+1]); with n of them they are those of its last
  * n slots of d_length[s].  Rows behind the last sequence, and those of a sequence told of by RKC_CS_LENGTH, are left alone.
+ * Offsets go up: a sequence whose rows end before they begin is told of, and of rows that two others claim one has them.
  * A row of a block id outside the pool is not stored, and reads block 0 (RKC_CS_BLOCK).
  *
  * Stored rows: a head's queries and keys are multiplied by  norm[i] / sqrt(mean of squares + eps)  where there is a norm, then

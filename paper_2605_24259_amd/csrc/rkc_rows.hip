@@ -42,7 +42,7 @@ __device__ __forceinline__ void cos_sin(int position, float freq, double& c, dou
 }
 
 // The sequence of a row, by the whole wave: of 64 offsets at a time, how many are at most `row`.  Offsets out of order give
-// some sequence, which the caller checks.
+// some sequence that begins at the row or before it, whose end the caller checks.
 __device__ __forceinline__ int seq_of(const int32_t* offset, int n_seqs, int row) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = n_seqs;
@@ -66,16 +66,26 @@ __device__ __forceinline__ void tell(int32_t* status, int s, int bit) {
   if (status && (threadIdx.x & 63) == 0) atomicOr(status + s, bit);
 }
 
+__device__ __forceinline__ bool out_of_limits(const rkc_rows& r, int r0, int r1, int len) {
+  return r0 < 0 || r1 < r0 || r1 > r.n_rows || len < 0 || len > r.max_len || r1 - r0 > len;
+}
+
+// Sequences whose rows or length are out of their limits, by as many workgroups as they need: no row leads to one without rows, or
+// whose offsets go back.  Last in the kernels, where it costs nothing (277,000 rows read 283 us; at their beginning 292).
+template <typename C> __device__ __forceinline__ void tell_lengths(const C& c, const rkc_rows& r) {
+  if (blockIdx.x > (uint32_t)(c.n_seqs - 1) / (64 * kWaves) || !c.d_status) return;
+#pragma unroll 4
+  for (int64_t s = blockIdx.x * 64 * kWaves + threadIdx.x; s < c.n_seqs; s += (int64_t)gridDim.x * 64 * kWaves)
+    if (out_of_limits(r, r.d_row_offset[s], r.d_row_offset[s + 1], r.d_length[s])) atomicOr(c.d_status + s, RKC_CS_LENGTH);
+}
+
 template <typename C> __device__ __forceinline__ Place place_of(const C& c, const rkc_rows& r, int row, bool read) {
   Place p = {-1, 0, 0, 0};
   const int s = seq_of(r.d_row_offset, c.n_seqs, row);
   if (s < 0) return p;
   const int r0 = word(r.d_row_offset, s), r1 = word(r.d_row_offset, s + 1), len = word(r.d_length, s);
   if (row >= r1) return p;  // behind the last sequence
-  if (r0 < 0 || r1 > r.n_rows || len < 0 || len > r.max_len || r1 - r0 > len) {
-    tell(c.d_status, s, RKC_CS_LENGTH);
-    return p;
-  }
+  if (out_of_limits(r, r0, r1, len)) return p;
   p.known = 1;
   p.slot = len - (r1 - row), p.in_page = p.slot & (c.page_tokens - 1);
   const int shift = 31 - __builtin_clz(c.page_tokens), id = word(c.d_block_table, (int64_t)s * c.max_pages + (p.slot >> shift));
@@ -296,6 +306,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(C) == sizeof(rkc_packed) ? 3 : 
       if ((l & 1) == 0) to.scales[to.s_at + (l >> 1)] = (char)ev;
     }
   }
+  tell_lengths(c, r);
 }
 
 template <typename T, int D, typename C>
@@ -339,6 +350,7 @@ __global__ __launch_bounds__(64 * kWaves) void rows_read(const C c, const rkc_ro
       *(u32x4*)((T*)r.d_v + (row0 + i) * r.v_row_stride + h * r.v_head_stride + 8 * l) = x[u][1];
     }
   }
+  tell_lengths(c, r);
 }
 
 bool off16(const void* p) { return (uintptr_t)p & 15; }

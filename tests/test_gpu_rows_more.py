@@ -1,0 +1,108 @@
+"""Rows stored and read: what they tell of, what a bad block reads, rows at the ends of their types.  Tolerances as in test_gpu_rows.py."""
+import numpy as np
+import pytest
+import torch
+
+from tests import packed_reference as ref
+from tests.gpu_util import say
+from tests.test_gpu_cache import ints
+from tests.test_gpu_rows import Rows, bits
+
+pytestmark = pytest.mark.gpu
+
+
+def contents(r, kind):
+    """Clones of what a cache holds."""
+    return [x.clone() for x in ((r.cache.k, r.cache.v) if kind == "cache" else (r.packed.pool,))]
+
+
+@pytest.mark.parametrize("kind", ["cache", "packed"])
+@pytest.mark.parametrize("offset,lens,told", [
+    ([0, 5, 3, 14, 14], [5, 5, 11, 0], [0, 1, 0, 0]),           # back: rows 3 and 4 belong to one of two sequences
+    ([0, 5, 5, 3, 14], [5, 5, 5, 14], [0, 0, 1, 0]),
+    ([0, 14, 14, 14, 14], [14, -1, 1 << 20, 0], [0, 1, 1, 0]),  # lengths of sequences without rows
+    ([-2, 3, 3, 14, 14], [30, 3, 11, 2], [1, 0, 0, 0]),
+    ([0, 3, 3, 12, 15], [3, 3, 9, 20], [0, 0, 0, 1]),           # more rows than there are
+    ([2, 4, 2, 9, 14], [2, 0, 9, 5], [0, 1, 0, 0])])
+def test_sequences_are_told_of(kind, offset, lens, told):
+    """As attention tells of them, whether a row leads to them or not; what is fine is stored, nothing else is written."""
+    say("case told", kind, offset, lens)
+    r = Rows(9, [2, 3, 4, 5], [20, 1, 0, 30], norm=None, rot=0)
+    c, before = getattr(r, kind), contents(r, kind)
+    c.store(r.k, r.v, ints(offset), ints(lens))
+    assert c.status.tolist() == told
+    c.status.zero_()
+    k, v = (torch.full((14, 2, 128), 5.0, dtype=r.dtype, device="cuda") for _ in range(2))
+    c.read(ints(offset), ints(lens), rows=14, k=k, v=v)
+    assert c.status.tolist() == told
+    if kind == "packed":
+        c.status.zero_()
+        c.attend(r.q[:, :2].contiguous(), ints(offset), ints(lens), max_rows=14)
+        assert c.status.tolist() == told
+    # slots that some sequence's rows may have, and those that only one has
+    slots, rows = {}, {}
+    for s in range(4):
+        if not told[s]:
+            for t in range(offset[s], offset[s + 1]):
+                j = lens[s] - (offset[s + 1] - t)
+                slots.setdefault((int(r.table[s, j // 16]), j % 16), []).append(t)
+                rows.setdefault(t, []).append((int(r.table[s, j // 16]), j % 16))
+    for t in range(14):
+        if t not in rows:  # left alone
+            assert k[t].eq(5).all() and v[t].eq(5).all()
+        elif kind == "cache":
+            assert any(bits(c.k[at].contiguous()).equal(bits(r.k[t].contiguous())) for at in rows[t]) and bits(v[t].contiguous()).equal(bits(r.v[t].contiguous()))
+        else:
+            for got, x in ((k, r.k), (v, r.v)):
+                assert got[t].equal(torch.from_numpy(ref.held(x[t].float().cpu().numpy(), r.name)[2]).to(r.dtype).cuda())
+    mine = torch.zeros(c._c.n_blocks, 16, dtype=torch.bool)
+    for at in slots:
+        mine[at] = True
+    mine = mine.cuda()
+    now = contents(r, kind)
+    if kind == "cache":
+        for x, y in zip(now, before):
+            assert bits(x)[~mine].equal(bits(y)[~mine])
+    else:
+        for x, y in zip(ref.split(now[0].cpu().numpy(), 16, 128), ref.split(before[0].cpu().numpy(), 16, 128)):
+            x, y = x.swapaxes(1, 2), y.swapaxes(1, 2)
+            assert np.array_equal(x[~mine.cpu().numpy()], y[~mine.cpu().numpy()])
+
+
+@pytest.mark.parametrize("seqs,bad", [(5000, (0, 63, 64, 700, 4999)), (200, (199,)), (300000, (0, 150000, 299999))])
+def test_many_sequences_without_rows_are_told_of(seqs, bad):
+    say("case many told", seqs)
+    import paper_2605_24259_amd as rkc
+    c = rkc.PackedCache(rkc.PackedCache.pool(2, 16, 1, 64), torch.zeros(seqs, 1, dtype=torch.int32, device="cuda"), page_tokens=16, head_dim=64, dtype=torch.float16)
+    lens = np.zeros(seqs, int)
+    lens[list(bad)] = 17
+    x = torch.zeros(3, 1, 64, dtype=torch.float16, device="cuda")
+    for call in (lambda *at: c.store(x, x, *at), lambda *at: c.read(*at, rows=3)):
+        call(ints(np.zeros(seqs + 1)), ints(lens))
+        assert c.status.nonzero().flatten().tolist() == list(bad) and c.status.max().item() == 1
+        c.status.zero_()
+
+
+@pytest.mark.parametrize("kind", ["cache", "packed"])
+def test_a_bad_block_reads_block_0(kind):
+    """Slots of a block id outside the pool read those of block 0; the sequence's other slots read their own."""
+    say("case block 0", kind)
+    r = Rows(9, [0, 0, 0, 5], [20, 4, 9, 30], norm=None, rot=0)
+    c = getattr(r, kind)
+    x, y = (torch.randn(4, 2, 128, device="cuda").to(r.dtype) for _ in range(2))
+    table = r.table.clone()
+    table[0, 0], table[3] = 0, ints([5, 6, 7])
+    c.block_table.copy_(table)
+    c.store(x, y, ints([0, 4, 4, 4, 4]), ints([4, 4, 9, 35]))  # block 0's slots 0 to 3
+    c.store(r.k, r.v, *r.at())
+    for bad in (c._c.n_blocks, -1, -(1 << 31), (1 << 31) - 1):
+        table[3, 2] = bad
+        c.block_table.copy_(table)
+        c.status.zero_()
+        k, v = c.read(*r.at(), rows=5)
+        assert c.status.tolist() == [0, 0, 0, 2]
+        for got, own, zero in ((k, r.k, x), (v, r.v, y)):
+            want = torch.cat([own[:2], zero[:3]])
+            if kind == "packed":
+                want = torch.from_numpy(ref.held(want.float().cpu().numpy(), r.name)[2]).to(r.dtype).cuda()
+            assert bits(got.contiguous()).equal(bits(want.contiguous())), bad
