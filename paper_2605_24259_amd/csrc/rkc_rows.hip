@@ -130,6 +130,15 @@ template <int L, typename W> __device__ __forceinline__ W sum_of(W x) {
   return x;
 }
 
+// The largest over them.
+template <int L> __device__ __forceinline__ float most_of(float x) {
+  x = fmaxf(x, swapped<0xb1>(x));
+  x = fmaxf(x, swapped<0x4e>(x));
+  if constexpr (L >= 8) x = fmaxf(x, swapped<0x141>(x));
+  if constexpr (L >= 16) x = fmaxf(x, swapped<0x140>(x));
+  return x;
+}
+
 template <typename W> struct Pair { W c, s; };
 template <typename T> struct Run { typename Vec8<T>::t a, b; };  // a lane's two runs of 8 elements
 
@@ -149,7 +158,23 @@ __device__ __forceinline__ void norm_turn(const Run<T>& in, const float* w0, con
     W sum = 0;
 #pragma unroll
     for (int k = 0; k < 16; k++) sum = mad(y[k], y[k], sum);
-    const W by = inverse_root(sum_of<L>(sum) * (W)(1.0 / D) + (W)r.eps);
+    W mean = sum_of<L>(sum) * (W)(1.0 / D) + (W)r.eps;
+    if constexpr (std::is_same<W, float>::value && std::is_same<T, __bf16>::value) {
+      // Squares past the range of 32 bits, or so far below one that bits are lost, which bfloat16 elements may have: the head, and eps
+      // by the square, by the power of two that brings the largest element, or 2^-30 times the root of eps, to 1.
+      if (__builtin_expect(!(mean >= 0x1p-100f && mean < kInf), 0)) {
+        float most = 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; k++) most = fmaxf(most, fabsf(y[k]));
+        int e = __builtin_amdgcn_frexp_expf(most_of<L>(most));
+        if (r.eps > 0.f) e = max(e, __builtin_amdgcn_frexp_expf(r.eps) / 2 - 30);
+        sum = 0;
+#pragma unroll
+        for (int k = 0; k < 16; k++) y[k] = ldexpf(y[k], -e), sum = mad(y[k], y[k], sum);
+        mean = sum_of<L>(sum) * (1.f / D) + ldexpf(r.eps, -2 * e);
+      }
+    }
+    const W by = inverse_root(mean);
 #pragma unroll
     for (int k = 0; k < 8; k++) y[k] = y[k] * by * (W)w0[k], y[8 + k] = y[8 + k] * by * (W)w1[k];
   }

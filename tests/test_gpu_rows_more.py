@@ -106,3 +106,35 @@ def test_a_bad_block_reads_block_0(kind):
             if kind == "packed":
                 want = torch.from_numpy(ref.held(want.float().cpu().numpy(), r.name)[2]).to(r.dtype).cuda()
             assert bits(got.contiguous()).equal(bits(want.contiguous())), bad
+
+
+@pytest.mark.parametrize("size,eps", [(1e25, 1e-6), (1e25, 0.0), (1e38, 1e-6), (1e19, 1e-3), (1e-19, 0.0), (1e-25, 0.0), (1e-25, 1e-12), (1e-38, 0.0),
+                                      (1e-25, 1e-38), (1e-25, 1e-40), (1e-30, 1e-44), (1e-30, 1e10), (1e25, 1e38), (1e-15, 1e-30)])
+@pytest.mark.parametrize("dim,heads", [(64, 5), (128, 3), (256, 2)])
+def test_norms_of_large_and_small_heads(dim, heads, size, eps):
+    """Heads whose squares are past the range of 32 bits, or below it, beside ordinary ones."""
+    say("case norms", dim, size, eps)
+    r = Rows(dim, [5, 1, 11], [3, 0, 20], dim=dim, q_heads=heads, kv_heads=2, norm="f32", rot=32, fused=False)
+    for x in (r.q, r.k):
+        x[::2, 1] = (x[::2, 1].float() * size).clamp(-3e38, 3e38).to(r.dtype)
+        x[1::4, 0] = (x[1::4, 0].float() * size).clamp(-3e38, 3e38).to(r.dtype)
+    r.kw["eps"] = float(np.float32(eps))  # what the call hands on
+    assert np.isfinite(r.wants()[0]).all() and np.isfinite(r.wants()[1]).all()
+    r.check_paged()
+    r.check_packed()
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_norms_of_heads_that_are_not_numbers(eps):
+    """They come out as none, and those beside them as ever; so do heads of zeros without an eps."""
+    say("case norms none", eps)
+    r = Rows(3, [9], [0], dim=128, q_heads=3, kv_heads=2, norm="type", rot=0, fused=False)
+    want = r.cache.store(r.k, r.v, *r.at(), q=r.q, eps=eps, **r.kw).clone()
+    r.q[0, 0, 5], r.q[1, 1, 127], r.q[2, 2, 0] = float("nan"), float("inf"), float("-inf")
+    r.q[3, 0] = 0
+    got = r.cache.store(r.k, r.v, *r.at(), q=r.q, eps=eps, **r.kw)
+    assert got[0, 0].isnan().all() and got[1, 1, 127].isnan() and got[2, 2, 0].isnan() and (got[3, 0].isnan().all() if eps == 0 else got[3, 0].eq(0).all())
+    same = torch.ones(9, 3, dtype=torch.bool, device="cuda")
+    for i, h in ((0, 0), (1, 1), (2, 2), (3, 0)):
+        same[i, h] = False
+    assert bits(got[same]).equal(bits(want[same]))
