@@ -53,7 +53,8 @@ typedef struct rkc_packed {
  * (a, b) becomes (a cos - b sin, a sin + b cos).  The position is that of axis d_axis[j] of the row, of one outside
  * [0, axes) that of axis 0; without d_position the slot's number.  Values, and elements from 2 n_freq on, do not turn.
  * Two rows of one call must not have the same slot.
- * Read rows: d_k and d_v are written; the fields of queries, norm and rotation are not used. */
+ * Read rows: d_k and d_v are written; the fields of queries, norm and rotation are not used.
+ * What is written shares no element with other rows of the call (d_k and d_v read, d_q_out and the rows stored). */
 typedef struct rkc_rows {
   int32_t n_rows;
   int32_t q_heads;     /* where there are queries: any number up to 65536                            */

@@ -21,7 +21,7 @@ import ctypes
 import math
 
 from . import RkcError, _stream_ptr
-from .rows import RowOps
+from .rows import RowOps, moves
 
 MAX_TREE_ROWS = 256
 HEAD_DIMS = (64, 128, 256)
@@ -125,6 +125,8 @@ class _Cached(RowOps):
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != self._index or out.stride(2) != 1:
             raise ValueError("out: a tensor like q, the last dimension contiguous, is wanted")
+        elif moves(q, out):
+            raise RkcError(-3, "out may be q, but not share elements with other rows or heads of it")
         rows, heads, _ = q.shape
         return out, torch.empty_strided((rows, heads), (heads, 1), dtype=torch.float32, device=self.device)
 

@@ -21,6 +21,34 @@ class _Rows(ctypes.Structure):
                                                 "d_axis", "d_freq", "d_q_norm", "d_k_norm")]
 
 
+def share(a, b):
+    """Whether rows a and b, [rows, heads, dim] with the last dimension contiguous, may share elements: found wherever they do,
+    and not where they lie one behind the other, side by side in the rows of one tensor, or head between heads."""
+    if a.untyped_storage().data_ptr() != b.untyped_storage().data_ptr() or not a.numel() or not b.numel():
+        return False
+    (rows, heads, dim), at = a.shape, (b.data_ptr() - a.data_ptr()) // a.element_size()
+    (row, head, _), (row_b, head_b, _) = a.stride(), b.stride()
+    in_row, in_row_b = (heads - 1) * head + dim, (b.shape[1] - 1) * head_b + b.shape[2]
+    if at >= (rows - 1) * row + in_row or -at >= (b.shape[0] - 1) * row_b + in_row_b:
+        return False
+    if rows > 1 and row != row_b or b.shape != a.shape or heads > 1 and head != head_b:
+        return True
+    if rows > 1 and row and in_row <= at % row <= row - in_row_b:
+        return False
+    for n, stride in sorted(((rows, row), (heads, head), (2, abs(at))), key=lambda x: x[1]):  # from the nearest on
+        if n > 1 and stride < dim:
+            return True
+        dim += (n - 1) * stride
+    return False
+
+
+def moves(a, b):
+    """Whether writing what comes of rows a into rows b, of the same shape, may change other rows or heads of a."""
+    if a is b or a.data_ptr() == b.data_ptr() and all(n == 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride())):
+        return False
+    return share(a, b)
+
+
 class RowOps:
     """``store`` and ``read`` of a cache with the fields of ``PagedCache``; ``_store`` and ``_read`` are the library's
     functions."""
@@ -63,7 +91,7 @@ class RowOps:
         position    [rows] or [axes, rows] int32 (default: the rows' slots); up to 8 axes
         axis        [pairs] int32: the axis whose position a pair turns by (time, height, width); with more than one
         interleaved pairs are elements 2 j and 2 j + 1 instead of j and j + pairs
-        q_out       takes the queries; may be q
+        q_out       takes the queries; may be q, and shares no other memory with q, k or v
 
         Returns the queries (q_out or a new tensor), or None without q.  A cache of 4 bits rounds keys and values as they
         are written; keys are computed in 64 bits up to that.
@@ -121,6 +149,8 @@ class RowOps:
                 out_at, out_heads = heads * self.head_dim, self.head_dim
             else:
                 out_at, out_heads = self._heads_of(q_out, "q_out", shape)
+                if moves(q, q_out):
+                    raise RkcError(-3, f"{self._store.__name__}: q_out may be q, but not share elements with other rows or heads of it")
             queries, outs = q.data_ptr(), q_out.data_ptr()
         elif q_norm is not None or q_out is not None:
             raise ValueError("q_norm and q_out are of queries, and there are none")
@@ -138,7 +168,8 @@ class RowOps:
         k, v        take the rows (default: new tensors)
         """
         shape, torch = (rows, self.kv_heads, self.head_dim), self._torch
-        if k is None or v is None:
+        given = k is not None and v is not None
+        if not given:
             if stream is not None:
                 with self._on(stream):
                     k, v = self._new_rows(shape) if k is None else k, self._new_rows(shape) if v is None else v
@@ -146,6 +177,8 @@ class RowOps:
                 k, v = self._new_rows(shape) if k is None else k, self._new_rows(shape) if v is None else v
         k_at, k_heads = self._heads_of(k, "k", shape)
         v_at, v_heads = self._heads_of(v, "v", shape)
+        if given and share(k, v):
+            raise RkcError(-3, f"{self._read.__name__}: k and v share elements")
         self._run_rows(self._read, (rows, 0, self.max_len, 0, 1, 0, 0, 0.0, k_at, k_heads, v_at, v_heads, 0, 0, 0, 0, k.data_ptr(), v.data_ptr(),
                                     None, None, self._ints(row_offset, "row_offset", self.n_seqs + 1), self._ints(length, "length", self.n_seqs)),
                        stream)

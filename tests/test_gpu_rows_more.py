@@ -138,3 +138,48 @@ def test_norms_of_heads_that_are_not_numbers(eps):
     for i, h in ((0, 0), (1, 1), (2, 2), (3, 0)):
         same[i, h] = False
     assert bits(got[same]).equal(bits(want[same]))
+
+
+def test_rows_that_share_memory_are_refused():
+    """What a read writes, and the queries that a store reads and writes elsewhere; tensors side by side are fine."""
+    import paper_2605_24259_amd as rkc
+    r = Rows(1, [4, 3], [4, 9], q_heads=2, kv_heads=2, norm=None, rot=0)
+    at = r.at()
+    for c in (r.cache, r.packed):
+        c.store(r.k, r.v, *at)
+        want = c.read(*at, rows=7)
+        flat, t = torch.zeros(9000, dtype=r.dtype, device="cuda"), torch.zeros(8, 4, 128, dtype=r.dtype, device="cuda")
+        for k, v in ((t[:7, :2], t[:7, :2]), (t[:7, :2], t[1:, :2]), (t[1:, 1:3], t[:7, 2:]), (flat[:7 * 256].view(7, 2, 128), flat[8: 8 + 7 * 256].view(7, 2, 128)),
+                     (flat[:7 * 256].view(7, 2, 128), flat.as_strided((7, 2, 128), (512, 256, 1)))):
+            with pytest.raises(rkc.RkcError, match="share"):
+                c.read(*at, rows=7, k=k, v=v)
+            assert flat.eq(0).all() and t.eq(0).all()
+        pair, outer = (torch.zeros(n, dtype=r.dtype, device="cuda") for n in ((7, 2, 2, 128), (2, 2, 7, 128)))
+        for k, v in ((t[:7, :2], t[:7, 2:]), (t[:7, 2:], t[:7, :2]), (t[:7, ::2], t[:7, 1::2]), (pair[:, :, 1], pair[:, :, 0]), (outer[0].transpose(0, 1), outer[1].transpose(0, 1)),
+                     (outer[:, 0].transpose(0, 1), outer[:, 1].transpose(0, 1)), (flat[:1792].view(7, 2, 128), flat[1792: 3584].view(7, 2, 128))):
+            got = c.read(*at, rows=7, k=k, v=v)
+            assert got[0] is k and got[1] is v and all(bits(a.contiguous()).equal(bits(b)) for a, b in zip(got, want))
+        q = torch.zeros(8, 4, 128, dtype=r.dtype, device="cuda")
+        q[:7, :2] = r.q
+        for out in (q[1:, :2], q[:7, 1:3]):
+            with pytest.raises(rkc.RkcError, match="share"):
+                c.store(r.k, r.v, *at, q=q[:7, :2], q_out=out)
+        assert bits(c.store(r.k, r.v, *at, q=q[:7, :2], q_out=q[:7, 2:]).contiguous()).equal(bits(r.q.contiguous()))
+        assert bits(c.store(r.k, r.v, *at, q=q[:7, :2], q_out=q[:7, :2]).contiguous()).equal(bits(r.q.contiguous()))
+
+
+@pytest.mark.parametrize("kind", ["cache", "packed"])
+def test_outputs_of_attention_that_share_memory_are_refused(kind):
+    """Outputs in the queries' place are fine, beside them too, over other rows or heads of them not."""
+    import paper_2605_24259_amd as rkc
+    r = Rows(1, [4, 3], [4, 9], q_heads=2, kv_heads=2, norm=None, rot=0)
+    c, at = getattr(r, kind), r.at()
+    c.store(r.k, r.v, *at)
+    x = torch.zeros(8, 4, 128, dtype=r.dtype, device="cuda")
+    x[:7, :2] = r.q
+    want = c.attend(x[:7, :2], *at, max_rows=4)[0]
+    for out in (x[1:, :2], x[:7, 1:3]):
+        with pytest.raises(rkc.RkcError, match="share"):
+            c.attend(x[:7, :2], *at, max_rows=4, out=out)
+    assert bits(c.attend(x[:7, :2], *at, max_rows=4, out=x[:7, 2:])[0].contiguous()).equal(bits(want))
+    assert bits(c.attend(x[:7, :2], *at, max_rows=4, out=x[:7, :2])[0].contiguous()).equal(bits(want))
