@@ -84,7 +84,10 @@ rkc_status rkc_read(const rkc_cache* c, const rkc_rows* r, void* s);
 rkc_status rkc_packed_store(const rkc_packed* c, const rkc_rows* r, void* s);
 rkc_status rkc_packed_read(const rkc_packed* c, const rkc_rows* r, void* s);
 
-/* Attention over a cache of 4 bits: as rkc_attend.  There is no account (d_weight_in and d_weight must be NULL). */
+/* Attention over a cache of 4 bits: as rkc_attend.  There is no account (d_weight_in and d_weight must be NULL).
+ * The products' operands have 16 bits, as there.  A value held is one of them (of float16: to the nearest multiple of 2^-24).  The
+ * softmax's weights are rounded to the cache's type where max_rows x query heads of a key/value head is more than 16, and keep twice
+ * its bits up to that; scores, maxima, sums and outputs up to the end are of 32 bits. */
 size_t rkc_packed_attend_scratch_bytes(const rkc_packed* c, const rkc_attention* a);
 rkc_status rkc_packed_attend(const rkc_packed* c, const rkc_attention* a, void* s);
 

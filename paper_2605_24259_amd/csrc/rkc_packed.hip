@@ -9,7 +9,7 @@
 // as much (32 packed rows over 40 sequences of 700 to 8,192 slots: 2.7 TB/s, 81 us).
 // A workgroup takes a chunk of one sequence's slots for one head, its waves take 32 slots at a time:
 //   K  a lane has a quarter of its slot's key (head_dim / 4 elements), which it makes the product's operand of by the
-//      conversion of two codes an instruction, exact with the scale in it;
+//      conversion of two codes an instruction with the scale in it (exact, but for float16 below 2^-24);
 //   V  likewise a quarter of a slot's value, converted and put into the wave's own tile in LDS, from where it is read
 //      transposed (no barriers);
 // both for the next 32 slots are in flight while these are worked on.
@@ -252,7 +252,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 && NB == 2 ? 1 : 2) void pack
       for (int e = 0; e < 8; e++) p[e] = ex2(__builtin_fmaf(sc[n][e >> 2][e & 3], f.post, -m));
       sum[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       // The products' operands have 16 bits.  Of one block a weight is the sum of two of them, with at least twice its bits, as the
-      // matrix units wait for the read anyway; of two it is rounded, as in the kernel of many rows.
+      // matrix units wait for the read anyway; of two it is rounded, as in the kernel of many rows (as the sum of two, 32 packed rows
+      // over 40 sequences of 700 to 8,192 slots 90 us instead of 84, 96 of them 190 instead of 166).
       pb[n] = __builtin_convertvector(p, V8);
       if (NB == 1) pr[n] = __builtin_convertvector(p - __builtin_convertvector(pb[n], f32x8), V8);
     }

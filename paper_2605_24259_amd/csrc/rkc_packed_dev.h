@@ -41,7 +41,8 @@ template <typename V> __device__ __forceinline__ V from_global(const char* p, ui
   return *(const __attribute__((address_space(1))) V*)((const __attribute__((address_space(1))) char*)fixed(p) + (uint32_t)here((int)offset));
 }
 
-// Two codes of a byte as T, times the scale: exact, as a scaled code has two bits of mantissa.
+// Two codes of a byte as T, times the scale: exact, as a scaled code has two bits of mantissa; but for what float16 has no number for,
+// odd multiples of 2^-25 and less, which are rounded to the nearest (halves to even): off by 2^-25 at most.
 template <int BYTE> __device__ __forceinline__ uint32_t unpack2(__bf16, uint32_t codes, float s) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, BYTE));
 }

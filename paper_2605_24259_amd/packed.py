@@ -91,7 +91,8 @@ class PackedCache(_Cached):
     def attend(self, q, row_offset, length, *, max_rows, max_len=None, scale=None, softcap=0.0, slope=None, prefix=None,
                row_start=None, parent=None, out=None, stream=None):
         """Attention of new rows, whose own keys and values are in the last slots of their sequences already: as
-        ``PagedCache.attend``, over the values that the 4 bits stand for.  Returns (out, lse)."""
+        ``PagedCache.attend``, over the values that the 4 bits stand for.  Returns (out, lse).  As there, the softmax's weights are
+        rounded to the cache's type where more than 16 rows (``max_rows`` times the query heads of a key/value head) share a key."""
         head, q_strides, tail = self._attention(q, row_offset, length, max_rows, max_len, scale, softcap, slope, prefix, row_start, parent)
         if stream is not None:
             with self._on(stream):

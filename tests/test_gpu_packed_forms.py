@@ -207,3 +207,45 @@ def test_256_rows_captured_and_on_other_streams(lib):  # noqa: F811
         torch.cuda.synchronize()
         for (a, b), r in zip(got, runs):
             assert torch.equal(a, r[2][0]) and torch.equal(b, r[2][1]), turn
+
+
+@pytest.mark.parametrize("dtype,top", [("bfloat16", 252), ("float16", 140)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_every_code_and_scale(dtype, top, dim):
+    """Read as the nearest value of the 16-bit type, of two as near the even one: the value itself but for float16 below 2^-24.
+    (Half of 2^-24, an odd multiple of it and the like are no float16 numbers.)"""
+    import paper_2605_24259_amd as rkc
+    say("case codes", dtype, dim)
+    f, page = getattr(torch, dtype), 256
+    code = (np.arange(dim)[None, None, None] * 7 + np.arange(page)[None, None, :, None]) % 16
+    scale = np.minimum(np.arange(page), top - 1)[None, None, :, None] + 1 + np.zeros((1, 1, 1, dim // 32), int)
+    parts = [x.astype(np.uint8) for x in (code, (code + 5) % 16, scale, scale[:, :, ::-1])]
+    pool = torch.from_numpy(ref.joined(*parts)).cuda()
+    c = rkc.PackedCache(pool, ints([[0]]), page_tokens=page, head_dim=dim, dtype=f)
+    at = ints([0, page]), ints([page])
+    inexact = 0
+    for got, codes, scales in zip(c.read(*at, rows=page), (parts[0], parts[1]), (parts[2], parts[3])):
+        value = torch.from_numpy(ref.values(codes[0, 0], scales[0, 0]))
+        want = value.to(f)  # of 64 bits, rounded once
+        assert bits_of(got[:, 0].cpu()).equal(bits_of(want))
+        inexact += int((want.double() != value).sum())
+        assert dtype == "float16" or torch.equal(want.double(), value)
+        assert (want.double() - value).abs().max() <= 2.0 ** -25
+    assert (inexact > 0) == (dtype == "float16")
+    # and attention over them, a query that sees them all: scores of the values themselves are off by 2^-25 sum |q| at most
+    g = torch.Generator().manual_seed(dim)
+    q = (torch.randn(1, 2, dim, generator=g) * 1e-4).to(f)
+    k, v = (torch.from_numpy(ref.values(a[0, 0], b[0, 0])) for a, b in ((parts[0], parts[2]), (parts[1], parts[3])))
+    k[150:], v[:100] = 0, 0
+    parts[2][:, :, 150:], parts[0][:, :, 150:], parts[1][:, :, :100] = 1, 0, 0  # the ordinary and the smallest
+    c.pool.copy_(torch.from_numpy(ref.joined(*parts)))
+    out, lse = c.attend(q.cuda(), ints([0, 1]), ints([page]), max_rows=1)
+    s = q[0].double() @ k.T / dim ** 0.5
+    p = torch.softmax(s, 1)
+    assert (lse[0].double().cpu() - torch.logsumexp(s, 1)).abs().max() <= 2.0 ** -20 * (8 + float(s.abs().max())) + 2.0 ** -25 * float(q.double().abs().sum(-1).max())
+    want, half = p @ v, 2.0 ** -8 if dtype == "bfloat16" else 2.0 ** -11
+    assert (out[0].double().cpu() - want).abs().max() <= half * float(want.abs().max()) + 2.0 ** -20 * (8 + float(s.abs().max())) * float((p @ v.abs()).max()) + 2.0 ** -24
+
+
+def bits_of(x):
+    return x.contiguous().view(torch.int16)
