@@ -2,12 +2,13 @@
 //
 // store: y = x w / sqrt(mean(x^2) + eps) for each head of queries and keys, then pairs (a, b) -> (a cos t - b sin t,
 // a sin t + b cos t) with t = frequency x position, in one pass over the rows.  What bounds it is the traffic, 2 bytes an
-// element read and 2 (keys and values in 4 bits: 17/32) written: 13,400 rows of 48 heads of 128 elements 67 us, 4.9 TB/s, 0.94
-// of a large copy's rate; 14,100 into 4 bits 71 us, 4.2 TB/s; and for a decode step's 64 rows a chain of loads, 4.8 and 5.3 us.
+// element read and 2 (keys and values in 4 bits: 17/32) written: 13,400 rows of 48 heads of 128 elements 65 us over inputs that no
+// cache has, 5.0 TB/s, 0.98 of a large copy's rate; 14,100 into 4 bits 72 us, 4.2 TB/s; and for a decode step's 64 rows a chain of loads,
+// 4.8 and 5.6 us.
 // A lane has 16 elements of a head: the two runs of 8 that turn into each other, so that a rotation needs no other lane.
 // A workgroup has up to 16 rows, whose angles it finds once for all heads.
-// read: the other way, a lane 8 elements of a head's key and value: 277,000 rows of 4 heads of 256 elements 281 us, 5.1 TB/s,
-// a large copy's rate.
+// read: the other way, a lane 8 elements of a head's key and value: 277,000 rows of 4 heads of 256 elements of 4 bits 283 us, 5.1 TB/s,
+// a large copy's rate; 258,000 of 16 bits 407 us, 5.2 TB/s.
 #include <type_traits>
 
 #include "rkc_packed_dev.h"
@@ -420,8 +421,8 @@ rkc_status rows_check(const rkc_rows* r, int n_seqs, int64_t cap, int heads, int
 }
 
 // Rows of a workgroup, and workgroups that share them: as many rows, up to `most`, as give its waves four turns and leave four
-// workgroups a CU, and a few rows' heads over as many workgroups.  (13,000 rows of 48 heads of 128 elements stored, 4 rows a
-// workgroup: 60.7 us; 2 rows 72, 8 rows 63.6, 16 rows 71.)
+// workgroups a CU, and a few rows' heads over as many workgroups.  (13,400 rows of 48 heads of 128 elements stored over
+// and over, their inputs in the last cache in part, 4 rows a workgroup: 60.7 us; 2 rows 72, 8 rows 63.6, 16 rows 71.)
 // Reading, a workgroup has the rows whose heads its lanes take at once, twice: fewer rows are all start, and more keep their
 // loads waiting for the stores before them (277,000 rows of 4 heads of 256 elements, 4 rows: 281 us; 2 rows 369, 8 rows 292,
 // 64 rows 325; 157,000 of 8 heads of 64, 8 rows: 104; 4 rows 126, 16 rows 109).
