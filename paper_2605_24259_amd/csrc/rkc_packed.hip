@@ -414,7 +414,8 @@ static int64_t cost_of(const rkc_cache* c, const rkc_plan* p) {
 // even out unlike lengths.  (Few rows and many, in us: 64 packed rows of 8 heads of 128 elements, 4 sequences of 500 slots 14 and 20,
 // 64 of 1,000 66 and 43, 64 of 4,096 150 and 135, 8 of 32,768 142 and 145, 40 of 700 to 8,192 123 and 192; 32 rows 14 and 19, 39 and
 // 37, 97 and 123, 99 and 128, 84 and 192; 96 rows 14 and 21, 93 and 46, 196 and 141, 181 and 151, 166 and 202.  Of those 118 sizes
-// none takes more than 1.11 times the other kernel's time.)
+// none takes more than 1.11 times the other kernel's time.  Of 60 others, drawn from 1 to 200 sequences of up to 58,000 slots, what is
+// chosen takes 1.03 times the faster kernel's time in the geometric mean and 1.40 at most; all by the first 1.11 and 2.1.)
 rkc_plan rkc_packed_plan(const rkc_cache* c, const rkc_attention* a) {
   const int64_t M = (int64_t)a->max_rows * (a->q_heads / c->kv_heads);
   if (M <= 16) return cut_plan(c, a, true);
